@@ -330,6 +330,129 @@ int bf1_decode_attn(const void* Q, const void* K_pages, const void* V_pages, con
                     void* workspace, int64_t workspace_bytes, void* stream);
 
 /*
+ * The operators around a served sequence's cache.
+ *
+ * A step of a batch of sequences appends new_lens[b] tokens to sequence b, which
+ * holds seq_lens[b] already.  The step's rows (queries, keys, values) are packed,
+ * sequence after sequence.  Sequences keep their place in the batch; an empty place
+ * has both numbers 0.
+ *
+ * bf1_page_step: the page table, slot map and positions of a step, in one launch.
+ *   seq_lens, new_lens : [batch] int32 (negative counts as 0)
+ *   page_table         : [batch, max_pages_per_seq] int32, updated in place: every
+ *                        block that gets its first token gets the next free page
+ *   free_pages         : [num_free] int32, taken in order from entry *free_head
+ *   seq_lens_out       : [batch] int32, the lengths after the step
+ *   token_start        : [batch + 1] int32, first row of each sequence (the sum of
+ *                        new_lens before it)
+ *   block_start        : [batch + 1] int32, the number of blocks that sequences
+ *                        before it write to in this step
+ *   positions, slots   : [max_tokens] int32 / int64; of row i: its token's position,
+ *                        and page * B + position % B.  Both are -1 for rows behind
+ *                        the last sequence and for tokens without a place.
+ *   free_head_out      : [1] int32
+ * A token has no place if its position is past the table or 2^31 - 1, its row
+ * past max_tokens, or no free page is left for its block; the tokens behind it in
+ * its sequence have none either, and seq_lens_out counts only those that have one
+ * (block_start likewise).  The caller sees it by comparing the lengths; nothing is
+ * taken from the free list for it.  Outputs are distinct from inputs:
+ * seq_lens_out == seq_lens or new_lens and free_head_out == free_head are refused.
+ * B in {64, 128}, max_tokens < 2^31.
+ */
+int bf1_page_step(int32_t batch, const int32_t* seq_lens, const int32_t* new_lens, int32_t* page_table,
+                  int32_t max_pages_per_seq, const int32_t* free_pages, int32_t num_free, const int32_t* free_head,
+                  int32_t B, int64_t max_tokens, int32_t* seq_lens_out, int32_t* token_start, int32_t* block_start,
+                  int32_t* positions, int64_t* slots, int32_t* free_head_out, void* stream);
+
+/*
+ * Rotary positions of queries and keys, in one launch.  Pair i of a head, i <
+ * rot_dim / 2, at position p turns by the angle p * freqs[i]:
+ *     (x, y) -> amplitude * (x cos - y sin, y cos + x sin)
+ * where the pair is elements i and i + rot_dim / 2, or with `interleaved` 2 i and
+ * 2 i + 1; elements from rot_dim on are copied.  `transposed` turns the other way:
+ * the gradient of the inputs from the gradient of the outputs.
+ *   Q, K      : bf16 or fp32 (in_type), any strides over batch, head and token,
+ *               elements of a head side by side; either may have 0 heads
+ *   positions : int32, [n], or one row per batch entry (positions_batch_stride >= n);
+ *               any value, also negative
+ *   freqs     : [rot_dim / 2] double, radians per position
+ *   Q_out, K_out : out_type: in_type, or bf16 of fp32; may be the inputs themselves
+ *               (same type and strides), otherwise do not overlap them
+ *   strides   : HOST int64[12], in elements: batch, head, token of Q, Q_out, K, K_out
+ * Angles are formed in double precision and the turn in fp32, rounded once.  Even
+ * head_dim <= 1024 and rot_dim; sixteen bytes at a time where strides, addresses and
+ * rot_dim are multiples of what 16 bytes hold, element by element otherwise.
+ */
+typedef enum { BF1_TYPE_BF16 = 0, BF1_TYPE_F32 = 1 } bf1_type;
+
+int bf1_rope(const void* Q, const void* K, const int32_t* positions, int64_t positions_batch_stride,
+             const double* freqs, void* Q_out, void* K_out, int32_t batch, int64_t n, int32_t Hq, int32_t Hkv,
+             int32_t head_dim, int32_t rot_dim, int32_t in_type, int32_t out_type, int32_t interleaved, float amplitude,
+             int32_t transposed, const int64_t* strides, void* stream);
+
+/*
+ * A step's keys and values into the bf16 cache of bf1_decode_attn.
+ *   K, V  : rows [tokens, Hkv, head_dim] bf16, 16-byte aligned, strides of token and
+ *           head in elements (multiples of 8)
+ *   slots : [tokens] int64; a row whose slot is negative or past the cache is left
+ *           out.  The slots of one call are distinct.
+ *   K_pages, V_pages : [num_pages, Hkv, B, head_dim] bf16
+ */
+int bf1_kv_append(const void* K, const void* V, int64_t k_token_stride, int64_t k_head_stride, int64_t v_token_stride,
+                  int64_t v_head_stride, const int64_t* slots, void* K_pages, void* V_pages, int64_t tokens,
+                  int32_t num_pages, int32_t Hkv, int32_t head_dim, int32_t B, void* stream);
+
+/*
+ * The cache in 8 bits.  A block that is complete is a page of 8-bit codes with one
+ * fp32 scale per kv-head for K and one for V; the block of a sequence's newest
+ * token stays in bf16, in the sequence's tail, until it is complete too, so that
+ * every value is rounded once.
+ *   K_pages : [num_pages, Hkv, B, head_dim], V_pages : [num_pages, Hkv, head_dim, B]
+ *             (keys side by side), codes of `format`; 16-byte aligned
+ *   K_scale, V_scale : [num_pages, Hkv] fp32; a code stands for scale * code
+ *   K_tail, V_tail   : [batch, Hkv, B, head_dim] bf16, 16-byte aligned
+ * Formats: BF1_Q8_E4M3 (1-4-3 floating point, largest 448; the scale is the least
+ * power of two that holds the block's largest magnitude) and BF1_Q8_INT8 (scale =
+ * largest magnitude / 127).  Codes are rounded to the nearest, ties to even.  A
+ * block below 2^-100 everywhere is stored as zeros with scale 1.  A block that
+ * holds a NaN or an infinity gets scale NaN and codes 0: its keys make NaN of every
+ * output that reads them.
+ *
+ * bf1_kv_append_q8: a step's rows K, V (as bf1_kv_append's, `tokens` of them) into
+ * the cache; seq_lens_before, seq_lens (after the step), token_start, block_start and
+ * page_table are bf1_page_step's.  Blocks that the step completes are quantised
+ * (their earlier rows come from the tail), then the rows of the block of each
+ * sequence's newest token go to its tail; tails of sequences without new tokens, and
+ * all other pages, are left as they were.  Rows behind the last sequence are not read.
+ * The pages that a step completes are distinct.
+ */
+typedef enum { BF1_Q8_E4M3 = 0, BF1_Q8_INT8 = 1 } bf1_q8_format;
+
+int bf1_kv_append_q8(const void* K, const void* V, int64_t k_token_stride, int64_t k_head_stride,
+                     int64_t v_token_stride, int64_t v_head_stride, int64_t tokens, int32_t batch,
+                     const int32_t* seq_lens_before, const int32_t* seq_lens, const int32_t* token_start,
+                     const int32_t* block_start, const int32_t* page_table, int32_t max_pages_per_seq,
+                     int32_t num_pages, void* K_pages, void* V_pages, float* K_scale, float* V_scale, void* K_tail,
+                     void* V_tail, int32_t Hkv, int32_t head_dim, int32_t B, int32_t format, void* stream);
+
+/*
+ * bf1_decode_attn over the 8-bit cache: the same step with the same plan
+ * (bf1_decode_plan); earlier pages are read in 8 bits, keys j*B .. t from the tail.
+ * Stale and unplannable sequences get NaN, foreign plan rows stay inside the cache,
+ * rows of the tail past t are masked exactly, as there.  The page of block j itself
+ * is not read.  Weights are applied with 16 bits, sums are fp32; deterministic.
+ * workspace: at least bf1_decode_q8_workspace_size() bytes, 16-byte aligned (none is
+ * needed, and it may be NULL, where that is 0).  Supported as bf1_decode_attn.
+ */
+int bf1_decode_q8_workspace_size(int32_t batch, int32_t Hq, int32_t Hkv, int32_t head_dim, int32_t B,
+                                 int32_t plan_stride, int64_t* bytes);
+int bf1_decode_attn_q8(const void* Q, const void* K_pages, const void* V_pages, const float* K_scale,
+                       const float* V_scale, const void* K_tail, const void* V_tail, const int32_t* seq_lens,
+                       int32_t num_pages, const int32_t* plan, int32_t plan_stride, void* O, float* LSE, int32_t batch,
+                       int32_t Hq, int32_t Hkv, int32_t head_dim, int32_t B, int32_t format, void* workspace,
+                       int64_t workspace_bytes, void* stream);
+
+/*
  * Key split of the forward kernels (bf1_attn_fwd, bf1_attn_fwd_noalloc,
  * bf1_attn_fwd_csr, bf1_dense_causal_fwd), process-wide:
  *   0  automatic (the default): when a launch has at most one work item (one

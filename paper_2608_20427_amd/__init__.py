@@ -13,13 +13,17 @@ h // (Hq // Hkv).  Block width ``B`` (tokens per block) and local width
 """
 
 import ctypes
+import math
 import os
+from typing import NamedTuple
 
 __all__ = [
     "BF1Error", "lib_path", "load", "version", "status_string", "plan_size", "plan",
     "attn_fwd", "attn_fwd_csr", "dense_causal_fwd", "release_plans", "selected_flops",
     "plan_transposed", "bwd_workspace_size", "attn_bwd", "selected_bwd_flops", "attn_fwd_noalloc",
     "set_forward_key_split",
+    "PageStep", "page_step", "rope_freqs", "rope", "rope_bwd", "kv_append", "CacheQ8", "cache_q8", "kv_append_q8",
+    "decode_q8_workspace_size", "attn_decode_q8",
 ]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -108,6 +112,21 @@ def load():
     lib.bf1_decode_attn.restype = ctypes.c_int
     lib.bf1_decode_attn.argtypes = [vp, vp, vp, vp, i32, vp, i32, vp, vp, i32, i32, i32, i32, i32, vp,
                                     i64, vp]
+    lib.bf1_page_step.restype = ctypes.c_int
+    lib.bf1_page_step.argtypes = [i32, vp, vp, vp, i32, vp, i32, vp, i32, i64, vp, vp, vp, vp, vp, vp, vp]
+    lib.bf1_rope.restype = ctypes.c_int
+    lib.bf1_rope.argtypes = [vp, vp, vp, i64, vp, vp, vp, i32, i64, i32, i32, i32, i32, i32, i32, i32, f32, i32,
+                             ctypes.POINTER(i64), vp]
+    lib.bf1_kv_append.restype = ctypes.c_int
+    lib.bf1_kv_append.argtypes = [vp, vp, i64, i64, i64, i64, vp, vp, vp, i64, i32, i32, i32, i32, vp]
+    lib.bf1_kv_append_q8.restype = ctypes.c_int
+    lib.bf1_kv_append_q8.argtypes = [vp, vp, i64, i64, i64, i64, i64, i32, vp, vp, vp, vp, vp, i32, i32, vp, vp, vp,
+                                     vp, vp, vp, i32, i32, i32, i32, vp]
+    lib.bf1_decode_q8_workspace_size.restype = ctypes.c_int
+    lib.bf1_decode_q8_workspace_size.argtypes = [i32, i32, i32, i32, i32, i32, ctypes.POINTER(i64)]
+    lib.bf1_decode_attn_q8.restype = ctypes.c_int
+    lib.bf1_decode_attn_q8.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, i32, vp, i32, vp, vp, i32, i32, i32, i32, i32,
+                                       i32, vp, i64, vp]
     _LIB = lib
     return lib
 
@@ -490,4 +509,324 @@ def attn_decode(q, k_pages, v_pages, seq_lens, plan, B=64, out=None, lse=None, w
     except BF1Error:  # refused before anything is launched; a small workspace is a ValueError
         check_workspace(workspace, "workspace", decode_workspace_size(batch, Hq, Hkv, d, stride), dev)
         raise
+    return out, lse
+
+
+# ---- a served sequence's cache ------------------------------------------------
+#
+# One step of a batch: page_step places the new tokens, rope turns their queries and
+# keys, kv_append or kv_append_q8 writes the cache, decode_plan and attn_decode or
+# attn_decode_q8 read it.  A step's rows are packed, sequence after sequence; a sequence
+# keeps its place in the batch.
+
+def _empty(shape, dtype, device, stream):
+    """An output or scratch tensor whose memory belongs to the stream it is used on."""
+    import torch
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+class PageStep(NamedTuple):
+    """What page_step writes: the lengths after the step [batch], the first row
+    [batch + 1] and the blocks written before [batch + 1] of every sequence, the
+    position [max_tokens] and slot [max_tokens] of every row (-1: no token, or none
+    that has a place), and the free list's new head [1]."""
+    seq_lens: object
+    token_start: object
+    block_start: object
+    positions: object
+    slots: object
+    free_head: object
+
+
+def page_step(seq_lens, new_lens, page_table, free_pages, free_head, max_tokens, B=64, out=None, stream=None):
+    """Page table, slot map and positions of a step that appends new_lens[b] tokens
+    to sequence b of seq_lens[b] tokens; returns a PageStep (`out`, if given).
+
+    page_table [batch, max_pages] is updated in place: a block that gets its first
+    token takes the next page of free_pages, from entry free_head[0] on.  All are
+    int32; slots are int64, page * B + position % B, and index the cache of
+    kv_append.  max_tokens (host) bounds the step's rows, so that no length has to
+    come back from the GPU.  A token without a free page, past the table or past
+    max_tokens has no place, nor do those behind it in its sequence: the returned
+    seq_lens count what was placed."""
+    import torch
+    _i32_cuda(seq_lens, "seq_lens", 1)
+    dev = seq_lens.device
+    _i32_cuda(page_table, "page_table", 2, dev)
+    batch, max_pages = page_table.shape
+    check_buffer(seq_lens, "seq_lens", (batch,), torch.int32, dev)
+    check_buffer(new_lens, "new_lens", (batch,), torch.int32, dev)
+    _i32_cuda(free_pages, "free_pages", 1, dev)
+    check_buffer(free_head, "free_head", (1,), torch.int32, dev)
+    max_tokens = int(max_tokens)
+    if max_tokens < 0:
+        raise ValueError("max_tokens must not be negative")
+    sizes = (batch, batch + 1, batch + 1, max_tokens, max_tokens, 1)
+    if out is None:
+        words = batch + 2 * (batch + 1) + max_tokens + 1
+        pad = (words + 1) & ~1  # slots are 8-byte entries behind the others
+        buf = _empty((pad + 2 * max_tokens,), torch.int32, dev, stream)
+        a, b, c, d, e, slots = buf.split((batch, batch + 1, batch + 1, max_tokens, 1 + pad - words, 2 * max_tokens))
+        out = PageStep(a, b, c, d, slots.view(torch.int64), e[:1])
+    else:
+        out = PageStep(*out)
+        for name, t, size in zip(PageStep._fields, out, sizes):
+            check_buffer(t, name, (size,), torch.int64 if name == "slots" else torch.int32, dev)
+    _call(load().bf1_page_step, "bf1_page_step", dev, stream, batch, _ptr(seq_lens), _ptr(new_lens), _ptr(page_table),
+          max_pages, _ptr(free_pages), free_pages.shape[0], _ptr(free_head), int(B), max_tokens, _ptr(out.seq_lens),
+          _ptr(out.token_start), _ptr(out.block_start), _ptr(out.positions), _ptr(out.slots), _ptr(out.free_head))
+    return out
+
+
+ROPE_SCALINGS = ("none", "linear", "base", "bands")
+
+
+def rope_freqs(rot_dim, theta=1e6, scaling="none", factor=1.0, original_len=32768, slow=1.0, fast=32.0, device=None):
+    """(freqs, amplitude) for rope: float64 [rot_dim / 2] radians per position on
+    `device` (None: the current CUDA device), theta^(-2 i / rot_dim), for contexts
+    `factor` times as long as the original ones:
+      "linear"  positions are divided by factor;
+      "base"    theta grows by factor^(rot_dim / (rot_dim - 2)), so that the slowest
+                pair slows down by factor and the fastest stays;
+      "bands"   pairs that turn less than `slow` times over original_len tokens slow
+                down by factor, those that turn more than `fast` times stay, the others
+                are blended; queries and keys grow by amplitude 0.1 ln(factor) + 1
+                (YaRN, arXiv 2309.00071, section 3)."""
+    import torch
+    if rot_dim < 2 or rot_dim % 2:
+        raise ValueError("rot_dim must be even and positive")
+    if scaling not in ROPE_SCALINGS:
+        raise ValueError(f"unknown scaling {scaling!r}; one of {ROPE_SCALINGS}")
+    if not (theta > 0 and factor >= 1 and original_len > 0 and fast > slow > 0):
+        raise ValueError("rope_freqs needs theta > 0, factor >= 1, original_len > 0 and fast > slow > 0")
+    if scaling == "base" and rot_dim > 2:
+        theta = theta * factor ** (rot_dim / (rot_dim - 2))
+    f = theta ** (-torch.arange(0, rot_dim, 2, dtype=torch.float64) / rot_dim)
+    amplitude = 1.0
+    if scaling == "linear":
+        f = f / factor
+    elif scaling == "bands":
+        turns = original_len * f / (2 * math.pi)
+        keep = ((turns - slow) / (fast - slow)).clamp(0, 1)
+        f = f * keep + f / factor * (1 - keep)
+        amplitude = 0.1 * math.log(factor) + 1
+    dev = torch.device("cuda", torch.cuda.current_device()) if device is None else device
+    return f.to(dev), amplitude
+
+
+def _rope_side(x, name, dim, lead, d, dtype, dev, out, out_dtype, stream):
+    """Check one of q, k and its output; returns (out, heads, six strides)."""
+    import torch
+    if not isinstance(x, torch.Tensor) or x.device != dev or x.dtype != dtype or x.dim() != dim:
+        raise ValueError(f"{name} must be a {dim}-D {dtype} tensor on {dev}")
+    shape = x.shape
+    rows = (1, shape[0]) if dim == 3 else (shape[0], shape[2])
+    if rows != lead or shape[-1] != d:
+        raise ValueError(f"{name} must agree with the other operand in every size but the heads")
+    if x.stride(-1) != 1:
+        raise ValueError(f"{name} must have the elements of a head side by side")
+    if out is None:
+        out = _empty(shape, out_dtype, dev, stream)
+    else:
+        check_buffer(out, name + "_out", shape, out_dtype, dev)
+    s, o = x.stride(), out.stride()
+    if dim == 3:  # rows [tokens, heads, d]
+        return out, shape[1], (0, s[1], s[0], 0, o[1], o[0])
+    return out, shape[1], (s[0], s[1], s[2], o[0], o[1], o[2])
+
+
+def _rope(q, k, positions, freqs, interleaved, amplitude, transposed, q_out, k_out, dtype, stream):
+    import torch
+    x = q if q is not None else k
+    dev = _cuda_device(x, "q" if q is not None else "k")
+    dim = x.dim()
+    if dim not in (3, 4) or x.dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError("q and k must be bf16 or float32, [batch, heads, n, d] or rows [tokens, heads, d]")
+    if dtype is None:
+        dtype = x.dtype
+    if dtype is not x.dtype and dtype is not torch.bfloat16:
+        raise ValueError(f"dtype must be {x.dtype} or bfloat16")
+    d = x.shape[-1]
+    batch, n = lead = (1, x.shape[0]) if dim == 3 else (x.shape[0], x.shape[2])
+    Hq = Hkv = 0
+    qs = ks = (0,) * 6
+    if q is not None:
+        q_out, Hq, qs = _rope_side(q, "q", dim, lead, d, x.dtype, dev, q_out, dtype, stream)
+    if k is not None:
+        k_out, Hkv, ks = _rope_side(k, "k", dim, lead, d, x.dtype, dev, k_out, dtype, stream)
+    if not isinstance(positions, torch.Tensor) or (positions.shape != (n,) and (dim == 3 or positions.shape != lead)):
+        raise ValueError(f"positions must have shape ({n},)" + (f" or ({batch}, {n})" if dim == 4 else ""))
+    check_buffer(positions, "positions", positions.shape, torch.int32, dev)
+    if not isinstance(freqs, torch.Tensor) or freqs.dim() != 1 or not 1 <= freqs.shape[0] <= d // 2:
+        raise ValueError("freqs must be a 1-D tensor of at most d / 2 entries")
+    check_buffer(freqs, "freqs", freqs.shape, torch.float64, dev)
+    _call(load().bf1_rope, "bf1_rope", dev, stream, _ptr(q), _ptr(k), _ptr(positions),
+          n if positions.dim() == 2 else 0, _ptr(freqs), _ptr(q_out), _ptr(k_out), batch, n, Hq, Hkv, d,
+          2 * freqs.shape[0], 0 if x.dtype is torch.bfloat16 else 1, 0 if dtype is torch.bfloat16 else 1,
+          int(bool(interleaved)), float(amplitude), transposed, (ctypes.c_int64 * 12)(*qs, *ks))
+    return q_out, k_out
+
+
+def rope(q, k, positions, freqs, interleaved=False, amplitude=1.0, q_out=None, k_out=None, dtype=None, stream=None):
+    """Rotary positions of queries and keys in one launch; returns (q_out, k_out),
+    contiguous tensors of the inputs' shapes.
+
+    q, k: [batch, heads, n, d] (any strides with the elements of a head side by side, so
+    a view of joined projections is split on the way) or a step's rows [tokens, heads,
+    d]; bf16 or float32; either may be None.  positions: int32 [n] or [batch, n].
+    freqs, amplitude: rope_freqs'; the first 2 * len(freqs) elements of a head are
+    turned, in pairs (i, i + len(freqs)) or, interleaved, (2 i, 2 i + 1); the others
+    are copied.  q_out and k_out may be the inputs where those are contiguous."""
+    if q is None and k is None:
+        raise ValueError("rope needs q or k")
+    return _rope(q, k, positions, freqs, interleaved, amplitude, 0, q_out, k_out, dtype, stream)
+
+
+def rope_bwd(dq, dk, positions, freqs, interleaved=False, amplitude=1.0, dq_out=None, dk_out=None, dtype=None,
+             stream=None):
+    """Gradients of rope's inputs from those of its outputs: the transposed turn.
+    Arguments as rope's; dtype=torch.bfloat16 rounds float32 gradients on the way."""
+    if dq is None and dk is None:
+        raise ValueError("rope_bwd needs dq or dk")
+    return _rope(dq, dk, positions, freqs, interleaved, amplitude, 1, dq_out, dk_out, dtype, stream)
+
+
+def _step_rows(k, v, Hkv, d, dev):
+    """Check a step's rows k, v [tokens, Hkv, d] (strided rows and heads)."""
+    import torch
+    for name, x in (("k", k), ("v", v)):
+        if not isinstance(x, torch.Tensor) or x.device != dev or x.dtype != torch.bfloat16 or x.dim() != 3:
+            raise ValueError(f"{name} must be a bf16 tensor [tokens, Hkv, d] on {dev}")
+        if x.shape[0] != k.shape[0] or x.shape[1] != Hkv or x.shape[2] != d or x.stride(2) != 1:
+            raise ValueError(f"{name} must have shape ({k.shape[0]}, {Hkv}, {d}) with the elements of a head side by side")
+    return k.shape[0], (k.stride(0), k.stride(1), v.stride(0), v.stride(1))
+
+
+def kv_append(k, v, slots, k_pages, v_pages, stream=None):
+    """Write a step's rows k, v [tokens, Hkv, d] bf16 into the bf16 pages
+    [num_pages, Hkv, B, d] of attn_decode at page_step's slots; rows with a negative
+    slot, or one past the cache, are left out.  Slots are distinct."""
+    import torch
+    dev = _cuda_device(k_pages, "k_pages")
+    if k_pages.dim() != 4:
+        raise ValueError("k_pages must be a 4-D tensor [num_pages, Hkv, B, d]")
+    num_pages, Hkv, B, d = k_pages.shape
+    check_buffer(k_pages, "k_pages", k_pages.shape, torch.bfloat16, dev)
+    check_buffer(v_pages, "v_pages", k_pages.shape, torch.bfloat16, dev)
+    tokens, strides = _step_rows(k, v, Hkv, d, dev)
+    check_buffer(slots, "slots", (tokens,), torch.int64, dev)
+    _call(load().bf1_kv_append, "bf1_kv_append", dev, stream, _ptr(k), _ptr(v), *strides, _ptr(slots), _ptr(k_pages),
+          _ptr(v_pages), tokens, num_pages, Hkv, d, B)
+
+
+class CacheQ8(NamedTuple):
+    """The 8-bit cache: pages of codes (int8, or e4m3 as torch.float8_e4m3fn), K
+    [num_pages, Hkv, B, d] and V [num_pages, Hkv, d, B] with keys side by side; float32
+    scales [num_pages, Hkv]; and the newest block of every sequence in bf16, tails
+    [batch, Hkv, B, d].  cache_q8 makes one."""
+    k_pages: object
+    v_pages: object
+    k_scale: object
+    v_scale: object
+    k_tail: object
+    v_tail: object
+
+
+def cache_q8(num_pages, batch, Hkv, d=128, B=64, dtype=None, device=None):
+    """An empty CacheQ8 for `batch` sequences over `num_pages` pages; dtype:
+    torch.float8_e4m3fn (default) or torch.int8."""
+    import torch
+    dtype = torch.float8_e4m3fn if dtype is None else dtype
+    if dtype not in (torch.float8_e4m3fn, torch.int8):
+        raise ValueError("dtype must be torch.float8_e4m3fn or torch.int8")
+    dev = torch.device("cuda", torch.cuda.current_device()) if device is None else device
+    pages = [torch.zeros(s, dtype=torch.int8, device=dev).view(dtype)
+             for s in ((num_pages, Hkv, B, d), (num_pages, Hkv, d, B))]
+    scales = [torch.ones((num_pages, Hkv), dtype=torch.float32, device=dev) for _ in range(2)]
+    tails = [torch.zeros((batch, Hkv, B, d), dtype=torch.bfloat16, device=dev) for _ in range(2)]
+    return CacheQ8(*pages, *scales, *tails)
+
+
+def _cache_q8(cache, batch):
+    """Check a CacheQ8 for `batch` sequences; returns (device, num_pages, Hkv, B, d,
+    format)."""
+    import torch
+    kp, vp, ks, vs, kt, vt = cache
+    dev = _cuda_device(kp, "k_pages")
+    if kp.dim() != 4 or kp.dtype not in (torch.float8_e4m3fn, torch.int8):
+        raise ValueError("k_pages must be an int8 or float8_e4m3fn tensor [num_pages, Hkv, B, d]")
+    num_pages, Hkv, B, d = kp.shape
+    check_buffer(kp, "k_pages", kp.shape, kp.dtype, dev)
+    check_buffer(vp, "v_pages", (num_pages, Hkv, d, B), kp.dtype, dev)
+    check_buffer(ks, "k_scale", (num_pages, Hkv), torch.float32, dev)
+    check_buffer(vs, "v_scale", (num_pages, Hkv), torch.float32, dev)
+    check_buffer(kt, "k_tail", (batch, Hkv, B, d), torch.bfloat16, dev)
+    check_buffer(vt, "v_tail", (batch, Hkv, B, d), torch.bfloat16, dev)
+    return dev, num_pages, Hkv, B, d, 1 if kp.dtype is torch.int8 else 0
+
+
+def kv_append_q8(k, v, lens_before, seq_lens, token_start, block_start, page_table, cache, stream=None):
+    """Write a step's rows k, v [tokens, Hkv, d] bf16 into a CacheQ8: blocks that the
+    step completes are quantised into their pages, the rows of each sequence's newest
+    block go to its tail.  lens_before: the lengths page_step was given; seq_lens,
+    token_start and block_start: what it returned; page_table: what it updated."""
+    import torch
+    _i32_cuda(page_table, "page_table", 2)
+    batch, max_pages = page_table.shape
+    dev, num_pages, Hkv, B, d, fmt = _cache_q8(cache, batch)
+    check_buffer(page_table, "page_table", page_table.shape, torch.int32, dev)
+    check_buffer(lens_before, "lens_before", (batch,), torch.int32, dev)
+    check_buffer(seq_lens, "seq_lens", (batch,), torch.int32, dev)
+    check_buffer(token_start, "token_start", (batch + 1,), torch.int32, dev)
+    check_buffer(block_start, "block_start", (batch + 1,), torch.int32, dev)
+    tokens, strides = _step_rows(k, v, Hkv, d, dev)
+    _call(load().bf1_kv_append_q8, "bf1_kv_append_q8", dev, stream, _ptr(k), _ptr(v), *strides, tokens, batch,
+          _ptr(lens_before), _ptr(seq_lens), _ptr(token_start), _ptr(block_start), _ptr(page_table), max_pages,
+          num_pages, *map(_ptr, cache), Hkv, d, B, fmt)
+
+
+def decode_q8_workspace_size(batch, Hq, Hkv, head_dim, B, stride):
+    out = ctypes.c_int64(0)
+    _check(load().bf1_decode_q8_workspace_size(int(batch), int(Hq), int(Hkv), int(head_dim), int(B), int(stride),
+                                               ctypes.byref(out)), "bf1_decode_q8_workspace_size")
+    return out.value
+
+
+def attn_decode_q8(q, cache, seq_lens, plan, B=64, out=None, lse=None, workspace=None, stream=None):
+    """attn_decode over a CacheQ8, with the same plan: earlier pages in 8 bits, the
+    newest block from the tail; returns (O [batch, Hq, d] bf16, LSE [batch, Hq]
+    fp32)."""
+    import torch
+    dev = _cuda_device(q, "q")
+    if q.dim() != 3:
+        raise ValueError("q must be 3-D [batch, Hq, d]")
+    batch, Hq, d = q.shape
+    check_buffer(q, "q", q.shape, torch.bfloat16, dev)
+    where, num_pages, Hkv, pw, dk, fmt = _cache_q8(cache, batch)
+    if where != dev or dk != d or pw != B:
+        raise ValueError("the cache must have q's device and head size, and pages of B tokens")
+    _i32_cuda(seq_lens, "seq_lens", 1, dev)
+    _i32_cuda(plan, "plan", 2, dev)
+    if seq_lens.shape[0] != batch or plan.shape[0] != batch:
+        raise ValueError("batch sizes disagree")
+    if out is None:
+        out = _empty(q.shape, torch.bfloat16, dev, stream)
+    else:
+        check_buffer(out, "out", q.shape, torch.bfloat16, dev)
+    if lse is None:
+        lse = _empty((batch, Hq), torch.float32, dev, stream)
+    else:
+        check_buffer(lse, "lse", (batch, Hq), torch.float32, dev)
+    stride = plan.shape[1]
+    need = decode_q8_workspace_size(batch, Hq, Hkv, d, B, stride)
+    if workspace is None:
+        workspace = _empty((need,), torch.uint8, dev, stream) if need else None
+        ws_bytes = need
+    else:
+        ws_bytes = check_workspace(workspace, "workspace", need, dev)
+    _call(load().bf1_decode_attn_q8, "bf1_decode_attn_q8", dev, stream, _ptr(q), *map(_ptr, cache), _ptr(seq_lens),
+          num_pages, _ptr(plan), stride, _ptr(out), _ptr(lse), batch, Hq, Hkv, d, int(B), fmt, _ptr(workspace), ws_bytes)
     return out, lse

@@ -47,6 +47,8 @@ def build(verbose=False, extra_hip_flags=()):
     b_obj = os.path.join(BUILD, "bf1_bwd.o")
     d_obj = os.path.join(BUILD, "bf1_decode.o")
     s_obj = os.path.join(BUILD, "bf1_stack.o")
+    c_obj = os.path.join(BUILD, "bf1_cache.o")
+    q_obj = os.path.join(BUILD, "bf1_decode_q8.o")
     a_obj = os.path.join(BUILD, "bf1_api.o")
     _run([hipcc, *HIP_FLAGS, *extra_hip_flags, "-c", os.path.join(CSRC, "bf1_kernels.hip"),
           "-o", k_obj], verbose)
@@ -56,9 +58,13 @@ def build(verbose=False, extra_hip_flags=()):
           "-o", d_obj], verbose)
     _run([hipcc, *HIP_FLAGS, *extra_hip_flags, "-c", os.path.join(CSRC, "bf1_stack.hip"),
           "-o", s_obj], verbose)
+    _run([hipcc, *HIP_FLAGS, *extra_hip_flags, "-c", os.path.join(CSRC, "bf1_cache.hip"),
+          "-o", c_obj], verbose)
+    _run([hipcc, *HIP_FLAGS, *extra_hip_flags, "-c", os.path.join(CSRC, "bf1_decode_q8.hip"),
+          "-o", q_obj], verbose)
     _run([gxx, *HOST_FLAGS, "-c", os.path.join(CSRC, "bf1_api.cpp"), "-o", a_obj], verbose)
     tmp = LIB + ".tmp"
-    _run([hipcc, f"--offload-arch={ARCH}", "-shared", "-fPIC", k_obj, b_obj, d_obj, s_obj, a_obj,
+    _run([hipcc, f"--offload-arch={ARCH}", "-shared", "-fPIC", k_obj, b_obj, d_obj, s_obj, c_obj, q_obj, a_obj,
           "-o", tmp,
           f"-L{ROCM}/lib", "-lamdhip64", f"-Wl,-rpath,{ROCM}/lib"], verbose)
     os.replace(tmp, LIB)

@@ -1,0 +1,738 @@
+// What a decode step needs around its attention, for gfx950: page tables and
+// slot maps from request lengths, rotary positions (and their transpose for
+// gradients), and the writers of the paged key/value cache, in bf16 and in 8
+// bits with one scale per block and kv-head.  Each is one launch.
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include "../../include/bf1.h"
+#include "bf1_device.h"
+
+namespace bf1 {
+namespace {
+
+constexpr int THREADS = 256;
+
+int status_of(hipError_t e) { return e == hipSuccess ? BF1_OK : BF1_ERR_HIP; }
+bool aligned(const void* p, uintptr_t a) { return p != nullptr && reinterpret_cast<uintptr_t>(p) % a == 0; }
+// A launch has fewer than 2^32 threads.
+bool launchable(int64_t blocks) { return blocks < (int64_t(1) << 32) / THREADS; }
+
+// Exclusive prefix sum of x over the workgroup in thread order; *total gets the
+// sum.  `part` is one slot per wave; ends with the slots free for the next call.
+template <typename T>
+__device__ __forceinline__ T group_scan(T x, T* part, T* total) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    T inc = x;
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) {
+        const T y = __shfl_up(inc, m);
+        if (lane >= m) inc += y;
+    }
+    if (lane == 63) part[wave] = inc;
+    __syncthreads();
+    T before = 0, all = 0;
+#pragma unroll
+    for (int w = 0; w < THREADS / 64; ++w) {
+        if (w < wave) before += part[w];
+        all += part[w];
+    }
+    __syncthreads();
+    *total = all;
+    return before + inc - x;
+}
+
+// ---------------------------------------------------------------------------
+// Page tables and slot maps of a step
+// ---------------------------------------------------------------------------
+// Sequence b holds old = seq_lens[b] tokens and gets want = new_lens[b]; the rows
+// of the step are packed, sequence after sequence.  Three prefix sums over the
+// batch give each sequence its first row (of want), its first free page (of the
+// pages it needs) and its first touched block; a row then finds its sequence by
+// binary search.  A new page starts with a new token, so the row of that token
+// writes the table entry, and no row reads an entry that this launch writes.
+//
+// Bound by latency: 20 bytes per sequence and 12 per row.  Every workgroup sums
+// the batch for itself (SEQS sequences at a time), so that one launch does it.
+constexpr int SPT = 4;                // sequences per thread and round
+constexpr int SEQS = THREADS * SPT;
+constexpr int ROWS_PER_GROUP = 1024;  // rows of a workgroup
+
+__device__ __forceinline__ int32_t clamp_i32(int64_t x) { return x > INT32_MAX ? INT32_MAX : (int32_t)x; }
+
+__global__ __launch_bounds__(THREADS) void page_step_kernel(
+    int32_t batch, const int32_t* __restrict__ seq_lens, const int32_t* __restrict__ new_lens, int32_t* page_table,
+    int32_t max_pages, const int32_t* __restrict__ free_pages, int32_t num_free, const int32_t* __restrict__ free_head,
+    int32_t shift, int64_t max_tokens, int32_t* __restrict__ lens_out, int32_t* __restrict__ token_start,
+    int32_t* __restrict__ block_start, int32_t* __restrict__ positions, int64_t* __restrict__ slots,
+    int32_t* __restrict__ head_out) {
+    __shared__ int64_t part64[THREADS / 64];
+    __shared__ int32_t part32[THREADS / 64];
+    __shared__ int32_t s_start[SEQS];   // first row
+    __shared__ int32_t s_old[SEQS], s_placed[SEQS], s_rank[SEQS];
+    const int tid = threadIdx.x;
+    const bool writer = blockIdx.x == 0;  // the per-sequence results
+    const int64_t t0 = (int64_t)blockIdx.x * ROWS_PER_GROUP;
+    const int64_t t1 = min(max_tokens, t0 + ROWS_PER_GROUP);
+    const int32_t B = 1 << shift;
+    const int64_t head = min(max(*free_head, 0), num_free);
+    const int64_t room = min((int64_t)max_pages << shift, (int64_t)INT32_MAX);
+    int64_t rows = 0, pages = 0;  // sums over the sequences before this round
+    int32_t blocks = 0, taken = 0;
+    for (int32_t b0 = 0; b0 < batch; b0 += SEQS) {
+        int64_t old[SPT], want[SPT], w_sum = 0;
+#pragma unroll
+        for (int i = 0; i < SPT; ++i) {
+            const int32_t b = b0 + tid * SPT + i;
+            old[i] = b < batch ? max(seq_lens[b], 0) : 0;
+            want[i] = b < batch ? max(new_lens[b], 0) : 0;
+            w_sum += want[i];
+        }
+        int64_t w_all, n_all;
+        int64_t row = rows + group_scan(w_sum, part64, &w_all);
+        int64_t fit[SPT], need[SPT], n_sum = 0;
+        int64_t at = row;
+#pragma unroll
+        for (int i = 0; i < SPT; ++i) {
+            fit[i] = max((int64_t)0, min(min(want[i], room - old[i]), max_tokens - at));
+            at += want[i];
+            need[i] = fit[i] > 0 ? ((old[i] + fit[i] + B - 1) >> shift) - ((old[i] + B - 1) >> shift) : 0;
+            n_sum += need[i];
+        }
+        int64_t rank = pages + group_scan(n_sum, part64, &n_all);
+        int32_t b_sum = 0, g_sum = 0;
+        int32_t touched[SPT];
+        int64_t rk = rank;
+        at = row;
+#pragma unroll
+        for (int i = 0; i < SPT; ++i) {
+            const int64_t have = (old[i] + B - 1) >> shift;
+            const int64_t got = min(max(num_free - head - rk, (int64_t)0), need[i]);
+            const int64_t placed = need[i] > got ? max(min(fit[i], ((have + got) << shift) - old[i]), (int64_t)0) : fit[i];
+            touched[i] = placed > 0 ? (int32_t)(((old[i] + placed - 1) >> shift) - (old[i] >> shift) + 1) : 0;
+            b_sum += touched[i];
+            g_sum += (int32_t)got;
+            const int s = tid * SPT + i;
+            s_start[s] = clamp_i32(at);
+            s_old[s] = (int32_t)old[i];
+            s_placed[s] = (int32_t)placed;
+            s_rank[s] = clamp_i32(head + rk);
+            rk += need[i];
+            at += want[i];
+        }
+        int32_t b_all, g_all;
+        int32_t blk = blocks + group_scan(b_sum, part32, &b_all);
+        group_scan(g_sum, part32, &g_all);
+        if (writer) {
+#pragma unroll
+            for (int i = 0; i < SPT; ++i) {
+                const int32_t s = tid * SPT + i, b = b0 + s;
+                if (b < batch) {
+                    lens_out[b] = s_old[s] + s_placed[s];
+                    token_start[b] = s_start[s];
+                    block_start[b] = blk;
+                }
+                blk += touched[i];
+            }
+        }
+        // the rows of this round's sequences among this workgroup's
+        const int64_t lo = max(t0, rows), hi = min(t1, rows + w_all);
+        const int32_t count = min(SEQS, batch - b0);
+        for (int64_t t = lo + tid; t < hi; t += THREADS) {
+            int32_t s = 0;  // the last sequence that starts at or before row t
+            for (int32_t step = SEQS / 2; step > 0; step >>= 1)
+                if (s + step < count && s_start[s + step] <= t) s += step;
+            const int64_t i = t - s_start[s];
+            int32_t pos = -1;
+            int64_t slot = -1;
+            if (i < s_placed[s]) {
+                pos = s_old[s] + (int32_t)i;
+                const int32_t block = pos >> shift;
+                const int32_t have = (int32_t)(((int64_t)s_old[s] + B - 1) >> shift);
+                int32_t* entry = page_table + (int64_t)(b0 + s) * max_pages + block;
+                int32_t page;
+                if (block < have) {
+                    page = *entry;
+                } else {
+                    page = free_pages[s_rank[s] + (block - have)];
+                    if ((pos & (B - 1)) == 0) *entry = page;
+                }
+                if (page >= 0) slot = ((int64_t)page << shift) + (pos & (B - 1));
+            }
+            positions[t] = pos;
+            slots[t] = slot;
+        }
+        rows += w_all;
+        pages += n_all;
+        blocks += b_all;
+        taken += g_all;
+        if (!writer && rows >= t1) return;
+        __syncthreads();  // before the next round's sequences take their places
+    }
+    for (int64_t t = max(t0, rows) + tid; t < t1; t += THREADS) {
+        positions[t] = -1;
+        slots[t] = -1;
+    }
+    if (writer && tid == 0) {
+        token_start[batch] = clamp_i32(rows);
+        block_start[batch] = blocks;
+        *head_out = (int32_t)head + taken;
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Rotary positions
+// ---------------------------------------------------------------------------
+// The pair (a, b) of frequency i at position p turns by the angle p * freqs[i]:
+// (a c - b s, b c + a s) with c, s the amplitude times cosine and sine.  The
+// gradient turns the other way (the rotation is orthogonal): `sign` = -1.  Pairs
+// are i and i + rot / 2, or (interleaved) 2 i and 2 i + 1; dims from rot on are
+// copied.  The angle is formed in 64 bits and reduced to a part of a turn there,
+// so that far positions lose nothing; cosine and sine are fp32.
+//
+// A lane owns P pairs of one token, 16 bytes of each half of the head, and walks
+// over heads with its cosines and sines in registers.
+struct RopeSide {
+    const void* in;
+    void* out;
+    int64_t ib, ih, it;  // strides of batch, head and token, in elements
+    int64_t ob, oh, ot;
+    int32_t heads;
+};
+
+template <typename T, int N>
+__device__ __forceinline__ void load_n(const T* p, float* f) {
+    if constexpr (N * sizeof(T) == 16 && sizeof(T) == 2) {
+        const u32x4 w = *reinterpret_cast<const u32x4*>(p);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            f[2 * k] = __uint_as_float(w[k] << 16);
+            f[2 * k + 1] = __uint_as_float(w[k] & 0xffff0000u);
+        }
+    } else if constexpr (N * sizeof(T) == 16) {
+        const f32x4 w = *reinterpret_cast<const f32x4*>(p);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) f[k] = w[k];
+    } else {
+#pragma unroll
+        for (int k = 0; k < N; ++k) f[k] = (float)p[k];
+    }
+}
+
+template <typename T, int N>
+__device__ __forceinline__ void store_n(T* p, const float* f) {
+    if constexpr (sizeof(T) == 2 && N == 8) {
+        bf16x8 v;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = (__bf16)f[k];
+        *reinterpret_cast<bf16x8*>(p) = v;
+    } else if constexpr (sizeof(T) == 2 && N == 4) {
+        bf16x4 v;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = (__bf16)f[k];
+        *reinterpret_cast<bf16x4*>(p) = v;
+    } else if constexpr (sizeof(T) == 4 && N == 4) {
+        *reinterpret_cast<f32x4*>(p) = f32x4{f[0], f[1], f[2], f[3]};
+    } else {
+#pragma unroll
+        for (int k = 0; k < N; ++k) p[k] = (T)f[k];
+    }
+}
+
+template <typename TI, typename TO, bool INTER, int P>
+__global__ __launch_bounds__(THREADS) void rope_kernel(RopeSide q, RopeSide k, const int32_t* __restrict__ positions,
+                                                       int64_t pos_batch, const double* __restrict__ freqs,
+                                                       uint32_t items, uint32_t n, uint32_t lanes, int32_t half,
+                                                       float amplitude, float sign) {
+    constexpr int E = INTER ? 2 * P : P;  // elements of one load
+    const uint32_t item = blockIdx.x * THREADS + threadIdx.x;
+    if (item >= items) return;
+    const uint32_t row = item / lanes, l = item - row * lanes;  // row: token of the batch
+    const uint32_t b = row / n, t = row - b * n;
+    const bool turn = (int32_t)(l * P) < half;
+    float c[P], s[P];
+    int32_t lo, hi = 0;  // element offsets in the head row
+    if (turn) {
+        const double p = (double)positions[b * pos_batch + t] * 0.15915494309189535;  // in turns: 1 / (2 pi)
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+            const double x = p * freqs[l * P + i];
+            float cs, sn;
+            sincospif(2.f * (float)(x - rint(x)), &sn, &cs);
+            c[i] = cs * amplitude;
+            s[i] = sn * (sign * amplitude);
+        }
+        lo = l * E;
+        hi = half + l * P;
+    } else {
+        lo = 2 * half + (int32_t)(l - half / P) * E;
+    }
+    for (int32_t h = blockIdx.y; h < q.heads + k.heads; h += gridDim.y) {
+        const bool isk = h >= q.heads;
+        const RopeSide& x = isk ? k : q;
+        const int32_t g = isk ? h - q.heads : h;
+        const TI* src = (const TI*)x.in + b * x.ib + g * x.ih + t * x.it;
+        TO* dst = (TO*)x.out + b * x.ob + g * x.oh + t * x.ot;
+        if (!turn) {
+            float v[E];
+            load_n<TI, E>(src + lo, v);
+            store_n<TO, E>(dst + lo, v);
+        } else if constexpr (INTER) {
+            float v[E], y[E];
+            load_n<TI, E>(src + lo, v);
+#pragma unroll
+            for (int i = 0; i < P; ++i) {
+                y[2 * i] = v[2 * i] * c[i] - v[2 * i + 1] * s[i];
+                y[2 * i + 1] = v[2 * i + 1] * c[i] + v[2 * i] * s[i];
+            }
+            store_n<TO, E>(dst + lo, y);
+        } else {
+            float a[P], d[P], ya[P], yd[P];
+            load_n<TI, P>(src + lo, a);
+            load_n<TI, P>(src + hi, d);
+#pragma unroll
+            for (int i = 0; i < P; ++i) {
+                ya[i] = a[i] * c[i] - d[i] * s[i];
+                yd[i] = d[i] * c[i] + a[i] * s[i];
+            }
+            store_n<TO, P>(dst + lo, ya);
+            store_n<TO, P>(dst + hi, yd);
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Rows into bf16 pages
+// ---------------------------------------------------------------------------
+// One lane per 16 bytes of a row of K or V; a row without a slot is left out.
+__global__ __launch_bounds__(THREADS) void kv_append_kernel(
+    const __bf16* __restrict__ k, const __bf16* __restrict__ v, int64_t kt, int64_t kh, int64_t vt, int64_t vh,
+    const int64_t* __restrict__ slots, __bf16* __restrict__ k_pages, __bf16* __restrict__ v_pages, int64_t items,
+    int32_t heads, int32_t dshift, int32_t shift, int64_t num_slots) {
+    const int64_t item = (int64_t)blockIdx.x * THREADS + threadIdx.x;
+    if (item >= items) return;
+    const int32_t cshift = dshift - 3;  // 16-byte chunks of a head row
+    const int64_t x = item >> cshift;
+    const int32_t c = (int32_t)(item & ((1 << cshift) - 1)) * 8;
+    const int64_t t = x / heads;
+    const int32_t h = (int32_t)(x - t * heads);
+    const int64_t slot = slots[t];
+    if (slot < 0 || slot >= num_slots) return;
+    const int64_t page = slot >> shift, off = slot & ((1 << shift) - 1);
+    const int64_t dst = ((((page * heads + h) << shift) + off) << dshift) + c;
+    *reinterpret_cast<u32x4*>(k_pages + dst) = *reinterpret_cast<const u32x4*>(k + t * kt + h * kh + c);
+    *reinterpret_cast<u32x4*>(v_pages + dst) = *reinterpret_cast<const u32x4*>(v + t * vt + h * vh + c);
+}
+
+// ---------------------------------------------------------------------------
+// Rows into 8-bit pages
+// ---------------------------------------------------------------------------
+// A block is quantised once, when its last token is there: until then its rows
+// are bf16 in the sequence's tail, so that no value is rounded twice and a scale
+// never changes.  Scale of a (block, kv-head), K and V apart, from the largest
+// magnitude a: e4m3, the least power of two with a <= 448 scale (codes are then
+// x / scale exactly, rounded once); int8, a / 127, codes 127 x / a rounded to
+// even.  A block below 2^-100 everywhere is zeros under scale 1; one with a NaN or an
+// infinity gets scale NaN, so that it shows.
+//
+// One workgroup per (touched block, kv-head).  A lane holds four consecutive keys
+// of 8 dims, so that V, which pages hold with keys side by side (the attention's
+// operand as it stands), is turned in registers and goes out through LDS.  The
+// workgroup of a sequence's first touched block also writes the tail, after it has
+// read it.
+struct QuantE4m3 {
+    static constexpr bool INT8 = false;
+};
+struct QuantInt8 {
+    static constexpr bool INT8 = true;
+};
+
+constexpr uint32_t TINY_BITS = 0x0D80;  // bf16 bits of 2^-100
+
+// How a block of largest magnitude `bits` (bf16, without sign) is coded.
+struct Coding {
+    float scale;  // what a code stands for
+    int32_t e;    // the power of two to divide by first
+    float a;      // int8: the largest magnitude after that, in [1, 2)
+    float inv;    // int8: about 1 / a
+    bool zero;
+};
+
+template <class F>
+__device__ __forceinline__ Coding coding(uint32_t bits) {
+    Coding q;
+    const float amax = __uint_as_float(bits << 16);
+    q.zero = bits < TINY_BITS;
+    const int32_t ex = (int32_t)(bits >> 7) - 127;  // amax = f 2^ex, f in [1, 2)
+    q.a = __uint_as_float(((bits & 0x7f) << 16) | 0x3f800000u);
+    q.inv = __builtin_amdgcn_rcpf(q.a);
+    if constexpr (F::INT8) {
+        q.e = ex;
+        q.scale = amax / 127.f;
+    } else {
+        q.e = q.a <= 1.75f ? ex - 8 : ex - 7;  // 448 = 1.75 * 2^8
+        q.scale = __uint_as_float((uint32_t)(q.e + 127) << 23);
+    }
+    if (q.zero) q.scale = 1.f;
+    if (bits >= 0x7f80) {
+        q.scale = __builtin_nanf("");
+        q.zero = true;
+    }
+    return q;
+}
+
+// 127 x / a rounded to even, exactly: the product is exact (15 bits), and so is what
+// it leaves of a multiple of a, which corrects the approximate quotient at ties.
+__device__ __forceinline__ int32_t code_int8(float x, const Coding& q) {
+    const float t = 127.f * ldexpf(x, -q.e);
+    float r = rintf(t * q.inv);
+    const float d = fmaf(-r, q.a, t), over = 2.f * fabsf(d) - q.a;
+    if (over > 0.f || (over == 0.f && ((int32_t)r & 1))) r += d > 0.f ? 1.f : -1.f;
+    return (int32_t)r;
+}
+
+// Four values, one byte each in order.
+template <class F>
+__device__ __forceinline__ uint32_t code4(float x0, float x1, float x2, float x3, const Coding& q) {
+    if constexpr (F::INT8) {
+        return (uint32_t)(code_int8(x0, q) & 255) | (uint32_t)(code_int8(x1, q) & 255) << 8 |
+               (uint32_t)(code_int8(x2, q) & 255) << 16 | (uint32_t)(code_int8(x3, q) & 255) << 24;
+    } else {
+        int w = __builtin_amdgcn_cvt_pk_fp8_f32(ldexpf(x0, -q.e), ldexpf(x1, -q.e), 0, false);
+        return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(ldexpf(x2, -q.e), ldexpf(x3, -q.e), w, true);
+    }
+}
+
+__device__ __forceinline__ float bf16_at(const u32x4& w, int k) {  // element k of 8
+    return __uint_as_float(k & 1 ? w[k >> 1] & 0xffff0000u : w[k >> 1] << 16);
+}
+
+// max over the workgroup of x (waves leave theirs in part)
+__device__ __forceinline__ uint32_t group_max(uint32_t x, uint32_t* part) {
+#pragma unroll
+    for (int m = 32; m > 0; m >>= 1) x = max(x, (uint32_t)__shfl_xor((int)x, m));
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = x;
+    __syncthreads();
+    uint32_t r = 0;
+#pragma unroll
+    for (int w = 0; w < THREADS / 64; ++w) r = max(r, part[w]);
+    return r;
+}
+
+template <class F, int D, int PW>
+__global__ __launch_bounds__(THREADS) void kv_append_q8_kernel(
+    const __bf16* __restrict__ k, const __bf16* __restrict__ v, int64_t kt, int64_t kh, int64_t vt, int64_t vh,
+    int64_t tokens, int32_t batch, const int32_t* __restrict__ lens_before, const int32_t* __restrict__ lens_after,
+    const int32_t* __restrict__ token_start, const int32_t* __restrict__ block_start,
+    const int32_t* __restrict__ page_table, int32_t max_pages, int32_t num_pages, uint8_t* __restrict__ k_pages,
+    uint8_t* __restrict__ v_pages, float* __restrict__ k_scale, float* __restrict__ v_scale, __bf16* k_tail,
+    __bf16* v_tail, int32_t heads) {
+    constexpr int CH = D / 8;                // 8-dim chunks of a row
+    constexpr int ITEMS = CH * (PW / 4);     // a chunk of four keys each
+    constexpr int NI = (ITEMS + THREADS - 1) / THREADS;
+    constexpr int VST = PW + 4;              // bytes per dim in LDS (spread over the banks)
+    __shared__ uint32_t vt_lds[D * VST / 4];
+    __shared__ uint32_t part_k[THREADS / 64], part_v[THREADS / 64];
+    const int tid = threadIdx.x;
+    const int32_t u = blockIdx.x;
+    const int32_t h = blockIdx.y;
+
+    // the sequence of unit u: 64 entries of block_start at a time
+    int32_t lo = 0, hi = batch;  // block_start[lo] <= u < block_start[hi]
+    if (u >= block_start[batch]) return;
+    while (hi - lo > 1) {
+        const int32_t step = (hi - lo + 63) / 64;
+        const int32_t at = lo + (tid & 63) * step;
+        const bool in = at < hi && block_start[at] <= u;
+        const int32_t c = __popcll(__ballot(in)) - 1;
+        if (c < 0) return;  // not a table of page_step
+        lo += c * step;
+        hi = min(hi, lo + step);
+    }
+    const int32_t b = lo;
+    const int32_t i = u - block_start[b];
+    if (i < 0) return;
+    const int64_t start = max(lens_before[b], 0), end = max((int64_t)lens_after[b], start);
+    if (end == start) return;
+    const int64_t first = start / PW, last = (end - 1) / PW;
+    const int64_t block = first + i;
+    if (block > last) return;
+    const int64_t row0 = (int64_t)token_start[b] - start;  // row of position p: row0 + p
+    const int64_t tail_at = ((int64_t)b * heads + h) * PW * D;
+    const int32_t page = block < max_pages ? page_table[(int64_t)b * max_pages + block] : -1;
+
+    if ((block + 1) * PW <= end && page >= 0 && page < num_pages) {
+        u32x4 kw[NI][4], vw[NI][4];
+        uint32_t km = 0, vm = 0;
+#pragma unroll
+        for (int n = 0; n < NI; ++n) {
+            const int it = tid + n * THREADS, c = it % CH, g = it / CH;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int key = 4 * g + r;
+                const int64_t pos = block * PW + key, row = row0 + pos;
+                u32x4 a = {0u, 0u, 0u, 0u}, w = {0u, 0u, 0u, 0u};
+                if (it < ITEMS) {
+                    if (pos < start) {
+                        a = *reinterpret_cast<const u32x4*>(k_tail + tail_at + key * D + 8 * c);
+                        w = *reinterpret_cast<const u32x4*>(v_tail + tail_at + key * D + 8 * c);
+                    } else if (row >= 0 && row < tokens) {
+                        a = *reinterpret_cast<const u32x4*>(k + row * kt + h * kh + 8 * c);
+                        w = *reinterpret_cast<const u32x4*>(v + row * vt + h * vh + 8 * c);
+                    }
+                }
+                kw[n][r] = a;
+                vw[n][r] = w;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    km = max(km, max(a[e] & 0x7fffu, a[e] >> 16 & 0x7fffu));
+                    vm = max(vm, max(w[e] & 0x7fffu, w[e] >> 16 & 0x7fffu));
+                }
+            }
+        }
+        km = group_max(km, part_k);
+        vm = group_max(vm, part_v);
+        const Coding kq = coding<F>(km), vq = coding<F>(vm);
+        const int64_t slice = (int64_t)page * heads + h;
+        if (tid == 0) {
+            k_scale[slice] = kq.scale;
+            v_scale[slice] = vq.scale;
+        }
+        uint8_t* kp = k_pages + slice * (PW * D);
+        uint8_t* vp = v_pages + slice * (PW * D);
+#pragma unroll
+        for (int n = 0; n < NI; ++n) {
+            const int it = tid + n * THREADS, c = it % CH, g = it / CH;
+            if (it < ITEMS) {
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    u32x2 o = {0u, 0u};
+                    if (!kq.zero) {
+#pragma unroll
+                        for (int e = 0; e < 2; ++e)
+                            o[e] = code4<F>(bf16_at(kw[n][r], 4 * e), bf16_at(kw[n][r], 4 * e + 1),
+                                            bf16_at(kw[n][r], 4 * e + 2), bf16_at(kw[n][r], 4 * e + 3), kq);
+                    }
+                    *reinterpret_cast<u32x2*>(kp + (4 * g + r) * D + 8 * c) = o;
+                }
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    vt_lds[(8 * c + e) * (VST / 4) + g] =
+                        vq.zero ? 0u
+                                : code4<F>(bf16_at(vw[n][0], e), bf16_at(vw[n][1], e), bf16_at(vw[n][2], e),
+                                           bf16_at(vw[n][3], e), vq);
+            }
+        }
+        __syncthreads();
+        for (int x = tid; x < D * PW / 16; x += THREADS) {
+            const int d = x / (PW / 16), q = x % (PW / 16);
+            u32x4 o;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] = vt_lds[d * (VST / 4) + 4 * q + e];
+            *reinterpret_cast<u32x4*>(vp + d * PW + 16 * q) = o;
+        }
+    }
+
+    if (i != 0) return;
+    __syncthreads();  // the tail has been read
+    const int64_t from = max(start, last * PW);
+    for (int x = tid; x < (int)(end - from) * CH; x += THREADS) {
+        const int64_t pos = from + x / CH, row = row0 + pos;
+        const int c = x % CH;
+        if (row < 0 || row >= tokens) continue;
+        const int64_t dst = tail_at + (pos - last * PW) * D + 8 * c;
+        *reinterpret_cast<u32x4*>(k_tail + dst) = *reinterpret_cast<const u32x4*>(k + row * kt + h * kh + 8 * c);
+        *reinterpret_cast<u32x4*>(v_tail + dst) = *reinterpret_cast<const u32x4*>(v + row * vt + h * vh + 8 * c);
+    }
+}
+
+bool strides16(int64_t a, int64_t b) { return a >= 0 && b >= 0 && a % 8 == 0 && b % 8 == 0; }
+
+template <typename TI, typename TO>
+hipError_t launch_rope(const RopeSide& q, const RopeSide& k, const int32_t* positions, int64_t pos_batch,
+                       const double* freqs, int64_t rows, int64_t n, int32_t d, int32_t rot, bool inter, bool wide,
+                       float amplitude, float sign, hipStream_t s, bool* fits) {
+    const int32_t P = wide ? (inter ? 8 : 16) / (int32_t)sizeof(TI) : 1;
+    const int32_t E = inter ? 2 * P : P;
+    const int32_t lanes = rot / 2 / P + (d - rot) / E;
+    const int64_t groups = (rows * lanes + THREADS - 1) / THREADS;
+    const int32_t heads = q.heads + k.heads;
+    // few rows: a head per lane; many: a lane walks over several heads
+    const int32_t hsplit = groups >= 2048 ? (heads + 7) / 8 : heads;
+    *fits = rows * lanes < (int64_t(1) << 31) && launchable(groups * hsplit) && hsplit < 65536;
+    if (!*fits) return hipSuccess;
+    auto go = [&](auto kern) {
+        hipLaunchKernelGGL(kern, dim3((unsigned)groups, (unsigned)hsplit), dim3(THREADS), 0, s, q, k, positions,
+                           pos_batch, freqs, (uint32_t)(rows * lanes), (uint32_t)n, (uint32_t)lanes, rot / 2, amplitude,
+                           sign);
+        return hipGetLastError();
+    };
+    if (inter) return wide ? go(rope_kernel<TI, TO, true, 8 / sizeof(TI)>) : go(rope_kernel<TI, TO, true, 1>);
+    return wide ? go(rope_kernel<TI, TO, false, 16 / sizeof(TI)>) : go(rope_kernel<TI, TO, false, 1>);
+}
+
+template <class F>
+hipError_t launch_append_q8(int64_t units, const __bf16* k, const __bf16* v, int64_t kt, int64_t kh, int64_t vt,
+                            int64_t vh, int64_t tokens, int32_t batch, const int32_t* before, const int32_t* after,
+                            const int32_t* token_start, const int32_t* block_start, const int32_t* page_table,
+                            int32_t max_pages, int32_t num_pages, void* kp, void* vp, float* ks, float* vs, void* ktl,
+                            void* vtl, int32_t heads, int32_t d, int32_t B, hipStream_t s) {
+    auto go = [&](auto kern) {
+        hipLaunchKernelGGL(kern, dim3((unsigned)units, (unsigned)heads), dim3(THREADS), 0, s, k, v, kt, kh, vt, vh,
+                           tokens, batch, before, after, token_start, block_start, page_table, max_pages, num_pages,
+                           (uint8_t*)kp, (uint8_t*)vp, ks, vs, (__bf16*)ktl, (__bf16*)vtl, heads);
+        return hipGetLastError();
+    };
+    if (d == 64) return B == 64 ? go(kv_append_q8_kernel<F, 64, 64>) : go(kv_append_q8_kernel<F, 64, 128>);
+    return B == 64 ? go(kv_append_q8_kernel<F, 128, 64>) : go(kv_append_q8_kernel<F, 128, 128>);
+}
+
+}  // namespace
+}  // namespace bf1
+
+extern "C" {
+
+int bf1_page_step(int32_t batch, const int32_t* seq_lens, const int32_t* new_lens, int32_t* page_table,
+                  int32_t max_pages_per_seq, const int32_t* free_pages, int32_t num_free, const int32_t* free_head,
+                  int32_t B, int64_t max_tokens, int32_t* seq_lens_out, int32_t* token_start, int32_t* block_start,
+                  int32_t* positions, int64_t* slots, int32_t* free_head_out, void* stream) {
+    if (batch < 0 || max_pages_per_seq < 1 || num_free < 0 || max_tokens < 0) return BF1_ERR_INVALID_ARG;
+    if (B != 64 && B != 128) return BF1_ERR_UNSUPPORTED;
+    if (max_tokens >= (int64_t(1) << 31)) return BF1_ERR_UNSUPPORTED;
+    for (const void* p : {(const void*)free_head, (const void*)token_start, (const void*)block_start,
+                          (const void*)free_head_out})
+        if (!bf1::aligned(p, 4)) return BF1_ERR_INVALID_ARG;
+    if (batch > 0)
+        for (const void* p : {(const void*)seq_lens, (const void*)new_lens, (const void*)page_table,
+                              (const void*)seq_lens_out})
+            if (!bf1::aligned(p, 4)) return BF1_ERR_INVALID_ARG;
+    if (num_free > 0 && !bf1::aligned(free_pages, 4)) return BF1_ERR_INVALID_ARG;
+    if (max_tokens > 0 && (!bf1::aligned(positions, 4) || !bf1::aligned(slots, 8))) return BF1_ERR_INVALID_ARG;
+    // every workgroup reads the lengths and the head while one writes the new ones
+    if (free_head_out == free_head || (batch > 0 && (seq_lens_out == seq_lens || seq_lens_out == new_lens)))
+        return BF1_ERR_INVALID_ARG;
+    const int64_t groups = max_tokens <= bf1::ROWS_PER_GROUP
+                               ? 1
+                               : (max_tokens + bf1::ROWS_PER_GROUP - 1) / bf1::ROWS_PER_GROUP;
+    hipLaunchKernelGGL(bf1::page_step_kernel, dim3((unsigned)groups), dim3(bf1::THREADS), 0, (hipStream_t)stream, batch,
+                       seq_lens, new_lens, page_table, max_pages_per_seq, free_pages, num_free, free_head,
+                       B == 64 ? 6 : 7, max_tokens, seq_lens_out, token_start, block_start, positions, slots,
+                       free_head_out);
+    return bf1::status_of(hipGetLastError());
+}
+
+int bf1_rope(const void* Q, const void* K, const int32_t* positions, int64_t positions_batch_stride,
+             const double* freqs, void* Q_out, void* K_out, int32_t batch, int64_t n, int32_t Hq, int32_t Hkv,
+             int32_t head_dim, int32_t rot_dim, int32_t in_type, int32_t out_type, int32_t interleaved, float amplitude,
+             int32_t transposed, const int64_t* strides, void* stream) {
+    if (batch < 0 || n < 0 || Hq < 0 || Hkv < 0 || !strides) return BF1_ERR_INVALID_ARG;
+    if (in_type < 0 || in_type > 1 || out_type < 0 || out_type > 1 || (interleaved & ~1) || (transposed & ~1))
+        return BF1_ERR_INVALID_ARG;
+    if (head_dim < 2 || head_dim > 1024 || head_dim % 2 || rot_dim < 2 || rot_dim > head_dim || rot_dim % 2)
+        return BF1_ERR_UNSUPPORTED;
+    if (in_type == BF1_TYPE_BF16 && out_type != BF1_TYPE_BF16) return BF1_ERR_UNSUPPORTED;
+    if (positions_batch_stride != 0 && positions_batch_stride < n) return BF1_ERR_INVALID_ARG;
+    if (n >= (int64_t(1) << 31)) return BF1_ERR_UNSUPPORTED;
+    if (batch == 0 || n == 0 || Hq + (int64_t)Hkv == 0) return BF1_OK;
+    if (Hq + (int64_t)Hkv > 65535) return BF1_ERR_UNSUPPORTED;
+    const int64_t esize = in_type == BF1_TYPE_BF16 ? 2 : 4, osize = out_type == BF1_TYPE_BF16 ? 2 : 4;
+    if (!bf1::aligned(positions, 4) || !bf1::aligned(freqs, 8)) return BF1_ERR_INVALID_ARG;
+    for (int i = 0; i < 12; ++i)
+        if (strides[i] < 0 || strides[i] > (int64_t(1) << 40)) return BF1_ERR_INVALID_ARG;
+    const int64_t vec = 16 / esize;  // elements of a 16-byte load
+    // 16 bytes at a time where the halves, the rest and every row allow it
+    bool wide = rot_dim % (2 * vec) == 0 && (head_dim - rot_dim) % vec == 0;
+    for (int side = 0; side < 2; ++side) {
+        if ((side ? Hkv : Hq) == 0) continue;
+        const void* in = side ? K : Q;
+        void* out = side ? K_out : Q_out;
+        if (!bf1::aligned(in, esize) || !bf1::aligned(out, osize)) return BF1_ERR_INVALID_ARG;
+        // in place only where an element keeps its place
+        if (in == out) {
+            if (in_type != out_type) return BF1_ERR_INVALID_ARG;
+            for (int i = 0; i < 3; ++i)
+                if (strides[6 * side + i] != strides[6 * side + 3 + i]) return BF1_ERR_INVALID_ARG;
+        }
+        wide = wide && bf1::aligned(in, 16) && bf1::aligned(out, vec * osize);
+        for (int i = 0; i < 6; ++i) wide = wide && strides[6 * side + i] % vec == 0;
+    }
+    const bf1::RopeSide q{Q, Q_out, strides[0], strides[1], strides[2], strides[3], strides[4], strides[5], Hq};
+    const bf1::RopeSide k{K, K_out, strides[6], strides[7], strides[8], strides[9], strides[10], strides[11], Hkv};
+    const float sign = transposed ? -1.f : 1.f;
+    bool fits = false;
+    hipStream_t s = (hipStream_t)stream;
+    hipError_t e;
+    const int64_t rows = (int64_t)batch * n;
+    if (rows >= (int64_t(1) << 31)) return BF1_ERR_UNSUPPORTED;
+    if (in_type == BF1_TYPE_BF16)
+        e = bf1::launch_rope<__bf16, __bf16>(q, k, positions, positions_batch_stride, freqs, rows, n, head_dim, rot_dim,
+                                             interleaved, wide, amplitude, sign, s, &fits);
+    else if (out_type == BF1_TYPE_BF16)
+        e = bf1::launch_rope<float, __bf16>(q, k, positions, positions_batch_stride, freqs, rows, n, head_dim, rot_dim,
+                                            interleaved, wide, amplitude, sign, s, &fits);
+    else
+        e = bf1::launch_rope<float, float>(q, k, positions, positions_batch_stride, freqs, rows, n, head_dim, rot_dim,
+                                           interleaved, wide, amplitude, sign, s, &fits);
+    return fits ? bf1::status_of(e) : BF1_ERR_UNSUPPORTED;
+}
+
+int bf1_kv_append(const void* K, const void* V, int64_t k_token_stride, int64_t k_head_stride, int64_t v_token_stride,
+                  int64_t v_head_stride, const int64_t* slots, void* K_pages, void* V_pages, int64_t tokens,
+                  int32_t num_pages, int32_t Hkv, int32_t head_dim, int32_t B, void* stream) {
+    if (tokens < 0 || num_pages < 1 || Hkv < 1) return BF1_ERR_INVALID_ARG;
+    if (head_dim != 64 && head_dim != 128) return BF1_ERR_UNSUPPORTED;
+    if (B != 64 && B != 128) return BF1_ERR_UNSUPPORTED;
+    if (tokens == 0) return BF1_OK;
+    if (!bf1::aligned(K, 16) || !bf1::aligned(V, 16) || !bf1::aligned(K_pages, 16) || !bf1::aligned(V_pages, 16) ||
+        !bf1::aligned(slots, 8))
+        return BF1_ERR_INVALID_ARG;
+    if (!bf1::strides16(k_token_stride, k_head_stride) || !bf1::strides16(v_token_stride, v_head_stride))
+        return BF1_ERR_INVALID_ARG;
+    if (tokens >= (int64_t(1) << 31) || (double)tokens * Hkv * (head_dim / 8) >= 4294967296.0) return BF1_ERR_UNSUPPORTED;
+    const int64_t items = tokens * Hkv * (head_dim / 8);
+    const int64_t groups = (items + bf1::THREADS - 1) / bf1::THREADS;
+    if (!bf1::launchable(groups)) return BF1_ERR_UNSUPPORTED;
+    hipLaunchKernelGGL(bf1::kv_append_kernel, dim3((unsigned)groups), dim3(bf1::THREADS), 0, (hipStream_t)stream,
+                       (const __bf16*)K, (const __bf16*)V, k_token_stride, k_head_stride, v_token_stride, v_head_stride,
+                       slots, (__bf16*)K_pages, (__bf16*)V_pages, items, Hkv, head_dim == 64 ? 6 : 7, B == 64 ? 6 : 7,
+                       (int64_t)num_pages * B);
+    return bf1::status_of(hipGetLastError());
+}
+
+int bf1_kv_append_q8(const void* K, const void* V, int64_t k_token_stride, int64_t k_head_stride,
+                     int64_t v_token_stride, int64_t v_head_stride, int64_t tokens, int32_t batch,
+                     const int32_t* seq_lens_before, const int32_t* seq_lens, const int32_t* token_start,
+                     const int32_t* block_start, const int32_t* page_table, int32_t max_pages_per_seq,
+                     int32_t num_pages, void* K_pages, void* V_pages, float* K_scale, float* V_scale, void* K_tail,
+                     void* V_tail, int32_t Hkv, int32_t head_dim, int32_t B, int32_t format, void* stream) {
+    if (tokens < 0 || batch < 0 || max_pages_per_seq < 1 || num_pages < 1 || Hkv < 1) return BF1_ERR_INVALID_ARG;
+    if (head_dim != 64 && head_dim != 128) return BF1_ERR_UNSUPPORTED;
+    if (B != 64 && B != 128) return BF1_ERR_UNSUPPORTED;
+    if (format != BF1_Q8_E4M3 && format != BF1_Q8_INT8) return BF1_ERR_INVALID_ARG;
+    if (tokens == 0 || batch == 0) return BF1_OK;
+    for (const void* p : {K, V, (const void*)K_pages, (const void*)V_pages, (const void*)K_tail, (const void*)V_tail})
+        if (!bf1::aligned(p, 16)) return BF1_ERR_INVALID_ARG;
+    for (const void* p : {(const void*)seq_lens_before, (const void*)seq_lens, (const void*)token_start,
+                          (const void*)block_start, (const void*)page_table, (const void*)K_scale,
+                          (const void*)V_scale})
+        if (!bf1::aligned(p, 4)) return BF1_ERR_INVALID_ARG;
+    if (!bf1::strides16(k_token_stride, k_head_stride) || !bf1::strides16(v_token_stride, v_head_stride))
+        return BF1_ERR_INVALID_ARG;
+    if (tokens >= (int64_t(1) << 31) || Hkv > 65535) return BF1_ERR_UNSUPPORTED;
+    // blocks that `tokens` rows of up to `batch` sequences can touch: one of x rows
+    // touches at most 1 + ceil((x - 1) / B)
+    const int64_t active = tokens < batch ? tokens : batch, rest = tokens - active;
+    const int64_t more = rest < active ? rest : active;
+    const int64_t units = active + more + (rest - more) / B;
+    if (!bf1::launchable(units * Hkv)) return BF1_ERR_UNSUPPORTED;
+    auto go = [&](auto f) {
+        return bf1::launch_append_q8<decltype(f)>(
+            units, (const __bf16*)K, (const __bf16*)V, k_token_stride, k_head_stride, v_token_stride, v_head_stride,
+            tokens, batch, seq_lens_before, seq_lens, token_start, block_start, page_table, max_pages_per_seq, num_pages,
+            K_pages, V_pages, K_scale, V_scale, K_tail, V_tail, Hkv, head_dim, B, (hipStream_t)stream);
+    };
+    return bf1::status_of(format == BF1_Q8_INT8 ? go(bf1::QuantInt8{}) : go(bf1::QuantE4m3{}));
+}
+
+}  // extern "C"
