@@ -16,6 +16,7 @@
 // instructions and the scales multiply fp32 numbers: the scores' sums, and the
 // weights before they are split in two bf16 parts (16 bits together).
 #include <hip/hip_runtime.h>
+#include <float.h>
 #include <math.h>
 #include <stdint.h>
 
@@ -30,8 +31,8 @@ namespace {
 constexpr int WAVES = 4;
 constexpr int THREADS = WAVES * 64;
 constexpr int UNIT = 64;               // keys of a wave's step
-constexpr float MIN_PART = 0x1p-132f;  // least first part of a weight of the tail
-constexpr int CPOL_NT = 2;             // a page is read once per step
+constexpr float MIN_PART = 0x1p-132f;  // least first part of a weight of the tail (a bf16 number)
+constexpr int CPOL_NT = 2;
 
 struct E4m3 {
     // four codes (one byte each) as bf16
@@ -65,6 +66,14 @@ __device__ __forceinline__ float col_sum(float x) {
     return pair_sum(__uint_as_float(r[0]) + __uint_as_float(r[1]));
 }
 
+// 2^x for what is at most 1.  The instruction gives 0 below 2^-126; every weight that
+// fp32 holds stays above 0, so that an infinite value counts under it.
+constexpr float LEAST = 0x1p-149f;
+__device__ __forceinline__ float decay(float x) {
+    const float e = __builtin_amdgcn_exp2f(x);
+    return x > -150.f ? fmaxf(e, LEAST) : e;
+}
+
 // What a step of one sequence reads; false if the plan row is another block's.
 struct View {
     int c;      // earlier pages
@@ -81,26 +90,29 @@ __device__ __forceinline__ bool view(const int32_t* __restrict__ seq_lens, const
     v->units = pc * (PW / UNIT) + (v->nv + UNIT - 1) / UNIT;
     return t >= 0 && pj == t / PW && pc >= 0 && pc <= cap;
 }
-// Units of a split of a list of `units`, at most nsplit splits.
-__device__ __forceinline__ int units_per_split(int units, int nsplit) {
-    return max(WAVES, (units + nsplit - 1) / nsplit);
+// Splits of a list that have work: the waves of split s take units s * WAVES + wave,
+// WAVES * nsplit further, ...
+__device__ __forceinline__ int splits_used(int units, int nsplit) {
+    return min(nsplit, (units + WAVES - 1) / WAVES);
 }
 
 template <class F, int D, int G, int PW>
-__global__ __launch_bounds__(THREADS) void decode_q8_kernel(
+__global__ __launch_bounds__(THREADS, 3) void decode_q8_kernel(
     const __bf16* __restrict__ Q, const uint8_t* __restrict__ Kp, const uint8_t* __restrict__ Vp,
     const float* __restrict__ k_scale, const float* __restrict__ v_scale, const __bf16* __restrict__ k_tail,
     const __bf16* __restrict__ v_tail, const int32_t* __restrict__ seq_lens, int32_t num_pages,
     const int32_t* __restrict__ plan, int32_t stride, int32_t cap, __bf16* __restrict__ O, float* __restrict__ LSE,
     float* __restrict__ ws, int32_t Hkv, int32_t nsplit, float c_log2) {
     constexpr int UPP = PW / UNIT;     // units of a page
+    // A page of 64 is read once, by one wave: past the caches it comes 5% (short lists) to
+    // 15% (long ones) sooner.  Two waves share the lines of the V rows of a page of 128:
+    // there it would cost 10 to 15%.
+    constexpr int CPOL = PW == UNIT ? CPOL_NT : 0;
     constexpr int KL = D / 64;         // 16-byte loads of a key row per lane
     constexpr int DT = D / 16;         // 16-wide tiles of O
-    constexpr int COLS = 2 * G;        // columns that carry a part
-    constexpr int OST = D + 4;         // floats per column in LDS
-    constexpr int REC = G * (D + 2);   // floats per partial record
+    constexpr int OST = D + 4;         // floats per q-head in LDS
     constexpr int V_BYTES = UPP * UNIT * 2 * D;  // V rows of the tail
-    constexpr int R_BYTES = WAVES * COLS * (OST + 2) * 4;
+    constexpr int R_BYTES = (WAVES * (OST + 2) + 1) * G * 4;
     __shared__ __align__(256) u32x4 lds[(V_BYTES > R_BYTES ? V_BYTES : R_BYTES) / 16 + 1];
 
     const int tid = threadIdx.x;
@@ -108,26 +120,12 @@ __global__ __launch_bounds__(THREADS) void decode_q8_kernel(
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 15;
     const int quad = lane >> 4;
-    const int s = blockIdx.x % nsplit;
-    const int bh = blockIdx.x / nsplit;
-    const int h = bh % Hkv;
-    const int b = bh / Hkv;
-    const int Hq = Hkv * G;
-    const int64_t orow = (int64_t)b * Hq + h * G;
+    const int b = blockIdx.x, h = blockIdx.y, s = blockIdx.z;
+    const int64_t bh = (int64_t)b * Hkv + h;
+    const int64_t orow = bh * G;
     const int32_t* row = plan + (int64_t)b * stride;
-
-    View sv;
-    if (!view<PW>(seq_lens, row, cap, b, &sv)) {
-        if (s == 0) {  // stale or unplannable
-            for (int x = tid; x < G * D; x += THREADS) O[orow * D + x] = (__bf16)__builtin_nanf("");
-            if (LSE != nullptr && tid < G) LSE[orow + tid] = __builtin_nanf("");
-        }
-        return;
-    }
-    const int ups = units_per_split(sv.units, nsplit);
-    const int nsb = (sv.units + ups - 1) / ups;
-    if (s >= nsb) return;
-    const int u0 = s * ups, u1 = min(sv.units, u0 + ups);
+    int u = s * WAVES + wave;                  // this wave's first unit
+    const int32_t first = row[2 + min(u / UPP, cap)];  // its page, on its way with what says whether it counts
 
     // Q rows as the score product's B operand: column col is head col % G; k-step
     // (kl, hf) of lane group quad is dims 64 kl + 16 quad + 8 hf ..
@@ -140,12 +138,23 @@ __global__ __launch_bounds__(THREADS) void decode_q8_kernel(
             for (int hf = 0; hf < 2; ++hf)
                 qf[kl][hf] = *reinterpret_cast<const bf16x8*>(src + 64 * kl + 16 * quad + 8 * hf);
     }
+    asm volatile("" ::: "memory");  // ahead of the cache's rows, so that waiting for Q waits for nothing else
+
+    View sv;
+    if (!view<PW>(seq_lens, row, cap, b, &sv)) {
+        if (s == 0) {  // stale or unplannable
+            for (int x = tid; x < G * D; x += THREADS) O[orow * D + x] = (__bf16)__builtin_nanf("");
+            if (LSE != nullptr && tid < G) LSE[orow + tid] = __builtin_nanf("");
+        }
+        return;
+    }
+    const int nsb = splits_used(sv.units, nsplit);
+    if (s >= nsb) return;
 
     f32x4 acc[DT];
 #pragma unroll
     for (int t = 0; t < DT; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
     float m_run = -INFINITY, l_run = 0.f;
-    const int part = col / G;  // which part of a weight this column carries
 
     // Scores of four 16-key tiles -> weights in place; what came before is rescaled.
     auto soften = [&](f32x4 (&sc)[4]) -> float {
@@ -157,7 +166,7 @@ __global__ __launch_bounds__(THREADS) void decode_q8_kernel(
         const float m_new = fmaxf(m_run, col_max(mx));
         const float m_use = m_new == -INFINITY ? 0.f : m_new;
         if (__any(m_new > m_run)) {
-            const float alpha = exp2f(m_run - m_use);
+            const float alpha = decay(m_run - m_use);
             l_run *= alpha;
 #pragma unroll
             for (int t = 0; t < DT; ++t)
@@ -167,228 +176,291 @@ __global__ __launch_bounds__(THREADS) void decode_q8_kernel(
         }
         return m_use;
     };
-    // This column's part of the weights a + b (bf16: 8 bits, the rounded rest: 8 more).
-    auto part_of = [&](float w, float first) -> __bf16 {
-        const __bf16 hi = (__bf16)first;
-        const __bf16 lo = (__bf16)(w - (float)hi);
-        return part == 0 ? hi : part == 1 ? lo : (__bf16)0.f;
+    // This column's part of two weights: their bf16 roundings, or the rounded rests (for
+    // 16 bits together).  `first` is what the roundings are made of.  Columns past the
+    // two parts repeat the second; nothing reads them.
+    const bool second = col >= G;
+    auto parts = [&](float w0, float w1, float first0, float first1) -> uint32_t {
+        const uint32_t hi = __builtin_bit_cast(uint32_t, bf16x2{(__bf16)first0, (__bf16)first1});
+        const float r0 = w0 - __uint_as_float(hi << 16), r1 = w1 - __uint_as_float(hi & 0xffff0000u);
+        const uint32_t lo = __builtin_bit_cast(uint32_t, bf16x2{(__bf16)r0, (__bf16)r1});
+        return second ? lo : hi;
     };
 
-    for (int u = u0 + wave; u < u1; u += WAVES) {
-        if (u < sv.c * UPP) {
-            // 64 keys of a page.  Row i = 4 q + r of tile t is key 16 q + 4 t + r, so that
-            // lane group q ends with the scores of keys 16 q .. 16 q + 15, in the order of
-            // the 16 bytes it loads of each V row.
-            const int page = __builtin_amdgcn_readfirstlane(min(max(row[2 + u / UPP], 0), num_pages - 1));
-            const int64_t slice = (int64_t)page * Hkv + h;
-            const float ks = k_scale[slice] * c_log2, vs = v_scale[slice];
-            const __amdgpu_buffer_rsrc_t kr = head_rsrc(Kp + slice * (PW * D), PW * D);
-            const __amdgpu_buffer_rsrc_t vr = head_rsrc(Vp + slice * (PW * D), PW * D);
-            const int un = u % UPP;
-            u32x4 kw[4][KL], vw[DT];
+    // 64 keys of a page.  Row i = 4 q + r of score tile t is key 16 q + 4 t + r, so that
+    // lane group q ends with the scores of keys 16 q .. 16 q + 15, in the order of the
+    // 16 bytes it loads of each V row.
+    u32x4 kw[4][KL], vw[DT];
+    float ks, vs;
+    auto slice_of = [&](int32_t page) {
+        return (int64_t)__builtin_amdgcn_readfirstlane(min(max(page, 0), num_pages - 1)) * Hkv + h;
+    };
+    auto load_k = [&](int u, int64_t slice, uint32_t bytes) {
+        const __amdgpu_buffer_rsrc_t r = head_rsrc(Kp + slice * (PW * D), bytes);
+        ks = k_scale[slice] * c_log2;
 #pragma unroll
-            for (int t = 0; t < 4; ++t)
+        for (int t = 0; t < 4; ++t)
 #pragma unroll
-                for (int kl = 0; kl < KL; ++kl)
-                    kw[t][kl] = __builtin_amdgcn_raw_buffer_load_b128(
-                        kr, (16 * (col >> 2) + (col & 3)) * D + 16 * quad + 4 * t * D + 64 * kl, un * UNIT * D, CPOL_NT);
+            for (int kl = 0; kl < KL; ++kl)
+                kw[t][kl] = __builtin_amdgcn_raw_buffer_load_b128(
+                    r, (16 * (col >> 2) + (col & 3)) * D + 16 * quad + 4 * t * D + 64 * kl, u % UPP * UNIT * D, CPOL);
+    };
+    auto load_v = [&](int u, int64_t slice, uint32_t bytes) {
+        const __amdgpu_buffer_rsrc_t r = head_rsrc(Vp + slice * (PW * D), bytes);
+        vs = v_scale[slice];
 #pragma unroll
-            for (int t = 0; t < DT; ++t)
-                vw[t] = __builtin_amdgcn_raw_buffer_load_b128(vr, col * PW + 16 * quad, un * UNIT + 16 * t * PW, CPOL_NT);
-            f32x4 sc[4];
+        for (int t = 0; t < DT; ++t)
+            vw[t] = __builtin_amdgcn_raw_buffer_load_b128(r, col * PW + 16 * quad, u % UPP * UNIT + 16 * t * PW, CPOL);
+    };
+
+    // This wave's units; at most one is the tail's, and it goes first: 64 rows in bf16,
+    // tile t is keys 16 t ..  Its K rows come to the registers that pages' rows use
+    // later, all at once; its V rows to LDS.  Rows past the valid ones read as zeros.
+    const int pages = sv.c * UPP, hop = WAVES * nsplit;
+    const int un = (u < pages ? u + (pages - u + hop - 1) / hop * hop : u) - pages;  // the tail's unit
+    const bool tail = pages + un < sv.units;
+    constexpr int RB = 2 * D, RPS = 1024 / RB;  // bytes per row, rows per 1 KB segment
+    auto vslot = [](int r) { return D == 128 ? (r & 7) : ((r >> 1) & 3); };
+    char* vbuf = reinterpret_cast<char*>(&lds[0]) + un * (UNIT * RB);
+    f32x4 ts[4];
+    float tm = 0.f;
+    if (tail) {
+        const __amdgpu_buffer_rsrc_t kr = head_rsrc(k_tail + bh * (PW * D), sv.nv * RB);
+        const __amdgpu_buffer_rsrc_t vr = head_rsrc(v_tail + bh * (PW * D), sv.nv * RB);
 #pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                sc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int i = 0; i < UNIT / RPS; ++i) {
+            const int r = i * RPS + lane / (RB / 16), pc = lane % (RB / 16);
+            const uint32_t off = r * RB + 16 * (2 * ((pc >> 1) ^ vslot(r)) + (pc & 1));
+            load_lds16(vr, vbuf + i * 1024, off, un * UNIT * RB);
+        }
+        u32x4 tk[4][KL][2];
 #pragma unroll
-                for (int kl = 0; kl < KL; ++kl)
+        for (int t = 0; t < 4; ++t)
 #pragma unroll
-                    for (int hf = 0; hf < 2; ++hf)
-                        sc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                            widen8<F>(kw[t][kl][2 * hf], kw[t][kl][2 * hf + 1]), qf[kl][hf], sc[t], 0, 0, 0);
+            for (int kl = 0; kl < KL; ++kl)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) sc[t][r] *= ks;
+                for (int hf = 0; hf < 2; ++hf)
+                    tk[t][kl][hf] = __builtin_amdgcn_raw_buffer_load_b128(
+                        kr, col * RB + 32 * quad + 16 * t * RB + 128 * kl + 16 * hf, un * UNIT * RB, 0);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            ts[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int kl = 0; kl < KL; ++kl)
+#pragma unroll
+                for (int hf = 0; hf < 2; ++hf)
+                    ts[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, tk[t][kl][hf]), qf[kl][hf],
+                                                                    ts[t], 0, 0, 0);
+            const int left = sv.nv - un * UNIT - 16 * t - 4 * quad;  // valid ones of this lane's four keys
+#pragma unroll
+            for (int r = 0; r < 4; ++r) ts[t][r] = r < left ? ts[t][r] * c_log2 : -INFINITY;
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_waitcnt(VMCNT0);  // the V rows, too, before the pages' are asked for
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    int32_t coming = row[2 + min((u + hop) / UPP, cap)];  // page of the next unit
+    {
+        const int64_t slice = slice_of(first);
+        const uint32_t bytes = u < pages ? PW * D : 0;
+        load_k(u, slice, bytes);
+        load_v(u, slice, bytes);
+    }
+#pragma unroll
+    for (int kl = 0; kl < KL; ++kl) asm volatile("; Q is there" ::"v"(qf[kl][0]), "v"(qf[kl][1]));
+    if (tail) {
+        tm = soften(ts);
+        // transpose reads: row 4 quad + col / 4 of a tile, dims 16 dt + 4 (col % 4) ..
+        const int tr = 4 * quad + (col >> 2);
+        const uint32_t vtr = lds_addr(vbuf) + tr * RB + 8 * (col & 3) + 32 * vslot(tr);
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            u32x2 pb;
+#pragma unroll
+            for (int r = 0; r < 4; r += 2) {
+                // the first part of a weight is not 0 while the weight is not (see decay)
+                const float x0 = ts[t][r] - tm, x1 = ts[t][r + 1] - tm;
+                const float w0 = __builtin_amdgcn_exp2f(x0), w1 = __builtin_amdgcn_exp2f(x1);
+                l_run += w0 + w1;
+                pb[r / 2] = parts(w0, w1, x0 > -150.f ? fmaxf(w0, MIN_PART) : w0, x1 > -150.f ? fmaxf(w1, MIN_PART) : w1);
             }
-            const float m = soften(sc);
-            bf16x8 pb[2];
 #pragma unroll
-            for (int t = 0; t < 4; ++t)
+            for (int d0 = 0; d0 < DT; d0 += 4) {
+                u32x2 vt[4];
+                asm volatile(
+                    "ds_read_b64_tr_b16 %0, %4 offset:%8\n\tds_read_b64_tr_b16 %1, %5 offset:%8\n\t"
+                    "ds_read_b64_tr_b16 %2, %6 offset:%8\n\tds_read_b64_tr_b16 %3, %7 offset:%8\n\t"
+                    "s_waitcnt lgkmcnt(0)"
+                    : "=&v"(vt[0]), "=&v"(vt[1]), "=&v"(vt[2]), "=&v"(vt[3])
+                    : "v"(vtr ^ (32 * d0)), "v"(vtr ^ (32 * d0 + 32)), "v"(vtr ^ (32 * d0 + 64)),
+                      "v"(vtr ^ (32 * d0 + 96)), "i"(t * 16 * RB)
+                    : "memory");
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const float w = __builtin_amdgcn_exp2f(sc[t][r] - m);
-                    l_run += w;
-                    pb[t >> 1][4 * (t & 1) + r] = part_of(w * vs, w * vs);
-                }
-#pragma unroll
-            for (int t = 0; t < DT; ++t)
-#pragma unroll
-                for (int x = 0; x < 2; ++x)
-                    acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8<F>(vw[t][2 * x], vw[t][2 * x + 1]), pb[x],
-                                                                     acc[t], 0, 0, 0);
-        } else {
-            // 64 rows of the tail, in bf16; tile t is keys 16 t .., V^T by transpose reads
-            // from LDS.  Rows past the valid ones read as zeros.
-            const int un = u - sv.c * UPP;
-            const int64_t base = (int64_t)bh * PW * D;
-            const __amdgpu_buffer_rsrc_t kr = head_rsrc(k_tail + base, sv.nv * 2 * D);
-            const __amdgpu_buffer_rsrc_t vr = head_rsrc(v_tail + base, sv.nv * 2 * D);
-            char* vbuf = reinterpret_cast<char*>(&lds[0]) + un * UNIT * 2 * D;
-            constexpr int RB = 2 * D, RPS = 1024 / RB;  // bytes per row, rows per 1 KB segment
-            auto vslot = [](int r) { return D == 128 ? (r & 7) : ((r >> 1) & 3); };
-#pragma unroll
-            for (int i = 0; i < UNIT / RPS; ++i) {
-                const int r = i * RPS + lane / (RB / 16), pc = lane % (RB / 16);
-                const uint32_t off = r * RB + 16 * (2 * ((pc >> 1) ^ vslot(r)) + (pc & 1));
-                load_lds16(vr, vbuf + i * 1024, off, un * UNIT * RB);
-            }
-            f32x4 sc[4];
-#pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                sc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int kl = 0; kl < KL; ++kl)
-#pragma unroll
-                    for (int hf = 0; hf < 2; ++hf) {
-                        const u32x4 w = __builtin_amdgcn_raw_buffer_load_b128(
-                            kr, (16 * t + col) * RB + 128 * kl + 32 * quad + 16 * hf, un * UNIT * RB, 0);
-                        sc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w), qf[kl][hf], sc[t], 0,
-                                                                        0, 0);
-                    }
-                const int left = sv.nv - un * UNIT - 16 * t - 4 * quad;  // valid ones of this lane's four keys
-#pragma unroll
-                for (int r = 0; r < 4; ++r) sc[t][r] = r < left ? sc[t][r] * c_log2 : -INFINITY;
-            }
-            const float m = soften(sc);
-            __builtin_amdgcn_sched_barrier(0);
-            __builtin_amdgcn_s_waitcnt(VMCNT0);
-            // transpose reads: row 4 quad + col / 4 of a tile, dims 16 dt + 4 (col % 4) ..
-            const int tr = 4 * quad + (col >> 2);
-            const uint32_t vtr = lds_addr(vbuf) + tr * RB + 8 * (col & 3) + 32 * vslot(tr);
-#pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                bf16x4 pb;
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    // an infinite value counts at every weight that fp32 holds, so the first
-                    // part of a weight is never 0 while the weight is not
-                    const float w = exp2f(sc[t][r] - m);
-                    l_run += w;
-                    pb[r] = part_of(w, w > 0.f ? fmaxf(w, MIN_PART) : w);
-                }
-#pragma unroll
-                for (int d0 = 0; d0 < DT; d0 += 4) {
-                    u32x2 v0, v1, v2, v3;
-                    asm volatile(
-                        "ds_read_b64_tr_b16 %0, %4\n\tds_read_b64_tr_b16 %1, %5\n\t"
-                        "ds_read_b64_tr_b16 %2, %6\n\tds_read_b64_tr_b16 %3, %7\n\t"
-                        "s_waitcnt lgkmcnt(0)"
-                        : "=&v"(v0), "=&v"(v1), "=&v"(v2), "=&v"(v3)
-                        : "v"((vtr ^ (32 * d0)) + t * 16 * RB), "v"((vtr ^ (32 * d0 + 32)) + t * 16 * RB),
-                          "v"((vtr ^ (32 * d0 + 64)) + t * 16 * RB), "v"((vtr ^ (32 * d0 + 96)) + t * 16 * RB)
-                        : "memory");
-                    const u32x2 vt[4] = {v0, v1, v2, v3};
-#pragma unroll
-                    for (int x = 0; x < 4; ++x)
-                        acc[d0 + x] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(
-                            __builtin_bit_cast(s16x4, vt[x]), __builtin_bit_cast(s16x4, pb), acc[d0 + x], 0, 0, 0);
-                }
+                for (int x = 0; x < 4; ++x)
+                    acc[d0 + x] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(
+                        __builtin_bit_cast(s16x4, vt[x]), __builtin_bit_cast(s16x4, pb), acc[d0 + x], 0, 0, 0);
             }
         }
+    }
+    // The next unit's K rows are asked for as soon as the scores have taken this one's,
+    // its V rows as soon as the output has.  Loads for which there is no unit read nothing
+    // (a size of 0): a branch around them would make every wait one for all loads.
+    while (u < pages) {
+        const int next = u + hop;
+        const uint32_t bytes = next < pages ? PW * D : 0;
+        const int64_t slice = slice_of(coming);
+        coming = row[2 + min((next + hop) / UPP, cap)];
+        f32x4 sc[4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            sc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int kl = 0; kl < KL; ++kl)
+#pragma unroll
+                for (int hf = 0; hf < 2; ++hf)
+                    sc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8<F>(kw[t][kl][2 * hf], kw[t][kl][2 * hf + 1]),
+                                                                    qf[kl][hf], sc[t], 0, 0, 0);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) sc[t][r] *= ks;
+        }
+        load_k(next, slice, bytes);
+        const float m = soften(sc);
+        u32x4 pb[2];
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; r += 2) {
+                const float w0 = __builtin_amdgcn_exp2f(sc[t][r] - m), w1 = __builtin_amdgcn_exp2f(sc[t][r + 1] - m);
+                l_run += w0 + w1;
+                pb[t >> 1][2 * (t & 1) + r / 2] = parts(w0 * vs, w1 * vs, w0 * vs, w1 * vs);
+            }
+#pragma unroll
+        for (int t = 0; t < DT; ++t)
+#pragma unroll
+            for (int y = 0; y < 2; ++y)
+                acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8<F>(vw[t][2 * y], vw[t][2 * y + 1]),
+                                                                 __builtin_bit_cast(bf16x8, pb[y]), acc[t],
+                                                                 0, 0, 0);
+        load_v(next, slice, bytes);
+        u = next;
     }
 
-    // ---- the waves' results through LDS (over the tail's V rows) ------------------
-    float* r_o = reinterpret_cast<float*>(&lds[0]);  // [wave][column][OST]
-    float* r_m = r_o + WAVES * COLS * OST;           // [wave][column][max, sum]
-    l_run = col_sum(l_run);
-    __syncthreads();
-    if (col < COLS) {
-        float* dst = r_o + (wave * COLS + col) * OST + 4 * quad;
+    // ---- the waves' results ------------------------------------------------------
+    // A q-head's second parts, G columns further, to its first.  Where a value is
+    // infinite the second part may be anything: a finite number leaves the first's
+    // infinity as it is (an fmax ignores a NaN).  A compare and select per element instead
+    // costs a step of one sequence 0.85 us.  Then all waves' sums under one maximum, through
+    // LDS, over the tail's V rows.
 #pragma unroll
-        for (int t = 0; t < DT; ++t) *reinterpret_cast<f32x4*>(dst + 16 * t) = acc[t];
-        if (quad == 0) {
-            r_m[(wave * COLS + col) * 2] = m_run;
-            r_m[(wave * COLS + col) * 2 + 1] = l_run;
+    for (int t = 0; t < DT; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const float lo = __uint_as_float(
+                __builtin_amdgcn_update_dpp(0, __float_as_uint(acc[t][r]), 0x100 + G, 0xf, 0xf, true));  // row_shl:G
+            acc[t][r] += fminf(fmaxf(lo, -FLT_MAX), FLT_MAX);
         }
+    l_run = col_sum(l_run);
+    float* r_m = reinterpret_cast<float*>(&lds[0]);  // [wave][q-head][max, sum]
+    float* r_o = r_m + WAVES * G * 2;                // [wave][q-head][OST]
+    float* r_l = r_o + WAVES * G * OST;              // [q-head]
+    __syncthreads();
+    if (quad == 0 && col < G) {
+        r_m[(wave * G + col) * 2] = m_run;
+        r_m[(wave * G + col) * 2 + 1] = l_run;
     }
     __syncthreads();
-    float* rec = ws + ((int64_t)bh * nsplit + s) * REC;
-    for (int x = tid; x < G * D; x += THREADS) {
-        const int e = x / D, d = x % D;
-        float M = -INFINITY;
+    float M = -INFINITY, l = 0.f;
 #pragma unroll
-        for (int w = 0; w < WAVES; ++w) M = fmaxf(M, r_m[(w * COLS + e) * 2]);
-        float o = 0.f, l = 0.f;
+    for (int w = 0; w < WAVES; ++w) M = fmaxf(M, r_m[(w * G + col % G) * 2]);
+    const float M_use = M == -INFINITY ? 0.f : M;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w)
+        l = fmaf(r_m[(w * G + col % G) * 2 + 1], decay(r_m[(w * G + col % G) * 2] - M_use), l);
+    const float scale = decay(m_run - M_use);
+    if (col < G) {
+        float* dst = r_o + (wave * G + col) * OST + 4 * quad;
+#pragma unroll
+        for (int t = 0; t < DT; ++t) {
+            f32x4 o;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) o[r] = acc[t][r] * scale;
+            *reinterpret_cast<f32x4*>(dst + 16 * t) = o;
+        }
+    }
+    const int64_t rec = bh * nsplit + s;
+    if (tid < G) {  // lane tid of the first wave holds q-head tid's
+        if (nsb == 1) {
+            if (LSE != nullptr) LSE[orow + tid] = (M + log2f(l)) * LN2;
+        } else {
+            float* ml = ws + (int64_t)gridDim.x * Hkv * nsplit * G * D + (rec * G + tid) * 2;
+            ml[0] = M;
+            ml[1] = l;
+        }
+        r_l[tid] = l;
+    }
+    __syncthreads();
+    for (int x = tid; x < G * D / 4; x += THREADS) {
+        const int e = x / (D / 4), d = x % (D / 4) * 4;
+        f32x4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int w = 0; w < WAVES; ++w) {
-            const float mw = r_m[(w * COLS + e) * 2];
-            const float sw = mw == -INFINITY ? 0.f : exp2f(mw - M);
-            float ow = r_o[(w * COLS + e) * OST + d];
-            // an infinite first part leaves no number in the other
-            ow = fabsf(ow) < INFINITY ? ow + r_o[(w * COLS + G + e) * OST + d] : ow;
-            o = fmaf(ow, sw, o);
-            l = fmaf(r_m[(w * COLS + e) * 2 + 1], sw, l);
+            const f32x4 y = *reinterpret_cast<const f32x4*>(r_o + (w * G + e) * OST + d);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) o[r] += y[r];
         }
         if (nsb == 1) {
-            O[orow * D + x] = (__bf16)(o / l);
-            if (d == 0 && LSE != nullptr) LSE[orow + e] = (M + log2f(l)) * LN2;
+            const float sum = r_l[e];
+            *reinterpret_cast<bf16x4*>(O + orow * D + 4 * x) =
+                bf16x4{(__bf16)(o[0] / sum), (__bf16)(o[1] / sum), (__bf16)(o[2] / sum), (__bf16)(o[3] / sum)};
         } else {
-            rec[e * (D + 2) + 2 + d] = o;
-            if (d == 0) {
-                rec[e * (D + 2)] = M;
-                rec[e * (D + 2) + 1] = l;
-            }
+            *reinterpret_cast<f32x4*>(ws + rec * (G * D) + 4 * x) = o;
         }
     }
 }
 
-// Sum of the split records of one (sequence, kv-head), in split order, eight loads
-// at a time; a thread owns one (q-head, dim).
+// Sum of the splits' records of one q-head, in split order.  Records: every split's
+// sums [G][D], then every split's [G][max, sum].  Lane q holds the maximum and the sum
+// of split q, so that one round trip brings all weights; the sums follow eight loads
+// at a time.
 template <int D, int G, int PW>
-__global__ __launch_bounds__(THREADS) void merge_q8_kernel(const int32_t* __restrict__ seq_lens,
-                                                           const int32_t* __restrict__ plan, int32_t stride,
-                                                           int32_t cap, __bf16* __restrict__ O, float* __restrict__ LSE,
-                                                           const float* __restrict__ ws, int32_t Hkv, int32_t nsplit) {
-    constexpr int REC = G * (D + 2);
-    constexpr int U = 8;
-    const int bh = blockIdx.x;
-    const int h = bh % Hkv;
-    const int b = bh / Hkv;
-    const int64_t orow = (int64_t)b * Hkv * G + h * G;
+__global__ __launch_bounds__(D) void merge_q8_kernel(const int32_t* __restrict__ seq_lens,
+                                                     const int32_t* __restrict__ plan, int32_t stride, int32_t cap,
+                                                     __bf16* __restrict__ O, float* __restrict__ LSE,
+                                                     const float* __restrict__ ws, int32_t Hkv,
+                                                     int32_t nsplit) {
+    const int b = blockIdx.x, h = blockIdx.y, e = blockIdx.z;
+    const int64_t bh = (int64_t)b * Hkv + h;
+    const int d = threadIdx.x, lane = d & 63;
     View sv;
-    if (!view<PW>(seq_lens, plan + (int64_t)b * stride, cap, b, &sv)) return;  // NaN stands there already
-    const int ups = units_per_split(sv.units, nsplit);
-    const int nsb = (sv.units + ups - 1) / ups;
-    if (nsb <= 1) return;  // so does the result
-    const float* recs = ws + (int64_t)bh * nsplit * REC;
-    for (int x = threadIdx.x; x < G * D; x += THREADS) {
-        const int e = x / D, d = x % D;
-        float M = -INFINITY, l = 0.f, o = 0.f;
-        for (int q0 = 0; q0 < nsb; q0 += U) {
-            float mq[U], lq[U], oq[U], mm = M;
+    const bool ok = view<PW>(seq_lens, plan + (int64_t)b * stride, cap, b, &sv);
+    const int nsb = splits_used(sv.units, nsplit);
+    const float* ml = ws + ((int64_t)gridDim.x * Hkv * nsplit * D + (bh * nsplit + min(lane, nsplit - 1)) * 2) * G + e * 2;
+    float m = ml[0];
+    const float l = ml[1];
+    if (!ok || nsb <= 1) return;  // NaN or the result stands there already
+    if (lane >= nsb) m = -INFINITY;
+    float M = m;
 #pragma unroll
-            for (int i = 0; i < U; ++i) {
-                const bool in = q0 + i < nsb;
-                const float* r = recs + (int64_t)(in ? q0 + i : 0) * REC + e * (D + 2);
-                mq[i] = in ? r[0] : -INFINITY;
-                lq[i] = in ? r[1] : 0.f;
-                oq[i] = in ? r[2 + d] : 0.f;
-            }
+    for (int x = 32; x > 0; x >>= 1) M = fmaxf(M, __shfl_xor(M, x));
+    const float w = decay(m - (M == -INFINITY ? 0.f : M));  // 0 past the splits
+    float L = lane < nsb ? l * w : 0.f;
 #pragma unroll
-            for (int i = 0; i < U; ++i) mm = fmaxf(mm, mq[i]);
-            if (mm == -INFINITY) continue;
-            const float a = exp2f(M - mm);  // 0 while nothing is accumulated
-            l *= a;
-            o *= a;
+    for (int x = 32; x > 0; x >>= 1) L += __shfl_xor(L, x);
+    const float* src = ws + (bh * nsplit * G + e) * D + d;
+    float o = 0.f;
+    constexpr int U = 8;
+    for (int q0 = 0; q0 < nsb; q0 += U) {
+        float y[U];
 #pragma unroll
-            for (int i = 0; i < U; ++i) {
-                const float w = mq[i] == -INFINITY ? 0.f : exp2f(mq[i] - mm);
-                l = fmaf(lq[i], w, l);
-                o = fmaf(oq[i], w, o);
-            }
-            M = mm;
-        }
-        O[orow * D + x] = (__bf16)(o / l);
-        if (d == 0 && LSE != nullptr) LSE[orow + e] = (M + log2f(l)) * LN2;
+        for (int i = 0; i < U; ++i) y[i] = src[(int64_t)min(q0 + i, nsb - 1) * (G * D)];
+#pragma unroll
+        for (int i = 0; i < U; ++i)
+            if (q0 + i < nsb) o = fmaf(y[i], __shfl(w, q0 + i), o);
     }
+    const int64_t at = bh * G + e;
+    O[at * D + d] = (__bf16)(o / L);
+    if (d == 0 && LSE != nullptr) LSE[at] = (M + log2f(L)) * LN2;
 }
 
 struct Args {
@@ -407,14 +479,14 @@ struct Args {
 
 template <class F, int D, int G, int PW>
 hipError_t launch_pw(const Args& a, hipStream_t st) {
-    const int64_t rows = (int64_t)a.batch * a.Hkv;
-    hipLaunchKernelGGL((decode_q8_kernel<F, D, G, PW>), dim3((unsigned)(rows * a.nsplit)), dim3(THREADS), 0, st,
+    hipLaunchKernelGGL((decode_q8_kernel<F, D, G, PW>), dim3((unsigned)a.batch, (unsigned)a.Hkv, (unsigned)a.nsplit),
+                       dim3(THREADS), 0, st,
                        (const __bf16*)a.Q, (const uint8_t*)a.K, (const uint8_t*)a.V, a.k_scale, a.v_scale,
                        (const __bf16*)a.k_tail, (const __bf16*)a.v_tail, a.seq_lens, a.num_pages, a.plan, a.stride,
                        a.stride - 3, (__bf16*)a.O, a.LSE, a.ws, a.Hkv, a.nsplit, LOG2E / sqrtf((float)D));
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.nsplit <= 1) return e;
-    hipLaunchKernelGGL((merge_q8_kernel<D, G, PW>), dim3((unsigned)rows), dim3(THREADS), 0, st, a.seq_lens, a.plan,
+    hipLaunchKernelGGL((merge_q8_kernel<D, G, PW>), dim3((unsigned)a.batch, (unsigned)a.Hkv, G), dim3(D), 0, st, a.seq_lens, a.plan,
                        a.stride, a.stride - 3, (__bf16*)a.O, a.LSE, a.ws, a.Hkv, a.nsplit);
     return hipGetLastError();
 }
@@ -433,16 +505,21 @@ hipError_t launch_d(const Args& a, int32_t G, int32_t B, hipStream_t st) {
     }
 }
 
-// Splits of a (sequence, kv-head): enough workgroups for the chip's compute units
-// (twice over), no more than a full plan row has rounds of WAVES units.
-constexpr int64_t WANTED_GROUPS = 512;
-constexpr int64_t MOST_SPLITS = 64;
+// Splits of a (sequence, kv-head) whose plan row holds `units` of 64 keys: one
+// workgroup per compute unit, and no split without a round of units for each of its
+// waves.  A round takes some 1.3 us, the merge 2 to 3 and a launch more: a list is cut
+// where that saves three rounds.  us, uncut / cut: 12 units, 1 sequence of 8 kv-heads
+// 8.8 / 8.4; 33 units 18.1 / 9.3; 128 units, 4 sequences 57 / 17.  Twice the workgroups:
+// 128 units, 4 sequences 17.5, 16 sequences 41.6 for 40.6; 1024 units, 1 sequence 31 for 28.
+// More than 32 splits cost the merge more than they save: 256 units, 2 kv-heads 16 for 14.
+constexpr int64_t WANTED_GROUPS = 256, MOST_SPLITS = 32;
 int32_t splits(int64_t rows, int64_t plan_stride, int32_t B) {
     const int64_t units = (plan_stride - 2) * (B / UNIT);
     const int64_t rounds = (units + WAVES - 1) / WAVES;
-    int64_t n = rows > 0 ? (WANTED_GROUPS + rows - 1) / rows : 1;
+    int64_t n = rows > 0 ? WANTED_GROUPS / rows : 1;
     if (n > rounds) n = rounds;
-    return (int32_t)(n < 1 ? 1 : n > MOST_SPLITS ? MOST_SPLITS : n);
+    if (n > MOST_SPLITS) n = MOST_SPLITS;
+    return n < 2 || rounds - (rounds + n - 1) / n < 3 ? 1 : (int32_t)n;
 }
 
 int64_t ws_bytes(int64_t rows, int32_t G, int32_t d, int32_t nsplit) {
