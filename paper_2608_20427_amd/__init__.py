@@ -192,10 +192,12 @@ def check_buffer(t, name, shape, dtype, device):
     and `dtype` on `device`.  Every buffer handed to the library goes through
     this check before its pointer is taken: a host tensor, or one of another
     size, would otherwise become a kernel access outside the intended memory."""
+    try:
+        if t.dtype is dtype and t.shape == shape and t.device == device and t.is_contiguous():
+            return t
+    except AttributeError:
+        pass  # no tensor: named below
     import torch
-    if isinstance(t, torch.Tensor) and t.dtype is dtype and t.shape == shape and t.device == device \
-            and t.is_contiguous():
-        return t
     if not isinstance(t, torch.Tensor):
         raise ValueError(f"{name} must be a tensor, got {type(t).__name__}")
     if t.device != device:
@@ -523,9 +525,9 @@ def _empty(shape, dtype, device, stream):
     """An output or scratch tensor whose memory belongs to the stream it is used on."""
     import torch
     if stream is None:
-        return torch.empty(shape, dtype=dtype, device=device)
+        return torch.empty(*shape, dtype=dtype, device=device)  # a tuple for a size costs 0.5 us more
     with torch.cuda.stream(stream):
-        return torch.empty(shape, dtype=dtype, device=device)
+        return torch.empty(*shape, dtype=dtype, device=device)
 
 
 class PageStep(NamedTuple):
@@ -553,31 +555,37 @@ def page_step(seq_lens, new_lens, page_table, free_pages, free_head, max_tokens,
     max_tokens has no place, nor do those behind it in its sequence: the returned
     seq_lens count what was placed."""
     import torch
-    _i32_cuda(seq_lens, "seq_lens", 1)
-    dev = seq_lens.device
-    _i32_cuda(page_table, "page_table", 2, dev)
+    dev = _cuda_device(page_table, "page_table")
+    if page_table.dim() != 2:
+        raise ValueError("page_table must be a 2-D tensor [batch, max_pages]")
     batch, max_pages = page_table.shape
+    check_buffer(page_table, "page_table", page_table.shape, torch.int32, dev)
     check_buffer(seq_lens, "seq_lens", (batch,), torch.int32, dev)
     check_buffer(new_lens, "new_lens", (batch,), torch.int32, dev)
-    _i32_cuda(free_pages, "free_pages", 1, dev)
+    if not isinstance(free_pages, torch.Tensor) or free_pages.dim() != 1:
+        raise ValueError("free_pages must be a 1-D tensor")
+    check_buffer(free_pages, "free_pages", free_pages.shape, torch.int32, dev)
     check_buffer(free_head, "free_head", (1,), torch.int32, dev)
     max_tokens = int(max_tokens)
     if max_tokens < 0:
         raise ValueError("max_tokens must not be negative")
-    sizes = (batch, batch + 1, batch + 1, max_tokens, max_tokens, 1)
     if out is None:
-        words = batch + 2 * (batch + 1) + max_tokens + 1
-        pad = (words + 1) & ~1  # slots are 8-byte entries behind the others
-        buf = _empty((pad + 2 * max_tokens,), torch.int32, dev, stream)
-        a, b, c, d, e, slots = buf.split((batch, batch + 1, batch + 1, max_tokens, 1 + pad - words, 2 * max_tokens))
-        out = PageStep(a, b, c, d, slots.view(torch.int64), e[:1])
+        # one allocation, slots (8 bytes) first; 4 us less than one each
+        buf = _empty((3 * max_tokens + 3 * batch + 3,), torch.int32, dev, stream)
+        slots, *rest = torch.unsafe_split_with_sizes(
+            buf, (2 * max_tokens, batch, batch + 1, batch + 1, max_tokens, 1))
+        lens, tstart, bstart, positions, head = rest
+        out = PageStep(lens, tstart, bstart, positions, slots.view(torch.int64), head)
     else:
         out = PageStep(*out)
+        sizes = (batch, batch + 1, batch + 1, max_tokens, max_tokens, 1)
         for name, t, size in zip(PageStep._fields, out, sizes):
             check_buffer(t, name, (size,), torch.int64 if name == "slots" else torch.int32, dev)
-    _call(load().bf1_page_step, "bf1_page_step", dev, stream, batch, _ptr(seq_lens), _ptr(new_lens), _ptr(page_table),
-          max_pages, _ptr(free_pages), free_pages.shape[0], _ptr(free_head), int(B), max_tokens, _ptr(out.seq_lens),
-          _ptr(out.token_start), _ptr(out.block_start), _ptr(out.positions), _ptr(out.slots), _ptr(out.free_head))
+    lens, tstart, bstart, positions, slots, head = out
+    _call(load().bf1_page_step, "bf1_page_step", dev, stream, batch, seq_lens.data_ptr(), new_lens.data_ptr(),
+          page_table.data_ptr(), max_pages, free_pages.data_ptr(), free_pages.shape[0], free_head.data_ptr(), int(B),
+          max_tokens, lens.data_ptr(), tstart.data_ptr(), bstart.data_ptr(), positions.data_ptr(), slots.data_ptr(),
+          head.data_ptr())
     return out
 
 
@@ -622,20 +630,21 @@ def _rope_side(x, name, dim, lead, d, dtype, dev, out, out_dtype, stream):
     import torch
     if not isinstance(x, torch.Tensor) or x.device != dev or x.dtype != dtype or x.dim() != dim:
         raise ValueError(f"{name} must be a {dim}-D {dtype} tensor on {dev}")
-    shape = x.shape
+    shape, s = x.shape, x.stride()
     rows = (1, shape[0]) if dim == 3 else (shape[0], shape[2])
     if rows != lead or shape[-1] != d:
         raise ValueError(f"{name} must agree with the other operand in every size but the heads")
-    if x.stride(-1) != 1:
+    if s[-1] != 1:
         raise ValueError(f"{name} must have the elements of a head side by side")
     if out is None:
         out = _empty(shape, out_dtype, dev, stream)
     else:
         check_buffer(out, name + "_out", shape, out_dtype, dev)
-    s, o = x.stride(), out.stride()
     if dim == 3:  # rows [tokens, heads, d]
-        return out, shape[1], (0, s[1], s[0], 0, o[1], o[0])
-    return out, shape[1], (s[0], s[1], s[2], o[0], o[1], o[2])
+        h = shape[1]
+        return out, h, (0, s[1], s[0], 0, d, h * d)
+    _, h, n, _ = shape
+    return out, h, (s[0], s[1], s[2], h * n * d, n * d, d)
 
 
 def _rope(q, k, positions, freqs, interleaved, amplitude, transposed, q_out, k_out, dtype, stream):
@@ -698,11 +707,14 @@ def _step_rows(k, v, Hkv, d, dev):
     """Check a step's rows k, v [tokens, Hkv, d] (strided rows and heads)."""
     import torch
     for name, x in (("k", k), ("v", v)):
-        if not isinstance(x, torch.Tensor) or x.device != dev or x.dtype != torch.bfloat16 or x.dim() != 3:
+        if not isinstance(x, torch.Tensor) or x.device != dev or x.dtype is not torch.bfloat16 or x.dim() != 3:
             raise ValueError(f"{name} must be a bf16 tensor [tokens, Hkv, d] on {dev}")
-        if x.shape[0] != k.shape[0] or x.shape[1] != Hkv or x.shape[2] != d or x.stride(2) != 1:
-            raise ValueError(f"{name} must have shape ({k.shape[0]}, {Hkv}, {d}) with the elements of a head side by side")
-    return k.shape[0], (k.stride(0), k.stride(1), v.stride(0), v.stride(1))
+    shape, (kt, kh, ke), (vt, vh, ve) = k.shape, k.stride(), v.stride()
+    if shape[1:] != (Hkv, d) or ke != 1:
+        raise ValueError(f"k must have shape (tokens, {Hkv}, {d}) with the elements of a head side by side")
+    if v.shape != shape or ve != 1:
+        raise ValueError(f"v must have shape {tuple(shape)} with the elements of a head side by side")
+    return shape[0], (kt, kh, vt, vh)
 
 
 def kv_append(k, v, slots, k_pages, v_pages, stream=None):
@@ -774,7 +786,8 @@ def kv_append_q8(k, v, lens_before, seq_lens, token_start, block_start, page_tab
     block go to its tail.  lens_before: the lengths page_step was given; seq_lens,
     token_start and block_start: what it returned; page_table: what it updated."""
     import torch
-    _i32_cuda(page_table, "page_table", 2)
+    if not isinstance(page_table, torch.Tensor) or page_table.dim() != 2:
+        raise ValueError("page_table must be a 2-D tensor [batch, max_pages]")
     batch, max_pages = page_table.shape
     dev, num_pages, Hkv, B, d, fmt = _cache_q8(cache, batch)
     check_buffer(page_table, "page_table", page_table.shape, torch.int32, dev)
@@ -783,9 +796,11 @@ def kv_append_q8(k, v, lens_before, seq_lens, token_start, block_start, page_tab
     check_buffer(token_start, "token_start", (batch + 1,), torch.int32, dev)
     check_buffer(block_start, "block_start", (batch + 1,), torch.int32, dev)
     tokens, strides = _step_rows(k, v, Hkv, d, dev)
-    _call(load().bf1_kv_append_q8, "bf1_kv_append_q8", dev, stream, _ptr(k), _ptr(v), *strides, tokens, batch,
-          _ptr(lens_before), _ptr(seq_lens), _ptr(token_start), _ptr(block_start), _ptr(page_table), max_pages,
-          num_pages, *map(_ptr, cache), Hkv, d, B, fmt)
+    kp, vp, ks, vs, kt, vt = cache
+    _call(load().bf1_kv_append_q8, "bf1_kv_append_q8", dev, stream, k.data_ptr(), v.data_ptr(), *strides, tokens, batch,
+          lens_before.data_ptr(), seq_lens.data_ptr(), token_start.data_ptr(), block_start.data_ptr(),
+          page_table.data_ptr(), max_pages, num_pages, kp.data_ptr(), vp.data_ptr(), ks.data_ptr(), vs.data_ptr(),
+          kt.data_ptr(), vt.data_ptr(), Hkv, d, B, fmt)
 
 
 def decode_q8_workspace_size(batch, Hq, Hkv, head_dim, B, stride):
@@ -803,14 +818,15 @@ def attn_decode_q8(q, cache, seq_lens, plan, B=64, out=None, lse=None, workspace
     dev = _cuda_device(q, "q")
     if q.dim() != 3:
         raise ValueError("q must be 3-D [batch, Hq, d]")
-    batch, Hq, d = q.shape
-    check_buffer(q, "q", q.shape, torch.bfloat16, dev)
+    batch, Hq, d = shape = q.shape
+    check_buffer(q, "q", shape, torch.bfloat16, dev)
     where, num_pages, Hkv, pw, dk, fmt = _cache_q8(cache, batch)
     if where != dev or dk != d or pw != B:
         raise ValueError("the cache must have q's device and head size, and pages of B tokens")
     _i32_cuda(seq_lens, "seq_lens", 1, dev)
     _i32_cuda(plan, "plan", 2, dev)
-    if seq_lens.shape[0] != batch or plan.shape[0] != batch:
+    rows, stride = plan.shape
+    if seq_lens.shape[0] != batch or rows != batch:
         raise ValueError("batch sizes disagree")
     if out is None:
         out = _empty(q.shape, torch.bfloat16, dev, stream)
@@ -820,13 +836,14 @@ def attn_decode_q8(q, cache, seq_lens, plan, B=64, out=None, lse=None, workspace
         lse = _empty((batch, Hq), torch.float32, dev, stream)
     else:
         check_buffer(lse, "lse", (batch, Hq), torch.float32, dev)
-    stride = plan.shape[1]
     need = decode_q8_workspace_size(batch, Hq, Hkv, d, B, stride)
-    if workspace is None:
-        workspace = _empty((need,), torch.uint8, dev, stream) if need else None
-        ws_bytes = need
-    else:
+    ws_bytes = need
+    if workspace is not None:
         ws_bytes = check_workspace(workspace, "workspace", need, dev)
-    _call(load().bf1_decode_attn_q8, "bf1_decode_attn_q8", dev, stream, _ptr(q), *map(_ptr, cache), _ptr(seq_lens),
-          num_pages, _ptr(plan), stride, _ptr(out), _ptr(lse), batch, Hq, Hkv, d, int(B), fmt, _ptr(workspace), ws_bytes)
+    elif need:
+        workspace = _empty((need,), torch.uint8, dev, stream)
+    kp, vp, ks, vs, kt, vt = cache
+    _call(load().bf1_decode_attn_q8, "bf1_decode_attn_q8", dev, stream, q.data_ptr(), kp.data_ptr(), vp.data_ptr(),
+          ks.data_ptr(), vs.data_ptr(), kt.data_ptr(), vt.data_ptr(), seq_lens.data_ptr(), num_pages, plan.data_ptr(),
+          stride, out.data_ptr(), lse.data_ptr(), batch, Hq, Hkv, d, int(B), fmt, _ptr(workspace), ws_bytes)
     return out, lse
