@@ -6,6 +6,8 @@
 #include <math.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "../../include/bf1.h"
 #include "bf1_device.h"
 
@@ -19,28 +21,41 @@ bool aligned(const void* p, uintptr_t a) { return p != nullptr && reinterpret_ca
 // A launch has fewer than 2^32 threads.
 bool launchable(int64_t blocks) { return blocks < (int64_t(1) << 32) / THREADS; }
 
-// Exclusive prefix sum of x over the workgroup in thread order; *total gets the
-// sum.  `part` is one slot per wave; ends with the slots free for the next call.
-template <typename T>
-__device__ __forceinline__ T group_scan(T x, T* part, T* total) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    T inc = x;
-#pragma unroll
-    for (int m = 1; m < 64; m <<= 1) {
-        const T y = __shfl_up(inc, m);
-        if (lane >= m) inc += y;
-    }
-    if (lane == 63) part[wave] = inc;
+__device__ __forceinline__ uint32_t add_sat(uint32_t a, uint32_t b) { return __builtin_elementwise_add_sat(a, b); }
+
+// Inclusive prefix sum over the wave in lane order, saturating (so that a sum past 32
+// bits stays the largest number), by lane moves in the vector ALU.
+__device__ __forceinline__ uint32_t wave_scan(uint32_t x) {
+#define BF1_SCAN_STEP(ctrl, rows) \
+    x = add_sat(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, ctrl, rows, 0xf, false))
+    BF1_SCAN_STEP(0x111, 0xf);  // row_shr:1, 2, 4, 8: within 16 lanes
+    BF1_SCAN_STEP(0x112, 0xf);
+    BF1_SCAN_STEP(0x114, 0xf);
+    BF1_SCAN_STEP(0x118, 0xf);
+    BF1_SCAN_STEP(0x142, 0xa);  // row_bcast:15 into rows 1 and 3
+    BF1_SCAN_STEP(0x143, 0xc);  // row_bcast:31 into rows 2 and 3
+#undef BF1_SCAN_STEP
+    return x;
+}
+
+// Exclusive prefix sum of x over the workgroup in thread order, saturating; *total gets
+// the sum.  `part` is one slot per wave, another call's are its own.
+__device__ __forceinline__ uint32_t group_scan(uint32_t x, uint32_t* part, uint32_t* total) {
+    const int wave = threadIdx.x >> 6;
+    const uint32_t inc = wave_scan(x);
+    if ((threadIdx.x & 63) == 63) part[wave] = inc;
     __syncthreads();
-    T before = 0, all = 0;
+    uint32_t before = 0, all = 0;
 #pragma unroll
     for (int w = 0; w < THREADS / 64; ++w) {
-        if (w < wave) before += part[w];
-        all += part[w];
+        const uint32_t p = part[w];
+        if (w < wave) before = add_sat(before, p);
+        all = add_sat(all, p);
     }
-    __syncthreads();
     *total = all;
-    return before + inc - x;
+    // the wave's sum without this lane: its left neighbour's
+    const uint32_t left = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)inc, 0x138, 0xf, 0xf, false);  // wave_shr:1
+    return add_sat(before, left);
 }
 
 // ---------------------------------------------------------------------------
@@ -53,103 +68,102 @@ __device__ __forceinline__ T group_scan(T x, T* part, T* total) {
 // binary search.  A new page starts with a new token, so the row of that token
 // writes the table entry, and no row reads an entry that this launch writes.
 //
-// Bound by latency: 20 bytes per sequence and 12 per row.  Every workgroup sums
-// the batch for itself (SEQS sequences at a time), so that one launch does it.
-constexpr int SPT = 4;                // sequences per thread and round
+// Bound by latency: 20 bytes per sequence and 12 per row.  Every workgroup sums the
+// batch for itself (SEQS sequences at a time), so that one launch does it.
+constexpr int SPT = 4;                   // sequences per thread and round
 constexpr int SEQS = THREADS * SPT;
-constexpr int ROWS_PER_GROUP = 1024;  // rows of a workgroup
-
-__device__ __forceinline__ int32_t clamp_i32(int64_t x) { return x > INT32_MAX ? INT32_MAX : (int32_t)x; }
+constexpr int ROWS_PER_GROUP = THREADS;  // a row per thread
 
 __global__ __launch_bounds__(THREADS) void page_step_kernel(
     int32_t batch, const int32_t* __restrict__ seq_lens, const int32_t* __restrict__ new_lens, int32_t* page_table,
     int32_t max_pages, const int32_t* __restrict__ free_pages, int32_t num_free, const int32_t* __restrict__ free_head,
-    int32_t shift, int64_t max_tokens, int32_t* __restrict__ lens_out, int32_t* __restrict__ token_start,
+    int32_t shift, int32_t max_tokens, int32_t* __restrict__ lens_out, int32_t* __restrict__ token_start,
     int32_t* __restrict__ block_start, int32_t* __restrict__ positions, int64_t* __restrict__ slots,
     int32_t* __restrict__ head_out) {
-    __shared__ int64_t part64[THREADS / 64];
-    __shared__ int32_t part32[THREADS / 64];
-    __shared__ int32_t s_start[SEQS];   // first row
+    __shared__ uint32_t part[3][THREADS / 64];
+    __shared__ uint32_t s_start[SEQS];  // first row
     __shared__ int32_t s_old[SEQS], s_placed[SEQS], s_rank[SEQS];
     const int tid = threadIdx.x;
     const bool writer = blockIdx.x == 0;  // the per-sequence results
-    const int64_t t0 = (int64_t)blockIdx.x * ROWS_PER_GROUP;
-    const int64_t t1 = min(max_tokens, t0 + ROWS_PER_GROUP);
+    const uint32_t t0 = blockIdx.x * (uint32_t)ROWS_PER_GROUP;
+    const uint32_t t1 = min((uint32_t)max_tokens, t0 + ROWS_PER_GROUP);
+    const uint32_t t = t0 + tid;
     const int32_t B = 1 << shift;
-    const int64_t head = min(max(*free_head, 0), num_free);
+    const int32_t head = min(max(*free_head, 0), num_free);
+    const int32_t left = num_free - head;  // free pages
     const int64_t room = min((int64_t)max_pages << shift, (int64_t)INT32_MAX);
-    int64_t rows = 0, pages = 0;  // sums over the sequences before this round
-    int32_t blocks = 0, taken = 0;
+    uint32_t rows = 0, pages = 0, blocks = 0;  // sums over the sequences before this round
     for (int32_t b0 = 0; b0 < batch; b0 += SEQS) {
-        int64_t old[SPT], want[SPT], w_sum = 0;
+        const int32_t count = min(SEQS, batch - b0);
+        int32_t old[SPT], want[SPT];
+        uint32_t sum = 0, all;
 #pragma unroll
         for (int i = 0; i < SPT; ++i) {
-            const int32_t b = b0 + tid * SPT + i;
-            old[i] = b < batch ? max(seq_lens[b], 0) : 0;
-            want[i] = b < batch ? max(new_lens[b], 0) : 0;
-            w_sum += want[i];
+            const int32_t s = tid * SPT + i;
+            old[i] = s < count ? max(seq_lens[b0 + s], 0) : 0;
+            want[i] = s < count ? max(new_lens[b0 + s], 0) : 0;
+            sum = add_sat(sum, (uint32_t)want[i]);
         }
-        int64_t w_all, n_all;
-        int64_t row = rows + group_scan(w_sum, part64, &w_all);
-        int64_t fit[SPT], need[SPT], n_sum = 0;
-        int64_t at = row;
+        uint32_t at = add_sat(rows, group_scan(sum, part[0], &all));
+        const uint32_t rows_after = add_sat(rows, all);
+        int32_t fit[SPT];
+        uint32_t need[SPT];
+        sum = 0;
 #pragma unroll
         for (int i = 0; i < SPT; ++i) {
-            fit[i] = max((int64_t)0, min(min(want[i], room - old[i]), max_tokens - at));
-            at += want[i];
-            need[i] = fit[i] > 0 ? ((old[i] + fit[i] + B - 1) >> shift) - ((old[i] + B - 1) >> shift) : 0;
-            n_sum += need[i];
+            s_start[tid * SPT + i] = at;
+            const int64_t f = min(min((int64_t)want[i], room - old[i]), (int64_t)max_tokens - at);
+            fit[i] = f > 0 ? (int32_t)f : 0;
+            at = add_sat(at, (uint32_t)want[i]);
+            need[i] = fit[i] > 0 ? (uint32_t)((((int64_t)old[i] + fit[i] + B - 1) >> shift) -
+                                              (((int64_t)old[i] + B - 1) >> shift))
+                                 : 0;
+            sum += need[i];
         }
-        int64_t rank = pages + group_scan(n_sum, part64, &n_all);
-        int32_t b_sum = 0, g_sum = 0;
-        int32_t touched[SPT];
-        int64_t rk = rank;
-        at = row;
+        uint32_t rank = pages + group_scan(sum, part[1], &all);
+        pages += all;
+        uint32_t touched[SPT];
+        sum = 0;
 #pragma unroll
         for (int i = 0; i < SPT; ++i) {
-            const int64_t have = (old[i] + B - 1) >> shift;
-            const int64_t got = min(max(num_free - head - rk, (int64_t)0), need[i]);
-            const int64_t placed = need[i] > got ? max(min(fit[i], ((have + got) << shift) - old[i]), (int64_t)0) : fit[i];
-            touched[i] = placed > 0 ? (int32_t)(((old[i] + placed - 1) >> shift) - (old[i] >> shift) + 1) : 0;
-            b_sum += touched[i];
-            g_sum += (int32_t)got;
             const int s = tid * SPT + i;
-            s_start[s] = clamp_i32(at);
-            s_old[s] = (int32_t)old[i];
-            s_placed[s] = (int32_t)placed;
-            s_rank[s] = clamp_i32(head + rk);
-            rk += need[i];
-            at += want[i];
+            const int64_t have = ((int64_t)old[i] + B - 1) >> shift;
+            const uint32_t got = rank < (uint32_t)left ? min((uint32_t)left - rank, need[i]) : 0;
+            const int32_t placed =
+                need[i] > got ? (int32_t)max(min((int64_t)fit[i], ((have + got) << shift) - old[i]), (int64_t)0) : fit[i];
+            touched[i] = placed > 0 ? (uint32_t)((old[i] + placed - 1) >> shift) - (uint32_t)(old[i] >> shift) + 1 : 0;
+            sum += touched[i];
+            s_old[s] = old[i];
+            s_placed[s] = placed;
+            s_rank[s] = head + (int32_t)min(rank, (uint32_t)left);
+            rank += need[i];
         }
-        int32_t b_all, g_all;
-        int32_t blk = blocks + group_scan(b_sum, part32, &b_all);
-        group_scan(g_sum, part32, &g_all);
         if (writer) {
+            uint32_t blk = blocks + group_scan(sum, part[2], &all);
+            blocks += all;
 #pragma unroll
             for (int i = 0; i < SPT; ++i) {
-                const int32_t s = tid * SPT + i, b = b0 + s;
-                if (b < batch) {
-                    lens_out[b] = s_old[s] + s_placed[s];
-                    token_start[b] = s_start[s];
-                    block_start[b] = blk;
+                const int32_t s = tid * SPT + i;
+                if (s < count) {
+                    lens_out[b0 + s] = s_old[s] + s_placed[s];
+                    token_start[b0 + s] = (int32_t)min(s_start[s], (uint32_t)INT32_MAX);
+                    block_start[b0 + s] = (int32_t)blk;
                 }
                 blk += touched[i];
             }
+        } else {
+            __syncthreads();
         }
-        // the rows of this round's sequences among this workgroup's
-        const int64_t lo = max(t0, rows), hi = min(t1, rows + w_all);
-        const int32_t count = min(SEQS, batch - b0);
-        for (int64_t t = lo + tid; t < hi; t += THREADS) {
-            int32_t s = 0;  // the last sequence that starts at or before row t
-            for (int32_t step = SEQS / 2; step > 0; step >>= 1)
+        if (t >= rows && t < min(t1, rows_after)) {  // this thread's row is one of this round's sequences'
+            int32_t s = 0;  // the last one that starts at or before it
+            for (int32_t step = 1 << (31 - __builtin_clz(count)); step > 0; step >>= 1)
                 if (s + step < count && s_start[s + step] <= t) s += step;
-            const int64_t i = t - s_start[s];
+            const int32_t i = (int32_t)(t - s_start[s]), o = s_old[s];
             int32_t pos = -1;
             int64_t slot = -1;
             if (i < s_placed[s]) {
-                pos = s_old[s] + (int32_t)i;
-                const int32_t block = pos >> shift;
-                const int32_t have = (int32_t)(((int64_t)s_old[s] + B - 1) >> shift);
+                pos = o + i;
+                const int32_t block = pos >> shift, have = (int32_t)(((int64_t)o + B - 1) >> shift);
                 int32_t* entry = page_table + (int64_t)(b0 + s) * max_pages + block;
                 int32_t page;
                 if (block < have) {
@@ -163,21 +177,18 @@ __global__ __launch_bounds__(THREADS) void page_step_kernel(
             positions[t] = pos;
             slots[t] = slot;
         }
-        rows += w_all;
-        pages += n_all;
-        blocks += b_all;
-        taken += g_all;
+        rows = rows_after;
         if (!writer && rows >= t1) return;
         __syncthreads();  // before the next round's sequences take their places
     }
-    for (int64_t t = max(t0, rows) + tid; t < t1; t += THREADS) {
+    if (t >= rows && t < t1) {
         positions[t] = -1;
         slots[t] = -1;
     }
     if (writer && tid == 0) {
-        token_start[batch] = clamp_i32(rows);
-        block_start[batch] = blocks;
-        *head_out = (int32_t)head + taken;
+        token_start[batch] = (int32_t)min(rows, (uint32_t)INT32_MAX);
+        block_start[batch] = (int32_t)blocks;
+        *head_out = head + (int32_t)min(pages, (uint32_t)left);
     }
 }
 
@@ -191,8 +202,10 @@ __global__ __launch_bounds__(THREADS) void page_step_kernel(
 // copied.  The angle is formed in 64 bits and reduced to a part of a turn there,
 // so that far positions lose nothing; cosine and sine are fp32.
 //
-// A lane owns P pairs of one token, 16 bytes of each half of the head, and walks
-// over heads with its cosines and sines in registers.
+// A lane owns P pairs of one token, 16 bytes of each half of the head, in HB heads.
+// Workgroups follow each other over the heads of the same tokens, so that rows of joined
+// projections are read where they lie: 32768 rows, 16 + 8 heads of 128, 83 us (403 MB,
+// 4.8 TB/s; a large copy reaches 5.0), 93 with the heads' workgroups far apart.
 struct RopeSide {
     const void* in;
     void* out;
@@ -240,13 +253,14 @@ __device__ __forceinline__ void store_n(T* p, const float* f) {
     }
 }
 
-template <typename TI, typename TO, bool INTER, int P>
+template <typename TI, typename TO, bool INTER, int P, int HB>
 __global__ __launch_bounds__(THREADS) void rope_kernel(RopeSide q, RopeSide k, const int32_t* __restrict__ positions,
                                                        int64_t pos_batch, const double* __restrict__ freqs,
-                                                       uint32_t items, uint32_t n, uint32_t lanes, int32_t half,
-                                                       float amplitude, float sign) {
+                                                       uint32_t items, uint32_t n, uint32_t lanes, uint32_t hsplit,
+                                                       int32_t half, float amplitude, float sign) {
     constexpr int E = INTER ? 2 * P : P;  // elements of one load
-    const uint32_t item = blockIdx.x * THREADS + threadIdx.x;
+    const uint32_t group = blockIdx.x / hsplit;
+    const uint32_t item = group * THREADS + threadIdx.x;
     if (item >= items) return;
     const uint32_t row = item / lanes, l = item - row * lanes;  // row: token of the batch
     const uint32_t b = row / n, t = row - b * n;
@@ -268,37 +282,42 @@ __global__ __launch_bounds__(THREADS) void rope_kernel(RopeSide q, RopeSide k, c
     } else {
         lo = 2 * half + (int32_t)(l - half / P) * E;
     }
-    for (int32_t h = blockIdx.y; h < q.heads + k.heads; h += gridDim.y) {
+    // HB heads: their loads go out together
+    const int32_t heads = q.heads + k.heads;
+    const int32_t h0 = (int32_t)(blockIdx.x - group * hsplit) * HB;
+    float v[HB][2 * P];
+    TO* dst[HB];
+#pragma unroll
+    for (int j = 0; j < HB; ++j) {
+        const int32_t h = min(h0 + j, heads - 1);
         const bool isk = h >= q.heads;
-        const RopeSide& x = isk ? k : q;
         const int32_t g = isk ? h - q.heads : h;
-        const TI* src = (const TI*)x.in + b * x.ib + g * x.ih + t * x.it;
-        TO* dst = (TO*)x.out + b * x.ob + g * x.oh + t * x.ot;
-        if (!turn) {
-            float v[E];
-            load_n<TI, E>(src + lo, v);
-            store_n<TO, E>(dst + lo, v);
-        } else if constexpr (INTER) {
-            float v[E], y[E];
-            load_n<TI, E>(src + lo, v);
+        const TI* src = isk ? (const TI*)k.in + b * k.ib + g * k.ih + t * k.it
+                            : (const TI*)q.in + b * q.ib + g * q.ih + t * q.it;
+        dst[j] = isk ? (TO*)k.out + b * k.ob + g * k.oh + t * k.ot : (TO*)q.out + b * q.ob + g * q.oh + t * q.ot;
+        load_n<TI, E>(src + lo, v[j]);
+        if constexpr (!INTER)
+            if (turn) load_n<TI, P>(src + hi, v[j] + P);
+    }
+#pragma unroll
+    for (int j = 0; j < HB; ++j) {
+        if (h0 + j >= heads) break;
+        float y[2 * P];
+        if (turn) {
 #pragma unroll
             for (int i = 0; i < P; ++i) {
-                y[2 * i] = v[2 * i] * c[i] - v[2 * i + 1] * s[i];
-                y[2 * i + 1] = v[2 * i + 1] * c[i] + v[2 * i] * s[i];
+                constexpr int step = INTER ? 2 : 1, far = INTER ? 1 : P;
+                const float x0 = v[j][step * i], x1 = v[j][step * i + far];
+                y[step * i] = x0 * c[i] - x1 * s[i];
+                y[step * i + far] = x1 * c[i] + x0 * s[i];
             }
-            store_n<TO, E>(dst + lo, y);
         } else {
-            float a[P], d[P], ya[P], yd[P];
-            load_n<TI, P>(src + lo, a);
-            load_n<TI, P>(src + hi, d);
 #pragma unroll
-            for (int i = 0; i < P; ++i) {
-                ya[i] = a[i] * c[i] - d[i] * s[i];
-                yd[i] = d[i] * c[i] + a[i] * s[i];
-            }
-            store_n<TO, P>(dst + lo, ya);
-            store_n<TO, P>(dst + hi, yd);
+            for (int i = 0; i < E; ++i) y[i] = v[j][i];
         }
+        store_n<TO, E>(dst[j] + lo, y);
+        if constexpr (!INTER)
+            if (turn) store_n<TO, P>(dst[j] + hi, y + P);
     }
 }
 
@@ -353,8 +372,8 @@ constexpr uint32_t TINY_BITS = 0x0D80;  // bf16 bits of 2^-100
 // How a block of largest magnitude `bits` (bf16, without sign) is coded.
 struct Coding {
     float scale;  // what a code stands for
-    int32_t e;    // the power of two to divide by first
-    float a;      // int8: the largest magnitude after that, in [1, 2)
+    float mul;    // what a value is multiplied by first: e4m3 1 / scale; int8 127 / 2^e, 2^e <= a
+    float a;      // int8: the largest magnitude over 2^e, in [1, 2)
     float inv;    // int8: about 1 / a
     bool zero;
 };
@@ -368,11 +387,12 @@ __device__ __forceinline__ Coding coding(uint32_t bits) {
     q.a = __uint_as_float(((bits & 0x7f) << 16) | 0x3f800000u);
     q.inv = __builtin_amdgcn_rcpf(q.a);
     if constexpr (F::INT8) {
-        q.e = ex;
+        q.mul = ldexpf(127.f, -ex);
         q.scale = amax / 127.f;
     } else {
-        q.e = q.a <= 1.75f ? ex - 8 : ex - 7;  // 448 = 1.75 * 2^8
-        q.scale = __uint_as_float((uint32_t)(q.e + 127) << 23);
+        const int32_t e = q.a <= 1.75f ? ex - 8 : ex - 7;  // 448 = 1.75 * 2^8
+        q.mul = __uint_as_float((uint32_t)(127 - e) << 23);
+        q.scale = __uint_as_float((uint32_t)(127 + e) << 23);
     }
     if (q.zero) q.scale = 1.f;
     if (bits >= 0x7f80) {
@@ -382,25 +402,34 @@ __device__ __forceinline__ Coding coding(uint32_t bits) {
     return q;
 }
 
-// 127 x / a rounded to even, exactly: the product is exact (15 bits), and so is what
-// it leaves of a multiple of a, which corrects the approximate quotient at ties.
-__device__ __forceinline__ int32_t code_int8(float x, const Coding& q) {
-    const float t = 127.f * ldexpf(x, -q.e);
-    float r = rintf(t * q.inv);
-    const float d = fmaf(-r, q.a, t), over = 2.f * fabsf(d) - q.a;
-    if (over > 0.f || (over == 0.f && ((int32_t)r & 1))) r += d > 0.f ? 1.f : -1.f;
-    return (int32_t)r;
-}
-
-// Four values, one byte each in order.
+// Four values, one byte each in order.  int8: 127 x / a rounded to even, exactly.  The
+// product t is exact (15 bits), 1.5 * 2^23 added in the same fma rounds the approximate
+// quotient to a whole number, with its two's complement in the low byte; what t leaves
+// of that multiple of a is exact, too, and tells where the rounding was a tie or off.
 template <class F>
 __device__ __forceinline__ uint32_t code4(float x0, float x1, float x2, float x3, const Coding& q) {
     if constexpr (F::INT8) {
-        return (uint32_t)(code_int8(x0, q) & 255) | (uint32_t)(code_int8(x1, q) & 255) << 8 |
-               (uint32_t)(code_int8(x2, q) & 255) << 16 | (uint32_t)(code_int8(x3, q) & 255) << 24;
+        constexpr float WHOLE = 12582912.f;
+        const float x[4] = {x0, x1, x2, x3};
+        float m[4], d[4], over[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float t = x[i] * q.mul;
+            m[i] = fmaf(t, q.inv, WHOLE);
+            d[i] = fmaf(-(m[i] - WHOLE), q.a, t);
+            over[i] = fmaf(2.f, fabsf(d[i]), -q.a);
+        }
+        if (fmaxf(fmaxf(over[0], over[1]), fmaxf(over[2], over[3])) >= 0.f) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (over[i] > 0.f || (over[i] == 0.f && (__float_as_uint(m[i]) & 1))) m[i] += d[i] > 0.f ? 1.f : -1.f;
+        }
+        const uint32_t lo = __builtin_amdgcn_perm(__float_as_uint(m[1]), __float_as_uint(m[0]), 0x0c0c0400u);
+        return __builtin_amdgcn_perm(__builtin_amdgcn_perm(__float_as_uint(m[3]), __float_as_uint(m[2]), 0x04000c0cu), lo,
+                                     0x07060100u);
     } else {
-        int w = __builtin_amdgcn_cvt_pk_fp8_f32(ldexpf(x0, -q.e), ldexpf(x1, -q.e), 0, false);
-        return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(ldexpf(x2, -q.e), ldexpf(x3, -q.e), w, true);
+        const int w = __builtin_amdgcn_cvt_pk_fp8_f32(x0 * q.mul, x1 * q.mul, 0, false);
+        return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x2 * q.mul, x3 * q.mul, w, true);
     }
 }
 
@@ -409,6 +438,7 @@ __device__ __forceinline__ float bf16_at(const u32x4& w, int k) {  // element k 
 }
 
 // max over the workgroup of x (waves leave theirs in part)
+template <int NT>
 __device__ __forceinline__ uint32_t group_max(uint32_t x, uint32_t* part) {
 #pragma unroll
     for (int m = 32; m > 0; m >>= 1) x = max(x, (uint32_t)__shfl_xor((int)x, m));
@@ -416,12 +446,17 @@ __device__ __forceinline__ uint32_t group_max(uint32_t x, uint32_t* part) {
     __syncthreads();
     uint32_t r = 0;
 #pragma unroll
-    for (int w = 0; w < THREADS / 64; ++w) r = max(r, part[w]);
+    for (int w = 0; w < NT / 64; ++w) r = max(r, part[w]);
     return r;
 }
 
+template <int D, int PW>
+constexpr int APPEND_ITEMS = (D / 8) * (PW / 4);  // 8 dims of four keys each
+template <int D, int PW>
+constexpr int APPEND_THREADS = APPEND_ITEMS<D, PW> < THREADS ? APPEND_ITEMS<D, PW> : THREADS;
+
 template <class F, int D, int PW>
-__global__ __launch_bounds__(THREADS) void kv_append_q8_kernel(
+__global__ __launch_bounds__((APPEND_THREADS<D, PW>)) void kv_append_q8_kernel(
     const __bf16* __restrict__ k, const __bf16* __restrict__ v, int64_t kt, int64_t kh, int64_t vt, int64_t vh,
     int64_t tokens, int32_t batch, const int32_t* __restrict__ lens_before, const int32_t* __restrict__ lens_after,
     const int32_t* __restrict__ token_start, const int32_t* __restrict__ block_start,
@@ -429,121 +464,120 @@ __global__ __launch_bounds__(THREADS) void kv_append_q8_kernel(
     uint8_t* __restrict__ v_pages, float* __restrict__ k_scale, float* __restrict__ v_scale, __bf16* k_tail,
     __bf16* v_tail, int32_t heads) {
     constexpr int CH = D / 8;                // 8-dim chunks of a row
-    constexpr int ITEMS = CH * (PW / 4);     // a chunk of four keys each
-    constexpr int NI = (ITEMS + THREADS - 1) / THREADS;
+    constexpr int NT = APPEND_THREADS<D, PW>;
+    constexpr int NI = APPEND_ITEMS<D, PW> / NT;
     constexpr int VST = PW + 4;              // bytes per dim in LDS (spread over the banks)
     __shared__ uint32_t vt_lds[D * VST / 4];
-    __shared__ uint32_t part_k[THREADS / 64], part_v[THREADS / 64];
+    __shared__ uint32_t part_k[NT / 64], part_v[NT / 64];
     const int tid = threadIdx.x;
-    const int32_t u = blockIdx.x;
-    const int32_t h = blockIdx.y;
+    const int32_t u = blockIdx.x / heads, h = blockIdx.x - u * heads;
 
-    // the sequence of unit u: 64 entries of block_start at a time
-    int32_t lo = 0, hi = batch;  // block_start[lo] <= u < block_start[hi]
-    if (u >= block_start[batch]) return;
-    while (hi - lo > 1) {
-        const int32_t step = (hi - lo + 63) / 64;
-        const int32_t at = lo + (tid & 63) * step;
-        const bool in = at < hi && block_start[at] <= u;
-        const int32_t c = __popcll(__ballot(in)) - 1;
-        if (c < 0) return;  // not a table of page_step
+    // the sequence of unit u, block_start[b] <= u < block_start[b + 1]: 256 entries at a time
+    const int32_t units = block_start[batch];
+    int32_t lo = 0, hi = batch;
+    for (;;) {
+        const int32_t step = (hi - lo + 255) / 256;
+        int32_t c = -1;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int32_t at = lo + ((tid & 63) + 64 * j) * step;
+            c += __popcll(__ballot(block_start[min(at, batch)] <= u && at < hi));
+        }
+        if (u >= units || c < 0) return;  // c < 0: not a table of page_step
         lo += c * step;
+        if (step == 1) break;
         hi = min(hi, lo + step);
     }
     const int32_t b = lo;
     const int32_t i = u - block_start[b];
-    if (i < 0) return;
     const int64_t start = max(lens_before[b], 0), end = max((int64_t)lens_after[b], start);
+    const int64_t row0 = (int64_t)token_start[b] - start;  // row of position p: row0 + p
+    if (i < 0) return;
     if (end == start) return;
     const int64_t first = start / PW, last = (end - 1) / PW;
     const int64_t block = first + i;
     if (block > last) return;
-    const int64_t row0 = (int64_t)token_start[b] - start;  // row of position p: row0 + p
     const int64_t tail_at = ((int64_t)b * heads + h) * PW * D;
     const int32_t page = block < max_pages ? page_table[(int64_t)b * max_pages + block] : -1;
 
-    if ((block + 1) * PW <= end && page >= 0 && page < num_pages) {
-        u32x4 kw[NI][4], vw[NI][4];
+    if ((block + 1) * PW <= end) {
+        // K: a lane's rows are NT / CH apart, so that a wave's codes go out side by side;
+        // V: four rows next to each other
+        u32x4 kw[4 * NI], vw[NI][4];
         uint32_t km = 0, vm = 0;
+        const int c = tid % CH;
+        auto fetch = [&](const __bf16* x, int64_t xt, int64_t xh, const __bf16* tail, int key) {
+            const int64_t pos = block * PW + key, row = row0 + pos;
+            if (pos < start) return *reinterpret_cast<const u32x4*>(tail + tail_at + key * D + 8 * c);
+            if (row >= 0 && row < tokens) return *reinterpret_cast<const u32x4*>(x + row * xt + h * xh + 8 * c);
+            return u32x4{0u, 0u, 0u, 0u};
+        };
+        auto widest = [](uint32_t m, const u32x4& w) {
 #pragma unroll
-        for (int n = 0; n < NI; ++n) {
-            const int it = tid + n * THREADS, c = it % CH, g = it / CH;
+            for (int e = 0; e < 4; ++e) m = max(m, max(w[e] & 0x7fffu, w[e] >> 16 & 0x7fffu));
+            return m;
+        };
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int key = 4 * g + r;
-                const int64_t pos = block * PW + key, row = row0 + pos;
-                u32x4 a = {0u, 0u, 0u, 0u}, w = {0u, 0u, 0u, 0u};
-                if (it < ITEMS) {
-                    if (pos < start) {
-                        a = *reinterpret_cast<const u32x4*>(k_tail + tail_at + key * D + 8 * c);
-                        w = *reinterpret_cast<const u32x4*>(v_tail + tail_at + key * D + 8 * c);
-                    } else if (row >= 0 && row < tokens) {
-                        a = *reinterpret_cast<const u32x4*>(k + row * kt + h * kh + 8 * c);
-                        w = *reinterpret_cast<const u32x4*>(v + row * vt + h * vh + 8 * c);
-                    }
-                }
-                kw[n][r] = a;
-                vw[n][r] = w;
+        for (int n = 0; n < 4 * NI; ++n) kw[n] = fetch(k, kt, kh, k_tail, tid / CH + n * (NT / CH));
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    km = max(km, max(a[e] & 0x7fffu, a[e] >> 16 & 0x7fffu));
-                    vm = max(vm, max(w[e] & 0x7fffu, w[e] >> 16 & 0x7fffu));
-                }
-            }
+        for (int n = 0; n < NI; ++n)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) vw[n][r] = fetch(v, vt, vh, v_tail, 4 * (tid / CH + n * (NT / CH)) + r);
+#pragma unroll
+        for (int n = 0; n < 4 * NI; ++n) {
+            km = widest(km, kw[n]);
+            vm = widest(vm, vw[n / 4][n % 4]);
         }
-        km = group_max(km, part_k);
-        vm = group_max(vm, part_v);
+        km = group_max<NT>(km, part_k);
+        vm = group_max<NT>(vm, part_v);
         const Coding kq = coding<F>(km), vq = coding<F>(vm);
-        const int64_t slice = (int64_t)page * heads + h;
-        if (tid == 0) {
+        const bool kept = page >= 0 && page < num_pages;
+        const int64_t slice = (int64_t)(kept ? page : 0) * heads + h;
+        if (kept && tid == 0) {
             k_scale[slice] = kq.scale;
             v_scale[slice] = vq.scale;
         }
         uint8_t* kp = k_pages + slice * (PW * D);
         uint8_t* vp = v_pages + slice * (PW * D);
 #pragma unroll
-        for (int n = 0; n < NI; ++n) {
-            const int it = tid + n * THREADS, c = it % CH, g = it / CH;
-            if (it < ITEMS) {
+        for (int n = 0; n < 4 * NI; ++n) {
+            u32x2 o = {0u, 0u};
+            if (!kq.zero) {
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    u32x2 o = {0u, 0u};
-                    if (!kq.zero) {
-#pragma unroll
-                        for (int e = 0; e < 2; ++e)
-                            o[e] = code4<F>(bf16_at(kw[n][r], 4 * e), bf16_at(kw[n][r], 4 * e + 1),
-                                            bf16_at(kw[n][r], 4 * e + 2), bf16_at(kw[n][r], 4 * e + 3), kq);
-                    }
-                    *reinterpret_cast<u32x2*>(kp + (4 * g + r) * D + 8 * c) = o;
-                }
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    vt_lds[(8 * c + e) * (VST / 4) + g] =
-                        vq.zero ? 0u
-                                : code4<F>(bf16_at(vw[n][0], e), bf16_at(vw[n][1], e), bf16_at(vw[n][2], e),
-                                           bf16_at(vw[n][3], e), vq);
+                for (int e = 0; e < 2; ++e)
+                    o[e] = code4<F>(bf16_at(kw[n], 4 * e), bf16_at(kw[n], 4 * e + 1), bf16_at(kw[n], 4 * e + 2),
+                                    bf16_at(kw[n], 4 * e + 3), kq);
             }
+            if (kept) *reinterpret_cast<u32x2*>(kp + (tid / CH + n * (NT / CH)) * D + 8 * c) = o;
         }
+#pragma unroll
+        for (int n = 0; n < NI; ++n)
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                vt_lds[(8 * c + e) * (VST / 4) + tid / CH + n * (NT / CH)] =
+                    vq.zero ? 0u
+                            : code4<F>(bf16_at(vw[n][0], e), bf16_at(vw[n][1], e), bf16_at(vw[n][2], e),
+                                       bf16_at(vw[n][3], e), vq);
         __syncthreads();
-        for (int x = tid; x < D * PW / 16; x += THREADS) {
+        for (int x = tid; x < D * PW / 16; x += NT) {
             const int d = x / (PW / 16), q = x % (PW / 16);
             u32x4 o;
 #pragma unroll
             for (int e = 0; e < 4; ++e) o[e] = vt_lds[d * (VST / 4) + 4 * q + e];
-            *reinterpret_cast<u32x4*>(vp + d * PW + 16 * q) = o;
+            if (kept) *reinterpret_cast<u32x4*>(vp + d * PW + 16 * q) = o;
         }
     }
 
     if (i != 0) return;
     __syncthreads();  // the tail has been read
     const int64_t from = max(start, last * PW);
-    for (int x = tid; x < (int)(end - from) * CH; x += THREADS) {
+    for (int x = tid; x < (int)(end - from) * CH; x += NT) {
         const int64_t pos = from + x / CH, row = row0 + pos;
-        const int c = x % CH;
+        const int cx = x % CH;
         if (row < 0 || row >= tokens) continue;
-        const int64_t dst = tail_at + (pos - last * PW) * D + 8 * c;
-        *reinterpret_cast<u32x4*>(k_tail + dst) = *reinterpret_cast<const u32x4*>(k + row * kt + h * kh + 8 * c);
-        *reinterpret_cast<u32x4*>(v_tail + dst) = *reinterpret_cast<const u32x4*>(v + row * vt + h * vh + 8 * c);
+        const int64_t dst = tail_at + (pos - last * PW) * D + 8 * cx;
+        *reinterpret_cast<u32x4*>(k_tail + dst) = *reinterpret_cast<const u32x4*>(k + row * kt + h * kh + 8 * cx);
+        *reinterpret_cast<u32x4*>(v_tail + dst) = *reinterpret_cast<const u32x4*>(v + row * vt + h * vh + 8 * cx);
     }
 }
 
@@ -558,18 +592,30 @@ hipError_t launch_rope(const RopeSide& q, const RopeSide& k, const int32_t* posi
     const int32_t lanes = rot / 2 / P + (d - rot) / E;
     const int64_t groups = (rows * lanes + THREADS - 1) / THREADS;
     const int32_t heads = q.heads + k.heads;
-    // few rows: a head per lane; many: a lane walks over several heads
-    const int32_t hsplit = groups >= 2048 ? (heads + 7) / 8 : heads;
-    *fits = rows * lanes < (int64_t(1) << 31) && launchable(groups * hsplit) && hsplit < 65536;
+    // Two heads per lane share its cosines and sines; one where that leaves compute units
+    // without a workgroup.  us, one / two / four: 32 rows of 24 heads of 128 3.2 / 3.6 /
+    // 4.1, 4096 14.2 / 12.7 / 11.7, 32768 107 / 84 / 88.
+    const int32_t hb = groups * heads < 256 ? 1 : 2;
+    const int32_t hsplit = (heads + hb - 1) / hb;
+    *fits = rows * lanes < (int64_t(1) << 31) && launchable(groups * hsplit);
     if (!*fits) return hipSuccess;
     auto go = [&](auto kern) {
-        hipLaunchKernelGGL(kern, dim3((unsigned)groups, (unsigned)hsplit), dim3(THREADS), 0, s, q, k, positions,
-                           pos_batch, freqs, (uint32_t)(rows * lanes), (uint32_t)n, (uint32_t)lanes, rot / 2, amplitude,
+        hipLaunchKernelGGL(kern, dim3((unsigned)(groups * hsplit)), dim3(THREADS), 0, s, q, k, positions, pos_batch, freqs,
+                           (uint32_t)(rows * lanes), (uint32_t)n, (uint32_t)lanes, (uint32_t)hsplit, rot / 2, amplitude,
                            sign);
         return hipGetLastError();
     };
-    if (inter) return wide ? go(rope_kernel<TI, TO, true, 8 / sizeof(TI)>) : go(rope_kernel<TI, TO, true, 1>);
-    return wide ? go(rope_kernel<TI, TO, false, 16 / sizeof(TI)>) : go(rope_kernel<TI, TO, false, 1>);
+    auto pick = [&](auto inter_c, auto p_c) {
+        constexpr bool I = decltype(inter_c)::value;
+        constexpr int PP = decltype(p_c)::value;
+        return hb == 1 ? go(rope_kernel<TI, TO, I, PP, 1>) : go(rope_kernel<TI, TO, I, PP, 2>);
+    };
+    using std::integral_constant;
+    if (inter)
+        return wide ? pick(std::true_type{}, integral_constant<int, 8 / sizeof(TI)>{})
+                    : pick(std::true_type{}, integral_constant<int, 1>{});
+    return wide ? pick(std::false_type{}, integral_constant<int, 16 / sizeof(TI)>{})
+                : pick(std::false_type{}, integral_constant<int, 1>{});
 }
 
 template <class F>
@@ -578,14 +624,17 @@ hipError_t launch_append_q8(int64_t units, const __bf16* k, const __bf16* v, int
                             const int32_t* token_start, const int32_t* block_start, const int32_t* page_table,
                             int32_t max_pages, int32_t num_pages, void* kp, void* vp, float* ks, float* vs, void* ktl,
                             void* vtl, int32_t heads, int32_t d, int32_t B, hipStream_t s) {
-    auto go = [&](auto kern) {
-        hipLaunchKernelGGL(kern, dim3((unsigned)units, (unsigned)heads), dim3(THREADS), 0, s, k, v, kt, kh, vt, vh,
+    auto go = [&](auto kern, int threads) {
+        hipLaunchKernelGGL(kern, dim3((unsigned)(units * heads)), dim3(threads), 0, s, k, v, kt, kh, vt, vh,
                            tokens, batch, before, after, token_start, block_start, page_table, max_pages, num_pages,
                            (uint8_t*)kp, (uint8_t*)vp, ks, vs, (__bf16*)ktl, (__bf16*)vtl, heads);
         return hipGetLastError();
     };
-    if (d == 64) return B == 64 ? go(kv_append_q8_kernel<F, 64, 64>) : go(kv_append_q8_kernel<F, 64, 128>);
-    return B == 64 ? go(kv_append_q8_kernel<F, 128, 64>) : go(kv_append_q8_kernel<F, 128, 128>);
+    if (d == 64)
+        return B == 64 ? go(kv_append_q8_kernel<F, 64, 64>, APPEND_THREADS<64, 64>)
+                       : go(kv_append_q8_kernel<F, 64, 128>, APPEND_THREADS<64, 128>);
+    return B == 64 ? go(kv_append_q8_kernel<F, 128, 64>, APPEND_THREADS<128, 64>)
+                   : go(kv_append_q8_kernel<F, 128, 128>, APPEND_THREADS<128, 128>);
 }
 
 }  // namespace
@@ -617,7 +666,7 @@ int bf1_page_step(int32_t batch, const int32_t* seq_lens, const int32_t* new_len
                                : (max_tokens + bf1::ROWS_PER_GROUP - 1) / bf1::ROWS_PER_GROUP;
     hipLaunchKernelGGL(bf1::page_step_kernel, dim3((unsigned)groups), dim3(bf1::THREADS), 0, (hipStream_t)stream, batch,
                        seq_lens, new_lens, page_table, max_pages_per_seq, free_pages, num_free, free_head,
-                       B == 64 ? 6 : 7, max_tokens, seq_lens_out, token_start, block_start, positions, slots,
+                       B == 64 ? 6 : 7, (int32_t)max_tokens, seq_lens_out, token_start, block_start, positions, slots,
                        free_head_out);
     return bf1::status_of(hipGetLastError());
 }
@@ -719,7 +768,7 @@ int bf1_kv_append_q8(const void* K, const void* V, int64_t k_token_stride, int64
         if (!bf1::aligned(p, 4)) return BF1_ERR_INVALID_ARG;
     if (!bf1::strides16(k_token_stride, k_head_stride) || !bf1::strides16(v_token_stride, v_head_stride))
         return BF1_ERR_INVALID_ARG;
-    if (tokens >= (int64_t(1) << 31) || Hkv > 65535) return BF1_ERR_UNSUPPORTED;
+    if (tokens >= (int64_t(1) << 31) || Hkv > 65535 || batch > (1 << 22)) return BF1_ERR_UNSUPPORTED;
     // blocks that `tokens` rows of up to `batch` sequences can touch: one of x rows
     // touches at most 1 + ceil((x - 1) / B)
     const int64_t active = tokens < batch ? tokens : batch, rest = tokens - active;
