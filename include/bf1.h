@@ -355,7 +355,8 @@ int bf1_decode_attn(const void* Q, const void* K_pages, const void* V_pages, con
  * past max_tokens, or no free page is left for its block; the tokens behind it in
  * its sequence have none either, and seq_lens_out counts only those that have one
  * (block_start likewise).  The caller sees it by comparing the lengths; nothing is
- * taken from the free list for it.  Outputs are distinct from inputs:
+ * taken from the free list for it.  An entry below 0 that the table holds for a
+ * block with tokens already gives its new tokens slot -1.  Outputs are distinct from inputs:
  * seq_lens_out == seq_lens or new_lens and free_head_out == free_head are refused.
  * B in {64, 128}, max_tokens < 2^31.
  */
@@ -377,7 +378,7 @@ int bf1_page_step(int32_t batch, const int32_t* seq_lens, const int32_t* new_len
  *               any value, also negative
  *   freqs     : [rot_dim / 2] double, radians per position
  *   Q_out, K_out : out_type: in_type, or bf16 of fp32; may be the inputs themselves
- *               (same type and strides), otherwise do not overlap them
+ *               (same type and strides), otherwise they overlap neither them nor each other
  *   strides   : HOST int64[12], in elements: batch, head, token of Q, Q_out, K, K_out
  * Angles are formed in double precision and the turn in fp32, rounded once.  Even
  * head_dim <= 1024 and rot_dim; sixteen bytes at a time where strides, addresses and
@@ -420,7 +421,8 @@ int bf1_kv_append(const void* K, const void* V, int64_t k_token_stride, int64_t 
  *
  * bf1_kv_append_q8: a step's rows K, V (as bf1_kv_append's, `tokens` of them) into
  * the cache; seq_lens_before, seq_lens (after the step), token_start, block_start and
- * page_table are bf1_page_step's.  Blocks that the step completes are quantised
+ * page_table are bf1_page_step's, and K and V hold the token_start[batch] rows that
+ * they count.  Blocks that the step completes are quantised
  * (their earlier rows come from the tail), then the rows of the block of each
  * sequence's newest token go to its tail; tails of sequences without new tokens, and
  * all other pages, are left as they were.  Rows behind the last sequence are not read.

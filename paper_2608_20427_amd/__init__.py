@@ -567,8 +567,8 @@ def page_step(seq_lens, new_lens, page_table, free_pages, free_head, max_tokens,
     check_buffer(free_pages, "free_pages", free_pages.shape, torch.int32, dev)
     check_buffer(free_head, "free_head", (1,), torch.int32, dev)
     max_tokens = int(max_tokens)
-    if max_tokens < 0:
-        raise ValueError("max_tokens must not be negative")
+    if not 0 <= max_tokens < 2 ** 31:
+        raise ValueError("max_tokens must not be negative, and below 2^31")
     if out is None:
         # one allocation, slots (8 bytes) first; 4 us less than one each
         buf = _empty((3 * max_tokens + 3 * batch + 3,), torch.int32, dev, stream)

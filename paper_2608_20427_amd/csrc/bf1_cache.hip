@@ -6,6 +6,7 @@
 #include <math.h>
 #include <stdint.h>
 
+#include <algorithm>
 #include <type_traits>
 
 #include "../../include/bf1.h"
@@ -688,7 +689,13 @@ int bf1_rope(const void* Q, const void* K, const int32_t* positions, int64_t pos
     const int64_t esize = in_type == BF1_TYPE_BF16 ? 2 : 4, osize = out_type == BF1_TYPE_BF16 ? 2 : 4;
     if (!bf1::aligned(positions, 4) || !bf1::aligned(freqs, 8)) return BF1_ERR_INVALID_ARG;
     for (int i = 0; i < 12; ++i)
-        if (strides[i] < 0 || strides[i] > (int64_t(1) << 40)) return BF1_ERR_INVALID_ARG;
+        if (strides[i] < 0) return BF1_ERR_INVALID_ARG;
+    // every element is within reach of a 64-bit byte offset
+    for (int i = 0; i < 12; i += 3)
+        if ((double)batch * strides[i] + (double)std::max(Hq, Hkv) * strides[i + 1] + (double)n * strides[i + 2] > 1e18)
+            return BF1_ERR_INVALID_ARG;
+    // a side's output is read by no other lane: it is not the other side's input or output
+    if (Hq > 0 && Hkv > 0 && (Q_out == K_out || Q_out == K || K_out == Q)) return BF1_ERR_INVALID_ARG;
     const int64_t vec = 16 / esize;  // elements of a 16-byte load
     // 16 bytes at a time where the halves, the rest and every row allow it
     bool wide = rot_dim % (2 * vec) == 0 && (head_dim - rot_dim) % vec == 0;

@@ -534,6 +534,7 @@ int check_sizes(int32_t batch, int32_t Hq, int32_t Hkv, int32_t d, int32_t B, in
     const int32_t G = Hq / Hkv;
     if ((d != 64 && d != 128) || (B != 64 && B != 128) || (G != 1 && G != 2 && G != 4 && G != 8))
         return BF1_ERR_UNSUPPORTED;
+    if (Hkv > 65535) return BF1_ERR_UNSUPPORTED;
     if ((int64_t)batch * Hkv > (int64_t(1) << 22)) return BF1_ERR_INVALID_ARG;
     return BF1_OK;
 }

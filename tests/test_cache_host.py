@@ -141,7 +141,7 @@ def test_page_step_refusals(lib):
 
 def test_rope_refusals(lib):
     st = (ctypes.c_int64 * 12)(*[4096, 128, 256] * 4)
-    ok = [FAKE, FAKE, FAKE, 0, FAKE, FAKE + 4096, FAKE + 4096, 2, 10, 4, 2, 128, 128, 0, 0, 0, 1.0, 0, st, None]
+    ok = [FAKE, FAKE + 8192, FAKE, 0, FAKE, FAKE + 4096, FAKE + 12288, 2, 10, 4, 2, 128, 128, 0, 0, 0, 1.0, 0, st, None]
     for at, want in [({7: -1}, INVALID), ({8: -1}, INVALID), ({9: -1}, INVALID), ({18: None}, INVALID),
                      ({13: 2}, INVALID), ({14: -1}, INVALID), ({15: 2}, INVALID), ({17: 3}, INVALID),
                      ({11: 127}, UNSUPPORTED), ({11: 2048, 12: 64}, UNSUPPORTED), ({12: 0}, UNSUPPORTED),
@@ -151,7 +151,11 @@ def test_rope_refusals(lib):
                      ({18: (ctypes.c_int64 * 12)(-1)}, INVALID),
                      # in place with other strides, or another type
                      ({5: FAKE, 18: (ctypes.c_int64 * 12)(*[4096, 128, 256, 4096, 256, 128] * 2)}, INVALID),
-                     ({5: FAKE, 13: 1, 14: 0}, INVALID)]:
+                     ({5: FAKE, 13: 1, 14: 0}, INVALID),
+                     # one side's output over the other side
+                     ({1: FAKE + 8192, 6: FAKE + 4096}, INVALID), ({1: FAKE + 4096, 6: FAKE + 8192}, INVALID),
+                     ({1: FAKE + 8192, 6: FAKE}, INVALID),
+                     ({18: (ctypes.c_int64 * 12)(*[1 << 60] * 12)}, INVALID)]:
         assert lib.bf1_rope(*_with(ok, at)) == want, at
     for at in ({7: 0}, {8: 0}, {9: 0, 10: 0}):  # nothing to do
         assert lib.bf1_rope(*_with(ok, at)) == bf1.BF1_OK
@@ -181,7 +185,7 @@ def test_decode_q8_refusals(lib):
     ok = [FAKE] * 8 + [7, FAKE, 19, FAKE, FAKE, 3, 16, 8, 128, 64, 0, FAKE, 1 << 40, None]
     for at, want in [({8: 0}, INVALID), ({10: 2}, INVALID), ({13: -1}, INVALID), ({14: 0}, INVALID), ({14: 17}, INVALID),
                      ({14: 24}, UNSUPPORTED), ({14: 128}, UNSUPPORTED), ({16: 96}, UNSUPPORTED), ({17: 32}, UNSUPPORTED),
-                     ({18: 2}, INVALID), ({13: 1 << 20}, INVALID), ({0: FAKE + 8}, INVALID), ({2: None}, INVALID),
+                     ({18: 2}, INVALID), ({13: 1 << 20}, INVALID), ({13: 1, 14: 65536, 15: 65536}, UNSUPPORTED), ({0: FAKE + 8}, INVALID), ({2: None}, INVALID),
                      ({3: FAKE + 2}, INVALID), ({5: None}, INVALID), ({7: None}, INVALID), ({9: None}, INVALID),
                      ({11: None}, INVALID), ({12: FAKE + 1}, INVALID), ({20: 0}, SMALL), ({19: FAKE + 4}, INVALID)]:
         assert lib.bf1_decode_attn_q8(*_with(ok, at)) == want, at
