@@ -505,18 +505,28 @@ hipError_t launch_d(const Args& a, int32_t G, int32_t B, hipStream_t st) {
     }
 }
 
-// Splits of a (sequence, kv-head) whose plan row holds `units` of 64 keys: one
-// workgroup per compute unit, and no split without a round of units for each of its
-// waves.  A round takes some 1.3 us, the merge 2 to 3 and a launch more: a list is cut
-// where that saves three rounds.  us, uncut / cut: 12 units, 1 sequence of 8 kv-heads
-// 8.8 / 8.4; 33 units 18.1 / 9.3; 128 units, 4 sequences 57 / 17.  Twice the workgroups:
-// 128 units, 4 sequences 17.5, 16 sequences 41.6 for 40.6; 1024 units, 1 sequence 31 for 28.
-// More than 32 splits cost the merge more than they save: 256 units, 2 kv-heads 16 for 14.
-constexpr int64_t WANTED_GROUPS = 256, MOST_SPLITS = 32;
+// Splits of a (sequence, kv-head) whose plan row holds `units` of 64 keys.
+//
+// Workgroups go to compute units in turns, and a unit of two while others have one ends
+// last: a long list (four rounds of a unit per wave and split, or more) gets the fewest
+// splits that leave less than one place in twenty empty.  us with one split, with 256
+// workgroups or the next below, and so chosen: 320 rows of 128 units 123 / 126 / 95; 160
+// rows 63 / 67 / 51; 192 rows 69 / 69 / 56; 96 rows of 256 units 116 / 71 / 55; 48 rows
+// of 512 units 217 / 63 / 57; 64 rows of 512 (heads of 64) 128 / 41 / 41.
+//
+// Shorter lists: at most 256 workgroups, and a list is cut only where that saves three
+// rounds.  A round takes some 1.5 us, the merge 2 to 3 and a launch more.  us, uncut /
+// cut: 12 units, 8 rows 8.7 / 8.4, 160 rows 12.1 / 13.1; 33 units, 8 rows 18.1 / 9.2.
+//
+// More than 32 splits cost the merge more than they save: 256 units, 2 rows 16 for 14.
+constexpr int64_t PLACES = 256, MOST_SPLITS = 32, MANY_ROWS = 2048;
 int32_t splits(int64_t rows, int64_t plan_stride, int32_t B) {
     const int64_t units = (plan_stride - 2) * (B / UNIT);
     const int64_t rounds = (units + WAVES - 1) / WAVES;
-    int64_t n = rows > 0 ? WANTED_GROUPS / rows : 1;
+    if (rows < 1 || rows > MANY_ROWS) return 1;
+    for (int64_t n = rows < PLACES ? PLACES / rows : 1; n <= MOST_SPLITS && 4 * n <= rounds; ++n)
+        if (20 * rows * n >= 19 * ((rows * n + PLACES - 1) / PLACES * PLACES)) return (int32_t)n;
+    int64_t n = PLACES / rows;
     if (n > rounds) n = rounds;
     if (n > MOST_SPLITS) n = MOST_SPLITS;
     return n < 2 || rounds - (rounds + n - 1) / n < 3 ? 1 : (int32_t)n;
