@@ -420,24 +420,33 @@ __global__ __launch_bounds__(THREADS, 3) void decode_q8_kernel(
 }
 
 // Sum of the splits' records of one q-head, in split order.  Records: every split's
-// sums [G][D], then every split's [G][max, sum].  Lane q holds the maximum and the sum
-// of split q, so that one round trip brings all weights; the sums follow eight loads
-// at a time.
+// sums [G][D], then every split's [G][max, sum].  Everything is asked for at once, before
+// what says how many of the splits had work: lane q holds the maximum and the sum of
+// split q, a lane's y the splits' sums of its dim.
+constexpr int MOST_SPLITS = 32;
 template <int D, int G, int PW>
 __global__ __launch_bounds__(D) void merge_q8_kernel(const int32_t* __restrict__ seq_lens,
                                                      const int32_t* __restrict__ plan, int32_t stride, int32_t cap,
                                                      __bf16* __restrict__ O, float* __restrict__ LSE,
-                                                     const float* __restrict__ ws, int32_t Hkv,
-                                                     int32_t nsplit) {
+                                                     const float* __restrict__ ws, int32_t Hkv, int32_t nsplit) {
+    constexpr int U = 8;
     const int b = blockIdx.x, h = blockIdx.y, e = blockIdx.z;
     const int64_t bh = (int64_t)b * Hkv + h;
     const int d = threadIdx.x, lane = d & 63;
-    View sv;
-    const bool ok = view<PW>(seq_lens, plan + (int64_t)b * stride, cap, b, &sv);
-    const int nsb = splits_used(sv.units, nsplit);
     const float* ml = ws + ((int64_t)gridDim.x * Hkv * nsplit * D + (bh * nsplit + min(lane, nsplit - 1)) * 2) * G + e * 2;
     float m = ml[0];
     const float l = ml[1];
+    const float* src = ws + (bh * nsplit * G + e) * D + d;
+    float y[MOST_SPLITS];
+#pragma unroll
+    for (int c = 0; c < MOST_SPLITS; c += U)
+        if (c < nsplit) {
+#pragma unroll
+            for (int i = c; i < c + U; ++i) y[i] = src[(int64_t)min(i, nsplit - 1) * (G * D)];
+        }
+    View sv;
+    const bool ok = view<PW>(seq_lens, plan + (int64_t)b * stride, cap, b, &sv);
+    const int nsb = splits_used(sv.units, nsplit);
     if (!ok || nsb <= 1) return;  // NaN or the result stands there already
     if (lane >= nsb) m = -INFINITY;
     float M = m;
@@ -447,17 +456,14 @@ __global__ __launch_bounds__(D) void merge_q8_kernel(const int32_t* __restrict__
     float L = lane < nsb ? l * w : 0.f;
 #pragma unroll
     for (int x = 32; x > 0; x >>= 1) L += __shfl_xor(L, x);
-    const float* src = ws + (bh * nsplit * G + e) * D + d;
     float o = 0.f;
-    constexpr int U = 8;
-    for (int q0 = 0; q0 < nsb; q0 += U) {
-        float y[U];
 #pragma unroll
-        for (int i = 0; i < U; ++i) y[i] = src[(int64_t)min(q0 + i, nsb - 1) * (G * D)];
+    for (int c = 0; c < MOST_SPLITS; c += U)
+        if (c < nsb) {
 #pragma unroll
-        for (int i = 0; i < U; ++i)
-            if (q0 + i < nsb) o = fmaf(y[i], __shfl(w, q0 + i), o);
-    }
+            for (int i = c; i < c + U; ++i)
+                if (i < nsb) o = fmaf(y[i], __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), i)), o);
+        }
     const int64_t at = bh * G + e;
     O[at * D + d] = (__bf16)(o / L);
     if (d == 0 && LSE != nullptr) LSE[at] = (M + log2f(L)) * LN2;
@@ -519,7 +525,7 @@ hipError_t launch_d(const Args& a, int32_t G, int32_t B, hipStream_t st) {
 // cut: 12 units, 8 rows 8.7 / 8.4, 160 rows 12.1 / 13.1; 33 units, 8 rows 18.1 / 9.2.
 //
 // More than 32 splits cost the merge more than they save: 256 units, 2 rows 16 for 14.
-constexpr int64_t PLACES = 256, MOST_SPLITS = 32, MANY_ROWS = 2048;
+constexpr int64_t PLACES = 256, MANY_ROWS = 2048;
 int32_t splits(int64_t rows, int64_t plan_stride, int32_t B) {
     const int64_t units = (plan_stride - 2) * (B / UNIT);
     const int64_t rounds = (units + WAVES - 1) / WAVES;
