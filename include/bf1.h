@@ -344,7 +344,7 @@ int bf1_decode_attn(const void* Q, const void* K_pages, const void* V_pages, con
  *   free_pages         : [num_free] int32, taken in order from entry *free_head
  *   seq_lens_out       : [batch] int32, the lengths after the step
  *   token_start        : [batch + 1] int32, first row of each sequence (the sum of
- *                        new_lens before it)
+ *                        new_lens before it, 2^31 - 1 at most)
  *   block_start        : [batch + 1] int32, the number of blocks that sequences
  *                        before it write to in this step
  *   positions, slots   : [max_tokens] int32 / int64; of row i: its token's position,

@@ -104,9 +104,10 @@ __global__ __launch_bounds__(THREADS, 3) void decode_q8_kernel(
     const int32_t* __restrict__ plan, int32_t stride, int32_t cap, __bf16* __restrict__ O, float* __restrict__ LSE,
     float* __restrict__ ws, int32_t Hkv, int32_t nsplit, float c_log2) {
     constexpr int UPP = PW / UNIT;     // units of a page
-    // A page of 64 is read once, by one wave: past the caches it comes 5% (short lists) to
-    // 15% (long ones) sooner.  Two waves share the lines of the V rows of a page of 128:
-    // there it would cost 10 to 15%.
+    // A page of 64 is read once, by one wave: past the caches, which brings much of it
+    // sooner (us, past / through: 128 sequences of 4K 29.8 / 30.7, one dense list of 64K 28.9
+    // / 33.6; 32 sequences of 64K 12.9 / 12.4).  Two waves share the lines of the V rows of a
+    // page of 128, which go through (12 dense lists of 32K 71 / 78).
     constexpr int CPOL = PW == UNIT ? CPOL_NT : 0;
     constexpr int KL = D / 64;         // 16-byte loads of a key row per lane
     constexpr int DT = D / 16;         // 16-wide tiles of O

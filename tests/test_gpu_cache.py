@@ -96,6 +96,14 @@ def test_page_step_shortages():
     check_page_step(np.zeros(0), np.zeros(0), np.zeros((0, 4)), np.arange(4), 1, 5, B)
 
 
+def test_page_step_sums_past_32_bits():
+    big = 2 ** 31 - 1
+    s = bf1.page_step(i32([0, 0, 5, 0]), i32([big, big, big, 7]), i32(np.full((4, 2), -1)), i32(range(9)), i32([0]), 200)
+    assert s.token_start.tolist() == [0, big, big, big, big]  # 2^31 - 1 at most
+    assert s.seq_lens.tolist() == [128, 0, 5, 0] and s.block_start.tolist() == [0, 2, 2, 2, 2] and int(s.free_head) == 2
+    assert s.positions.tolist() == list(range(128)) + [-1] * 72
+
+
 def test_page_step_into_buffers_and_refusals():
     old, new, free, head = i32([3, 60]), i32([2, 9]), i32(range(9)), i32([0])
     a = bf1.page_step(old, new, i32(np.full((2, 4), 1)), free, head, 20)
@@ -541,6 +549,47 @@ def test_decode_q8_long_and_many(fmt, lens, Hq, Hkv, d, B, L, dense):
                 bo, bl = decode_bars(f64(q)[b, x], k, ref)
                 assert (np.abs(f64(o)[b, x] - ref[0]) <= bo).all() and abs(f64(lse)[b, x] - ref[1]) <= bl
     assert torch.isfinite(o).all() and torch.isfinite(lse).all()
+
+
+def test_decode_q8_many_rows_of_long_lists():
+    """320 (sequence, kv-head) rows, cut so that the compute units fill evenly."""
+    lens = [7000 + 13 * i for i in range(40)]
+    q, cache, table = decode_case("e4m3", lens, 8, 8, 64, 64, 2, True, 8)
+    assert bf1.decode_q8_workspace_size(40, 8, 8, 64, 64, 122) > 0
+    (o, lse), _ = run_decode(q, cache, table, lens, 64, 2, True)
+    for b, h in ((0, 0), (17, 3), (39, 7)):
+        k, v = keys_of(cache, table, b, h, lens[b], 64, 2, True)
+        ref = co.decode(f64(q)[b, h], k, v)
+        bo, bl = decode_bars(f64(q)[b, h], k, ref)
+        assert (np.abs(f64(o)[b, h] - ref[0]) <= bo).all() and abs(f64(lse)[b, h] - ref[1]) <= bl
+    assert torch.isfinite(o).all() and torch.isfinite(lse).all()
+
+
+def test_decode_q8_into_buffers():
+    """The caller's outputs and a workspace that holds anything: the same bits; without
+    an LSE the outputs alone."""
+    lens = [5000, 900]
+    q, cache, table = decode_case("e4m3", lens, 4, 2, 128, 128, 2, True, 9)
+    (a, la), plan = run_decode(q, cache, table, lens, 128, 2, True)
+    need = bf1.decode_q8_workspace_size(2, 4, 2, 128, 128, plan.shape[1])
+    ws = torch.full((need + 64,), 255, dtype=torch.uint8, device="cuda")
+    out, lse = torch.full_like(a, 7), torch.full_like(la, 7)
+    got = bf1.attn_decode_q8(q, cache, i32(lens), plan, B=128, out=out, lse=lse, workspace=ws)
+    assert got[0] is out and got[1] is lse and torch.equal(out, a) and torch.equal(lse, la)
+    assert (ws[need:] == 255).all()
+
+
+def test_nothing_to_do():
+    none = i32([])
+    cache = bf1.cache_q8(3, 0, 2, 64)
+    o, lse = bf1.attn_decode_q8(normal(1, 0, 4, 64), cache, none, i32(np.zeros((0, 5))))
+    assert o.shape == (0, 4, 64) and lse.shape == (0, 4)
+    k = normal(1, 0, 2, 64)
+    bf1.kv_append_q8(k, k, none, none, i32([0]), i32([0]), i32(np.zeros((0, 3))), cache)
+    pages = normal(2, 3, 2, 64, 64)
+    want = pages.clone()
+    bf1.kv_append(k, k, torch.empty(0, dtype=torch.int64, device="cuda"), pages, pages.clone())
+    assert torch.equal(pages, want)
 
 
 def test_decode_q8_short_lists_in_wide_rows():
