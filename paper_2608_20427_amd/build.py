@@ -3,19 +3,24 @@
     python -m paper_2608_20427_amd.build          # or __graft_entry__.build()
 
 The device code is compiled by hipcc for gfx950 only; the C-ABI shim is plain
-host C++ (g++ against the HIP runtime headers).  Packed FP32 VALU forms are
-disabled in device code on purpose.
+host C++ (g++ against the HIP runtime headers), and so is _marshal.so, the native
+marshalling of the cache's operators (against torch's headers; torch itself is not
+imported).  Packed FP32 VALU forms are disabled in device code on purpose.
 """
+
+import importlib.util
 
 import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libbf1.so")
+MARSHAL = os.path.join(HERE, "_marshal.so")
 ROCM = os.environ.get("ROCM_PATH", "/opt/rocm")
 ARCH = "gfx950"
 
@@ -68,6 +73,15 @@ def build(verbose=False, extra_hip_flags=()):
           "-o", tmp,
           f"-L{ROCM}/lib", "-lamdhip64", f"-Wl,-rpath,{ROCM}/lib"], verbose)
     os.replace(tmp, LIB)
+    torch = importlib.util.find_spec("torch").submodule_search_locations[0]
+    inc, lib = os.path.join(torch, "include"), os.path.join(torch, "lib")
+    tmp = MARSHAL + ".tmp"
+    _run([gxx, "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-D__HIP_PLATFORM_AMD__", "-DUSE_ROCM",
+          "-D_GLIBCXX_USE_CXX11_ABI=1", "-isystem", inc, "-isystem", os.path.join(inc, "torch", "csrc", "api", "include"),
+          "-isystem", sysconfig.get_paths()["include"], "-isystem", f"{ROCM}/include",
+          os.path.join(CSRC, "bf1_torch.cpp"), "-o", tmp, f"-L{lib}", "-lc10", "-lc10_hip", "-ltorch_cpu",
+          "-ltorch_python", f"-L{HERE}", "-l:libbf1.so", "-Wl,-rpath,$ORIGIN"], verbose)
+    os.replace(tmp, MARSHAL)
     return LIB
 
 

@@ -812,6 +812,61 @@ def test_serving_steps_captured_and_replayed(fmt, B):
     serve(fmt, B, 2, [125, 62, 300], 6, graph=True)
 
 
+def test_both_ways_of_marshalling_agree():
+    """The usual call goes through native code, one that names a stream (or is unusual
+    otherwise) through Python: the same results, on the same stream."""
+    here = torch.cuda.current_stream()
+    lens, new, free, head = i32([3, 60, 0]), i32([2, 9, 700]), i32(range(30)), i32([2])
+    tables = [i32(np.full((3, 12), 1)) for _ in range(3)]
+    a = bf1.page_step(lens, new, tables[0], free, head, 720)
+    b = bf1.page_step(lens, new, tables[1], free, head, 720, stream=here)
+    c = bf1.page_step(lens, new, tables[2], free, head, np.int64(720))
+    for x, y, z in zip(a, b, c):
+        assert torch.equal(x, y) and torch.equal(x, z) and x.dtype == y.dtype and x.shape == y.shape
+    assert torch.equal(tables[0], tables[1]) and torch.equal(tables[0], tables[2])
+
+    freqs, amp = bf1.rope_freqs(64, scaling="bands", factor=2.0)
+    for dtype in (torch.bfloat16, torch.float32):
+        rows = normal(1, 2, 37, 6, 128, dtype=dtype)
+        for q, k, pos in ((rows[0, :, :4], rows[0, :, 4:], i32(range(37))),
+                          (rows[:, :, :4].transpose(1, 2), rows[:, :, 4:].transpose(1, 2), i32(range(37))),
+                          (rows[:, :, :4].transpose(1, 2), rows[:, :, 4:].transpose(1, 2), i32(np.arange(74).reshape(2, 37)))):
+            for fn in (bf1.rope, bf1.rope_bwd):
+                for inter in (False, True):
+                    x = fn(q, k, pos, freqs, interleaved=inter, amplitude=amp)
+                    y = fn(q, k, pos, freqs, interleaved=inter, amplitude=amp, stream=here)
+                    assert all(torch.equal(u, v) and u.is_contiguous() for u, v in zip(x, y))
+        p = torch.nn.Parameter(q.clone(), requires_grad=True)  # served, and no graph is made
+        assert torch.equal(bf1.rope(p, k, pos, freqs, amplitude=amp)[0], bf1.rope(q, k, pos, freqs, amplitude=amp)[0])
+        assert torch.equal(bf1.rope(q, k, pos, freqs, amplitude=1)[0], bf1.rope(q, k, pos, freqs, amplitude=1.0)[0])
+
+    kv = normal(3, 720, 4, 64)
+    pages = [normal(4, 32, 2, 64, 64) for _ in range(4)]
+    bf1.kv_append(kv[:, :2], kv[:, 2:], a.slots, pages[0], pages[1])
+    bf1.kv_append(kv[:, :2], kv[:, 2:], a.slots, pages[2], pages[3], stream=here)
+    assert torch.equal(pages[0], pages[2]) and torch.equal(pages[1], pages[3])
+
+    caches = [filled_cache("e4m3", 32, 3, 2, 64, 64) for _ in range(2)]
+    bf1.kv_append_q8(kv[:, :2], kv[:, 2:], lens, a.seq_lens, a.token_start, a.block_start, tables[0], caches[0])
+    bf1.kv_append_q8(kv[:, :2], kv[:, 2:], lens, a.seq_lens, a.token_start, a.block_start, tables[0], caches[1], stream=here)
+    for x, y in zip(*caches):
+        assert torch.equal(x.view(torch.uint8), y.view(torch.uint8))
+
+    for many, dense in (([200, 9], False), ([9000, 70], True)):  # without and with splits
+        q, cache, table = decode_case("int8", many, 4, 2, 64, 64, 2, dense, 12)
+        (x, lx), plan = run_decode(q, cache, table, many, 64, 2, dense)
+        y, ly = bf1.attn_decode_q8(q, tuple(cache), i32(many), plan, stream=here)
+        assert torch.equal(x, y) and torch.equal(lx, ly) and lx.shape == ly.shape
+    side = torch.cuda.Stream()
+    side.wait_stream(here)
+    with torch.cuda.stream(side):  # the current stream, whichever it is
+        torch.cuda._sleep(10 ** 7)
+        z, lz = bf1.attn_decode_q8(q, cache, i32(many), plan)
+        z, lz = z.clone(), lz.clone()
+    side.synchronize()
+    assert torch.equal(x, z) and torch.equal(lx, lz)
+
+
 def test_another_stream():
     """On a stream of the caller's, with memory of the operators' own: the same bits."""
     lens = [5000, 321, 64]
