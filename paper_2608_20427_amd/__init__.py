@@ -524,10 +524,11 @@ def attn_decode(q, k_pages, v_pages, seq_lens, plan, B=64, out=None, lse=None, w
 
 # The usual call of each operator (plain tensors on the current device, outputs of its
 # own) is marshalled natively, in _marshal.so: the same checks, allocations and library
-# call, which cost 6 to 10 us as Python code and 1 to 3 there.  Anything else, also what
-# has to be refused, goes through the Python code below it, which names what is wrong.
-# Host time per call, Python / native, us: page_step 12.1 / 7.9, rope of q and k 13.4 /
-# 6.6, kv_append 8.6 / 4.5, kv_append_q8 12.4 / 4.8, attn_decode_q8 14.6 / 6.4.
+# call, of which all but the launch (3.8 us) cost 5 to 11 us as Python code and 0.4 to 3
+# there.  Anything else, also what has to be refused, goes through the Python code below
+# it, which names what is wrong.  Host time per call, Python / native, us: page_step
+# 12.1 / 7.0, rope of q and k 13.4 / 5.8, kv_append 8.6 / 4.2, kv_append_q8 12.4 / 4.8,
+# attn_decode_q8 14.6 / 7.0.
 _MARSHAL = None
 
 

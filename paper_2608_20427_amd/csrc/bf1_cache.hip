@@ -70,7 +70,9 @@ __device__ __forceinline__ uint32_t group_scan(uint32_t x, uint32_t* part, uint3
 // writes the table entry, and no row reads an entry that this launch writes.
 //
 // Bound by latency: 20 bytes per sequence and 12 per row.  Every workgroup sums the
-// batch for itself (SEQS sequences at a time), so that one launch does it.
+// batch for itself (SEQS sequences at a time), so that one launch does it.  32 sequences
+// of a row each 4.4 us, 48 of 84K rows 4.6, 2000 of a row 7.5 (two rounds); an empty
+// kernel takes 2.2.  Four rows per thread and scans through LDS moves: 5.4 and 8.4.
 constexpr int SPT = 4;                   // sequences per thread and round
 constexpr int SEQS = THREADS * SPT;
 constexpr int ROWS_PER_GROUP = THREADS;  // a row per thread
@@ -325,7 +327,9 @@ __global__ __launch_bounds__(THREADS) void rope_kernel(RopeSide q, RopeSide k, c
 // ---------------------------------------------------------------------------
 // Rows into bf16 pages
 // ---------------------------------------------------------------------------
-// One lane per 16 bytes of a row of K or V; a row without a slot is left out.
+// One lane per 16 bytes of a row of K and of V; a row without a slot is left out.  Bound
+// by memory: 16294 rows of 8 heads of 128 27 us for 134 MB (4.9 TB/s; a large copy reaches
+// 5.1).
 __global__ __launch_bounds__(THREADS) void kv_append_kernel(
     const __bf16* __restrict__ k, const __bf16* __restrict__ v, int64_t kt, int64_t kh, int64_t vt, int64_t vh,
     const int64_t* __restrict__ slots, __bf16* __restrict__ k_pages, __bf16* __restrict__ v_pages, int64_t items,
@@ -360,7 +364,11 @@ __global__ __launch_bounds__(THREADS) void kv_append_kernel(
 // of 8 dims, so that V, which pages hold with keys side by side (the attention's
 // operand as it stands), is turned in registers and goes out through LDS.  The
 // workgroup of a sequence's first touched block also writes the tail, after it has
-// read it.
+// read it.  Neighbouring workgroups take the heads of the same rows.
+//
+// Bound by memory, a block's load, scale and code behind each other: 36585 rows of 8 heads
+// of 128 49 us (e4m3) and 51 (int8) for 225 MB (4.6 and 4.4 TB/s).  A row each for 64
+// sequences 5.4 us: where the sequence is, its lengths, its rows, one after the other.
 struct QuantE4m3 {
     static constexpr bool INT8 = false;
 };

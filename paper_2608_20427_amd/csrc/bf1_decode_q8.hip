@@ -15,6 +15,12 @@
 // the sum of p.  Codes are exact in bf16, so both products run on the bf16 matrix
 // instructions and the scales multiply fp32 numbers: the scores' sums, and the
 // weights before they are split in two bf16 parts (16 bits together).
+//
+// Bound by memory (the vector unit is busy a fifth of a long list's time): one dense
+// list of 64K, 16/8 heads of 128 27.7 us with its merge for 134 MB, 12 ragged ones of up to
+// 32K with groups of 8 60 us for 293 MB, 32 sequences of 64K on the BF1 route 12.7 us for 51
+// MB (the bf16 decode 19.6 for 101), one sequence 8.7 us: 5.2 for a launch and a single
+// unit, the rest what one compute unit takes to fetch eleven.
 #include <hip/hip_runtime.h>
 #include <float.h>
 #include <math.h>
