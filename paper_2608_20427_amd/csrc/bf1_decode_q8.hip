@@ -17,9 +17,9 @@
 // weights before they are split in two bf16 parts (16 bits together).
 //
 // Bound by memory (the vector unit is busy a fifth of a long list's time): one dense
-// list of 64K, 16/8 heads of 128 27.7 us with its merge for 134 MB, 12 ragged ones of up to
-// 32K with groups of 8 60 us for 293 MB, 32 sequences of 64K on the BF1 route 12.7 us for 51
-// MB (the bf16 decode 19.6 for 101), one sequence 8.7 us: 5.2 for a launch and a single
+// list of 64K, 16/8 heads of 128 27.0 us with its merge for 134 MB, 12 ragged ones of up to
+// 32K with groups of 8 60 us for 293 MB, 32 sequences of 64K on the BF1 route 12.6 us for 51
+// MB (the bf16 decode 19.6 for 101), one sequence 8.1 us: 4.7 for a launch and a single
 // unit, the rest what one compute unit takes to fetch eleven.
 #include <hip/hip_runtime.h>
 #include <float.h>
@@ -118,9 +118,9 @@ __global__ __launch_bounds__(THREADS, 3) void decode_q8_kernel(
     constexpr int KL = D / 64;         // 16-byte loads of a key row per lane
     constexpr int DT = D / 16;         // 16-wide tiles of O
     constexpr int OST = D + 4;         // floats per q-head in LDS
-    constexpr int V_BYTES = UPP * UNIT * 2 * D;  // V rows of the tail
-    constexpr int R_BYTES = (WAVES * (OST + 2) + 1) * G * 4;
-    __shared__ __align__(256) u32x4 lds[(V_BYTES > R_BYTES ? V_BYTES : R_BYTES) / 16 + 1];
+    __shared__ __align__(256) u32x4 lds[UPP * UNIT * 2 * D / 16];  // V rows of the tail
+    __shared__ __align__(16) float r_o[WAVES * G * OST];          // the waves' sums
+    __shared__ float r_m[WAVES * G * 2];                          // and their maxima and sums of weights
 
     const int tid = threadIdx.x;
     const int lane = tid & 63;
@@ -358,7 +358,7 @@ __global__ __launch_bounds__(THREADS, 3) void decode_q8_kernel(
     // infinite the second part may be anything: a finite number leaves the first's
     // infinity as it is (an fmax ignores a NaN).  A compare and select per element instead
     // costs a step of one sequence 0.85 us.  Then all waves' sums under one maximum, through
-    // LDS, over the tail's V rows.
+    // LDS of their own: one barrier; over the tail's V rows it took three, 0.55 us more.
 #pragma unroll
     for (int t = 0; t < DT; ++t)
 #pragma unroll
@@ -368,60 +368,43 @@ __global__ __launch_bounds__(THREADS, 3) void decode_q8_kernel(
             acc[t][r] += fminf(fmaxf(lo, -FLT_MAX), FLT_MAX);
         }
     l_run = col_sum(l_run);
-    float* r_m = reinterpret_cast<float*>(&lds[0]);  // [wave][q-head][max, sum]
-    float* r_o = r_m + WAVES * G * 2;                // [wave][q-head][OST]
-    float* r_l = r_o + WAVES * G * OST;              // [q-head]
-    __syncthreads();
-    if (quad == 0 && col < G) {
-        r_m[(wave * G + col) * 2] = m_run;
-        r_m[(wave * G + col) * 2 + 1] = l_run;
-    }
-    __syncthreads();
-    float M = -INFINITY, l = 0.f;
-#pragma unroll
-    for (int w = 0; w < WAVES; ++w) M = fmaxf(M, r_m[(w * G + col % G) * 2]);
-    const float M_use = M == -INFINITY ? 0.f : M;
-#pragma unroll
-    for (int w = 0; w < WAVES; ++w)
-        l = fmaf(r_m[(w * G + col % G) * 2 + 1], decay(r_m[(w * G + col % G) * 2] - M_use), l);
-    const float scale = decay(m_run - M_use);
     if (col < G) {
         float* dst = r_o + (wave * G + col) * OST + 4 * quad;
 #pragma unroll
-        for (int t = 0; t < DT; ++t) {
-            f32x4 o;
-#pragma unroll
-            for (int r = 0; r < 4; ++r) o[r] = acc[t][r] * scale;
-            *reinterpret_cast<f32x4*>(dst + 16 * t) = o;
+        for (int t = 0; t < DT; ++t) *reinterpret_cast<f32x4*>(dst + 16 * t) = acc[t];
+        if (quad == 0) {
+            r_m[(wave * G + col) * 2] = m_run;
+            r_m[(wave * G + col) * 2 + 1] = l_run;
         }
-    }
-    const int64_t rec = bh * nsplit + s;
-    if (tid < G) {  // lane tid of the first wave holds q-head tid's
-        if (nsb == 1) {
-            if (LSE != nullptr) LSE[orow + tid] = (M + log2f(l)) * LN2;
-        } else {
-            float* ml = ws + (int64_t)gridDim.x * Hkv * nsplit * G * D + (rec * G + tid) * 2;
-            ml[0] = M;
-            ml[1] = l;
-        }
-        r_l[tid] = l;
     }
     __syncthreads();
+    const int64_t rec = bh * nsplit + s;
     for (int x = tid; x < G * D / 4; x += THREADS) {
         const int e = x / (D / 4), d = x % (D / 4) * 4;
+        float M = -INFINITY, l = 0.f;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) M = fmaxf(M, r_m[(w * G + e) * 2]);
+        const float M_use = M == -INFINITY ? 0.f : M;
         f32x4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int w = 0; w < WAVES; ++w) {
+            const float scale = decay(r_m[(w * G + e) * 2] - M_use);
             const f32x4 y = *reinterpret_cast<const f32x4*>(r_o + (w * G + e) * OST + d);
+            l = fmaf(r_m[(w * G + e) * 2 + 1], scale, l);
 #pragma unroll
-            for (int r = 0; r < 4; ++r) o[r] += y[r];
+            for (int r = 0; r < 4; ++r) o[r] = fmaf(y[r], scale, o[r]);
         }
         if (nsb == 1) {
-            const float sum = r_l[e];
             *reinterpret_cast<bf16x4*>(O + orow * D + 4 * x) =
-                bf16x4{(__bf16)(o[0] / sum), (__bf16)(o[1] / sum), (__bf16)(o[2] / sum), (__bf16)(o[3] / sum)};
+                bf16x4{(__bf16)(o[0] / l), (__bf16)(o[1] / l), (__bf16)(o[2] / l), (__bf16)(o[3] / l)};
+            if (d == 0 && LSE != nullptr) LSE[orow + e] = (M + log2f(l)) * LN2;
         } else {
             *reinterpret_cast<f32x4*>(ws + rec * (G * D) + 4 * x) = o;
+            if (d == 0) {
+                float* ml = ws + (int64_t)gridDim.x * Hkv * nsplit * G * D + (rec * G + e) * 2;
+                ml[0] = M;
+                ml[1] = l;
+            }
         }
     }
 }
@@ -523,13 +506,13 @@ hipError_t launch_d(const Args& a, int32_t G, int32_t B, hipStream_t st) {
 // Workgroups go to compute units in turns, and a unit of two while others have one ends
 // last: a long list (four rounds of a unit per wave and split, or more) gets the fewest
 // splits that leave less than one place in twenty empty.  us with one split, with 256
-// workgroups or the next below, and so chosen: 320 rows of 128 units 123 / 126 / 95; 160
-// rows 63 / 67 / 51; 192 rows 69 / 69 / 56; 96 rows of 256 units 116 / 71 / 55; 48 rows
-// of 512 units 217 / 63 / 57; 64 rows of 512 (heads of 64) 128 / 41 / 41.
+// workgroups or the next below, and so chosen: 320 rows of 128 units 124 / 124 / 95; 160
+// rows 67 / 67 / 51; 192 rows 69 / 69 / 56; 96 rows of 256 units 118 / 68 / 56; 48 rows
+// of 512 units 218 / 60 / 56; 64 rows of 512 (heads of 64) 129 / 41 / 41.
 //
 // Shorter lists: at most 256 workgroups, and a list is cut only where that saves three
 // rounds.  A round takes some 1.5 us, the merge 2 to 3 and a launch more.  us, uncut /
-// cut: 12 units, 8 rows 8.7 / 8.4, 160 rows 12.1 / 13.1; 33 units, 8 rows 18.1 / 9.2.
+// cut: 12 units, 8 rows 8.1 / 7.7, 160 rows 11.7 / 12.6; 33 units, 8 rows 17.5 / 8.5.
 //
 // More than 32 splits cost the merge more than they save: 256 units, 2 rows 16 for 14.
 constexpr int64_t PLACES = 256, MANY_ROWS = 2048;
