@@ -111,10 +111,14 @@ __global__ __launch_bounds__(THREADS, 3) void decode_q8_kernel(
     float* __restrict__ ws, int32_t Hkv, int32_t nsplit, float c_log2) {
     constexpr int UPP = PW / UNIT;     // units of a page
     // A page of 64 is read once, by one wave: past the caches, which brings much of it
-    // sooner (us, past / through: 128 sequences of 4K 29.8 / 30.7, one dense list of 64K 28.9
-    // / 33.6; 32 sequences of 64K 12.9 / 12.4).  Two waves share the lines of the V rows of a
-    // page of 128, which go through (12 dense lists of 32K 71 / 78).
-    constexpr int CPOL = PW == UNIT ? CPOL_NT : 0;
+    // sooner (us, past / through: 128 sequences of 4K 28.5 / 30.2, one dense list of 64K 26.8
+    // / 30.1, 32 sequences of 64K 12.6 / 13.5).  Two waves share the lines of the V rows of a
+    // page of 128, which go through (12 dense lists of 32K 70 / 67).  Its K rows are one
+    // wave's: those of heads of 64 past (8 dense lists of 32K 42.9 / 46.1), those of heads
+    // of 128 through, where past both gains and loses (128 sequences of 4K 45.7 / 46.5, the 12
+    // lists 67.5 / 66.9).
+    constexpr int V_POL = PW == UNIT ? CPOL_NT : 0;
+    constexpr int K_POL = PW == UNIT || D == 64 ? CPOL_NT : 0;
     constexpr int KL = D / 64;         // 16-byte loads of a key row per lane
     constexpr int DT = D / 16;         // 16-wide tiles of O
     constexpr int OST = D + 4;         // floats per q-head in LDS
@@ -210,14 +214,14 @@ __global__ __launch_bounds__(THREADS, 3) void decode_q8_kernel(
 #pragma unroll
             for (int kl = 0; kl < KL; ++kl)
                 kw[t][kl] = __builtin_amdgcn_raw_buffer_load_b128(
-                    r, (16 * (col >> 2) + (col & 3)) * D + 16 * quad + 4 * t * D + 64 * kl, u % UPP * UNIT * D, CPOL);
+                    r, (16 * (col >> 2) + (col & 3)) * D + 16 * quad + 4 * t * D + 64 * kl, u % UPP * UNIT * D, K_POL);
     };
     auto load_v = [&](int u, int64_t slice, uint32_t bytes) {
         const __amdgpu_buffer_rsrc_t r = head_rsrc(Vp + slice * (PW * D), bytes);
         vs = v_scale[slice];
 #pragma unroll
         for (int t = 0; t < DT; ++t)
-            vw[t] = __builtin_amdgcn_raw_buffer_load_b128(r, col * PW + 16 * quad, u % UPP * UNIT + 16 * t * PW, CPOL);
+            vw[t] = __builtin_amdgcn_raw_buffer_load_b128(r, col * PW + 16 * quad, u % UPP * UNIT + 16 * t * PW, V_POL);
     };
 
     // This wave's units; at most one is the tail's, and it goes first: 64 rows in bf16,
