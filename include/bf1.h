@@ -442,7 +442,7 @@ int bf1_kv_append_q8(const void* K, const void* V, int64_t k_token_stride, int64
  * (bf1_decode_plan); earlier pages are read in 8 bits, keys j*B .. t from the tail.
  * Stale and unplannable sequences get NaN, foreign plan rows stay inside the cache,
  * rows of the tail past t are masked exactly, as there.  The page of block j itself
- * is not read.  Weights are applied with 16 bits, sums are fp32; deterministic.
+ * is not read.  Weights are applied with their 24 bits, sums are fp32; deterministic.
  * workspace: at least bf1_decode_q8_workspace_size() bytes, 16-byte aligned (none is
  * needed, and it may be NULL, where that is 0).  Supported as bf1_decode_attn.
  */

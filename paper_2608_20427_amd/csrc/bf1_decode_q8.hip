@@ -14,7 +14,7 @@
 // Score of a key: c * scale_k * sum_d q code; output: sum of p * scale_v * code over
 // the sum of p.  Codes are exact in bf16, so both products run on the bf16 matrix
 // instructions and the scales multiply fp32 numbers: the scores' sums, and the
-// weights before they are split in two bf16 parts (16 bits together).
+// weights before they are split in three bf16 parts (all 24 bits of them).
 //
 // Bound by memory (the vector unit is busy a fifth of a long list's time): one dense
 // list of 64K, 16/8 heads of 128 27.0 us with its merge for 134 MB, 12 ragged ones of up to
@@ -187,16 +187,27 @@ __global__ __launch_bounds__(THREADS, 3) void decode_q8_kernel(
         }
         return m_use;
     };
-    // This column's part of two weights: their bf16 roundings, or the rounded rests (for
-    // 16 bits together).  `first` is what the roundings are made of.  Columns past the
-    // two parts repeat the second; nothing reads them.
-    const bool second = col >= G;
-    auto parts = [&](float w0, float w1, float first0, float first1) -> uint32_t {
-        const uint32_t hi = __builtin_bit_cast(uint32_t, bf16x2{(__bf16)first0, (__bf16)first1});
-        const float r0 = w0 - __uint_as_float(hi << 16), r1 = w1 - __uint_as_float(hi & 0xffff0000u);
-        const uint32_t lo = __builtin_bit_cast(uint32_t, bf16x2{(__bf16)r0, (__bf16)r1});
-        return second ? lo : hi;
+    // A weight's 24 bits are three bf16 parts, 8 bits each.  Column col takes part col / G of
+    // head col % G, so groups up to 4 have all three side by side (columns past them repeat
+    // the third; nothing reads them), and groups of 8 the first two; the third is a product
+    // of its own there, added to the columns of the first.  With two parts an output that
+    // is a small difference of large weights lost bits, and 12 dense lists of 32K were 1.2e-4
+    // (2-norm, mostly bf16 steps) from the same in fp32, 6.6e-5 with three; us, two / three:
+    // those lists, groups of 8, 70.6 / 71.5, 32 sequences of 64K on the BF1 route 11.65 /
+    // 11.71, one sequence 8.06 / 8.20.
+    constexpr bool OWN3 = 3 * G > 16;
+    constexpr uint32_t FIRST = 0xffff0000u, TWO = 0xffffff00u;  // where a weight holds them
+    const uint32_t upto = OWN3 || col < 2 * G ? TWO : ~0u, from = col < G ? 0 : OWN3 || col < 2 * G ? FIRST : TWO;
+    auto between = [](float w, uint32_t above, uint32_t below) {  // the bits of `above` without those of `below`
+        const uint32_t x = __float_as_uint(w);
+        return __uint_as_float(x & above) - __uint_as_float(x & below);
     };
+    auto uppers = [](float w0, float w1) {
+        return __builtin_amdgcn_perm(__float_as_uint(w1), __float_as_uint(w0), 0x07060302u);
+    };
+    auto parts = [&](float w0, float w1) { return uppers(between(w0, upto, from), between(w1, upto, from)); };
+    auto third = [&](float w) { return between(w, ~0u, TWO); };
+    auto thirds = [&](float r0, float r1) { return from == 0 ? uppers(r0, r1) : 0u; };  // in the first's columns
 
     // 64 keys of a page.  Row i = 4 q + r of score tile t is key 16 q + 4 t + r, so that
     // lane group q ends with the scores of keys 16 q .. 16 q + 15, in the order of the
@@ -287,14 +298,18 @@ __global__ __launch_bounds__(THREADS, 3) void decode_q8_kernel(
         const uint32_t vtr = lds_addr(vbuf) + tr * RB + 8 * (col & 3) + 32 * vslot(tr);
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
-            u32x2 pb;
+            u32x2 pb, pb3;
 #pragma unroll
             for (int r = 0; r < 4; r += 2) {
-                // the first part of a weight is not 0 while the weight is not (see decay)
+                // what multiplies a value in a column of first parts is not 0 while the
+                // weight is not (see decay)
                 const float x0 = ts[t][r] - tm, x1 = ts[t][r + 1] - tm;
                 const float w0 = __builtin_amdgcn_exp2f(x0), w1 = __builtin_amdgcn_exp2f(x1);
                 l_run += w0 + w1;
-                pb[r / 2] = parts(w0, w1, x0 > -150.f ? fmaxf(w0, MIN_PART) : w0, x1 > -150.f ? fmaxf(w1, MIN_PART) : w1);
+                const float least0 = x0 > -150.f ? MIN_PART : 0.f, least1 = x1 > -150.f ? MIN_PART : 0.f;
+                const float y0 = fmaxf(w0, least0), y1 = fmaxf(w1, least1);
+                pb[r / 2] = parts(y0, y1);
+                if constexpr (OWN3) pb3[r / 2] = thirds(fmaxf(third(y0), least0), fmaxf(third(y1), least1));
             }
 #pragma unroll
             for (int d0 = 0; d0 < DT; d0 += 4) {
@@ -311,6 +326,11 @@ __global__ __launch_bounds__(THREADS, 3) void decode_q8_kernel(
                 for (int x = 0; x < 4; ++x)
                     acc[d0 + x] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(
                         __builtin_bit_cast(s16x4, vt[x]), __builtin_bit_cast(s16x4, pb), acc[d0 + x], 0, 0, 0);
+                if constexpr (OWN3)
+#pragma unroll
+                    for (int x = 0; x < 4; ++x)
+                        acc[d0 + x] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(
+                            __builtin_bit_cast(s16x4, vt[x]), __builtin_bit_cast(s16x4, pb3), acc[d0 + x], 0, 0, 0);
             }
         }
     }
@@ -337,38 +357,46 @@ __global__ __launch_bounds__(THREADS, 3) void decode_q8_kernel(
         }
         load_k(next, slice, bytes);
         const float m = soften(sc);
-        u32x4 pb[2];
+        u32x4 pb[2], pb3[2];
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
             for (int r = 0; r < 4; r += 2) {
                 const float w0 = __builtin_amdgcn_exp2f(sc[t][r] - m), w1 = __builtin_amdgcn_exp2f(sc[t][r + 1] - m);
                 l_run += w0 + w1;
-                pb[t >> 1][2 * (t & 1) + r / 2] = parts(w0 * vs, w1 * vs, w0 * vs, w1 * vs);
+                pb[t >> 1][2 * (t & 1) + r / 2] = parts(w0 * vs, w1 * vs);
+                if constexpr (OWN3) pb3[t >> 1][2 * (t & 1) + r / 2] = thirds(third(w0 * vs), third(w1 * vs));
             }
 #pragma unroll
         for (int t = 0; t < DT; ++t)
 #pragma unroll
-            for (int y = 0; y < 2; ++y)
-                acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8<F>(vw[t][2 * y], vw[t][2 * y + 1]),
-                                                                 __builtin_bit_cast(bf16x8, pb[y]), acc[t],
-                                                                 0, 0, 0);
+            for (int y = 0; y < 2; ++y) {
+                const bf16x8 v = widen8<F>(vw[t][2 * y], vw[t][2 * y + 1]);
+                acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, __builtin_bit_cast(bf16x8, pb[y]), acc[t], 0, 0, 0);
+                if constexpr (OWN3) {
+                    const bf16x8 p3 = __builtin_bit_cast(bf16x8, pb3[y]);
+                    acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p3, acc[t], 0, 0, 0);
+                }
+            }
         load_v(next, slice, bytes);
         u = next;
     }
 
     // ---- the waves' results ------------------------------------------------------
-    // A q-head's second parts, G columns further, to its first.  Where a value is
-    // infinite the second part may be anything: a finite number leaves the first's
-    // infinity as it is (an fmax ignores a NaN).  A compare and select per element instead
-    // costs a step of one sequence 0.85 us.  Then all waves' sums under one maximum, through
-    // LDS of their own: one barrier; over the tail's V rows it took three, 0.55 us more.
+    // A q-head's second (and third) parts, G columns further (and as many again), to its
+    // first.  Where a value is infinite these may be anything: a finite number leaves the
+    // first's infinity as it is (an fmax ignores a NaN).  A compare and select per element
+    // instead costs a step of one sequence 0.85 us.  Then all waves' sums under one
+    // maximum, through LDS of their own: one barrier; over the tail's V rows it took three,
+    // 0.55 us more.
 #pragma unroll
     for (int t = 0; t < DT; ++t)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            const float lo = __uint_as_float(
-                __builtin_amdgcn_update_dpp(0, __float_as_uint(acc[t][r]), 0x100 + G, 0xf, 0xf, true));  // row_shl:G
+            auto next = [](float x) {  // of the column G further (row_shl:G)
+                return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), 0x100 + G, 0xf, 0xf, true));
+            };
+            const float lo = next(OWN3 ? acc[t][r] : acc[t][r] + next(acc[t][r]));
             acc[t][r] += fminf(fmaxf(lo, -FLT_MAX), FLT_MAX);
         }
     l_run = col_sum(l_run);

@@ -1,0 +1,91 @@
+"""GPU tests of the cache's operators where their size or their inputs change the
+path: precision of the decode's weights, searches over many sequences, lanes that own
+two heads, far positions, guards around every buffer.  Against the plain definitions
+(oracle/cache_oracle.py); helpers and bars are tests/test_gpu_cache.py's."""
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2608_20427_amd as bf1
+from oracle import cache_oracle as co
+from test_gpu_cache import CODES, f64, i32
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _need_gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    bf1.load()
+    yield
+    torch.cuda.synchronize()
+
+
+# ---- attn_decode_q8: bits of the weights -------------------------------------------------
+
+@pytest.mark.parametrize("fmt", ["e4m3", "int8", "tail"])
+@pytest.mark.parametrize("G", [1, 2, 4, 8])
+@pytest.mark.parametrize("d,B", [(64, 64), (128, 64), (64, 128), (128, 128)])
+def test_decode_q8_weights_keep_their_bits(fmt, G, d, B):
+    """Pairs of keys whose weights differ by 2^-16 of themselves, with opposite values: an
+    output is the difference.  Weights of w bits put an error of up to 2^-w of the pair's
+    mass on it.  In fp32: four roundings of a score below 1.5 (4 |s| 2^-24 of the weight),
+    exp2 (2^-23), the value's scale (2^-24), six sums (6 2^-24): below 2^-20; then half
+    a bf16 step of the output."""
+    tail, Hkv = fmt == "tail", 2
+    Hq = G * Hkv
+    cache = bf1.cache_q8(2, 1, Hkv, d, B, CODES["int8" if tail else fmt])
+    code = torch.zeros((B, d))
+    value = torch.zeros((B, d))
+    for i in range(B // 2):
+        code[2 * i:2 * i + 2, 0] = -(1 + i % 15)
+        code[2 * i + 1, 1] = 1
+        value[2 * i, i], value[2 * i + 1, i] = 1, -1
+    ks, vs = (0.5, 0.75) if not tail else (1.0, 1.0)
+    q = torch.zeros((1, Hq, d))
+    for h in range(Hq):
+        q[0, h, 0] = (0.5 + h / 32) * (0.5 if tail else 1)
+        q[0, h, 1] = 2.0 ** -13 if tail else 2.0 ** -12
+    q = q.to(torch.bfloat16).cuda()
+    if tail:
+        cache.k_tail.copy_(code.cuda().expand(1, Hkv, B, d))
+        cache.v_tail.copy_(value.cuda().expand(1, Hkv, B, d))
+        n, plan = B, [[0, 0, 0]]
+        keys, values = code, value
+    else:
+        cache.k_pages[1] = code.cuda().to(CODES[fmt])
+        cache.v_pages[1] = value.t().contiguous().cuda().to(CODES[fmt])
+        cache.k_scale.fill_(ks)
+        cache.v_scale.fill_(vs)
+        n, plan = B + 1, [[1, 1, 1, 0]]  # and one key of the tail: zeros
+        keys, values = (torch.cat([x * s, torch.zeros(1, d)]) for x, s in ((code, ks), (value, vs)))
+    o, _ = bf1.attn_decode_q8(q, cache, i32([n]), i32(plan), B=B)
+    o = f64(o)
+    for h in range(Hq):
+        ref, _, mass = co.decode(f64(q)[0, h], f64(keys), f64(values))
+        assert (np.abs(ref[:B // 2]) > 0).all()
+        bad = np.abs(o[0, h] - ref) > 2.0 ** -8 * np.abs(ref) + 2.0 ** -20 * mass
+        assert not bad.any(), (h, bad.sum(), np.abs(o[0, h] - ref).max() / mass.max())
+
+
+@pytest.mark.parametrize("G", [1, 2, 4, 8])
+@pytest.mark.parametrize("d", [64, 128])
+def test_decode_q8_infinite_values_under_every_part(G, d):
+    """An infinite value shows as itself whatever the parts of its key's weight: under a
+    weight of 1 (two of them are 0), of e^-100, and of any other size."""
+    cache = bf1.cache_q8(1, 1, 1, d, 64)
+    q = torch.ones((1, G, d), dtype=torch.bfloat16, device="cuda")
+    for key, score in enumerate((100.0, 0.0, 99.3, 99.9, 95.0)):
+        cache.k_tail[0, 0, key, 0] = round(score * d ** 0.5)
+        cache.v_tail[0, 0, key] = 1.0
+        cache.v_tail[0, 0, key, 2 * key] = float("inf")
+        cache.v_tail[0, 0, key, 2 * key + 1] = -float("inf")
+    cache.v_tail[0, 0, 3, 20] = float("nan")
+    cache.v_tail[0, 0, 1, 21], cache.v_tail[0, 0, 2, 21] = float("inf"), -float("inf")
+    o, lse = bf1.attn_decode_q8(q, cache, i32([5]), i32([[0, 0, 0]]))
+    o = o[0].float()
+    assert (o[:, 0:10:2] == float("inf")).all() and (o[:, 1:10:2] == -float("inf")).all()
+    assert torch.isnan(o[:, 20:22]).all() and (o[:, 10:20] == 1).all() and (o[:, 22:] == 1).all()
+    assert torch.isfinite(lse).all()
