@@ -380,7 +380,8 @@ int bf1_page_step(int32_t batch, const int32_t* seq_lens, const int32_t* new_len
  *   Q_out, K_out : out_type: in_type, or bf16 of fp32; may be the inputs themselves
  *               (same type and strides), otherwise they overlap neither them nor each other
  *   strides   : HOST int64[12], in elements: batch, head, token of Q, Q_out, K, K_out
- * Angles are formed in double precision and the turn in fp32, rounded once.  Even
+ * Angles are exact products, reduced to a part of a turn in double precision for any
+ * position; cosine, sine and the turn are fp32, rounded once.  Even
  * head_dim <= 1024 and rot_dim; sixteen bytes at a time where strides, addresses and
  * rot_dim are multiples of what 16 bytes hold, element by element otherwise.
  */

@@ -202,8 +202,14 @@ __global__ __launch_bounds__(THREADS) void page_step_kernel(
 // (a c - b s, b c + a s) with c, s the amplitude times cosine and sine.  The
 // gradient turns the other way (the rotation is orthogonal): `sign` = -1.  Pairs
 // are i and i + rot / 2, or (interleaved) 2 i and 2 i + 1; dims from rot on are
-// copied.  The angle is formed in 64 bits and reduced to a part of a turn there,
-// so that far positions lose nothing; cosine and sine are fp32.
+// copied.  The angle is the exact product of position and frequency, in two 64-bit
+// parts, and is reduced to a part of a turn with a 106-bit 1 / (2 pi), so that the
+// part is right to 2^-53 for every position.  Cosine and sine are taken at the nearest
+// fp32 part and turned by what that leaves, so that fp32 holds them to the function's
+// own few ulp.  With one 64-bit product each and no turn back they were up to 3.8e-7 off
+// at positions of 2^31 (2-norm of the error of float32 gradients, positions below 8191:
+// 3.4e-8, now 2.8e-8), in the same time: 32768 rows of 24 heads of 128 81.3 us, now
+// 80.3; those gradients 14.1 and 14.1.
 //
 // A lane owns P pairs of one token, 16 bytes of each half of the head, in HB heads.
 // Workgroups follow each other over the heads of the same tokens, so that rows of joined
@@ -256,6 +262,20 @@ __device__ __forceinline__ void store_n(T* p, const float* f) {
     }
 }
 
+// p * f radians without its whole turns: the nearest fp32 number of half turns, in
+// [-1, 1], and the radians left (below 2^-23).
+struct Turn {
+    float half_turns, rest;
+};
+__device__ __forceinline__ Turn turn_of(double p, double f) {
+    constexpr double INV = 0x1.45f306dc9c883p-3, INV_LOW = -0x1.6b01ec5417056p-57;  // 1 / (2 pi)
+    const double a = p * f, a_low = fma(p, f, -a);
+    const double t = a * INV, t_low = fma(a, INV, -t) + fma(a, INV_LOW, a_low * INV);
+    const double x = 2. * ((t - rint(t)) + t_low);
+    const float h = (float)x;
+    return {h, (float)((x - (double)h) * 3.141592653589793)};
+}
+
 template <typename TI, typename TO, bool INTER, int P, int HB>
 __global__ __launch_bounds__(THREADS) void rope_kernel(RopeSide q, RopeSide k, const int32_t* __restrict__ positions,
                                                        int64_t pos_batch, const double* __restrict__ freqs,
@@ -271,14 +291,14 @@ __global__ __launch_bounds__(THREADS) void rope_kernel(RopeSide q, RopeSide k, c
     float c[P], s[P];
     int32_t lo, hi = 0;  // element offsets in the head row
     if (turn) {
-        const double p = (double)positions[b * pos_batch + t] * 0.15915494309189535;  // in turns: 1 / (2 pi)
+        const double p = (double)positions[b * pos_batch + t];
 #pragma unroll
         for (int i = 0; i < P; ++i) {
-            const double x = p * freqs[l * P + i];
+            const Turn a = turn_of(p, freqs[l * P + i]);
             float cs, sn;
-            sincospif(2.f * (float)(x - rint(x)), &sn, &cs);
-            c[i] = cs * amplitude;
-            s[i] = sn * (sign * amplitude);
+            sincospif(a.half_turns, &sn, &cs);
+            c[i] = fmaf(-sn, a.rest, cs) * amplitude;
+            s[i] = fmaf(cs, a.rest, sn) * (sign * amplitude);
         }
         lo = l * E;
         hi = half + l * P;

@@ -89,3 +89,25 @@ def test_decode_q8_infinite_values_under_every_part(G, d):
     assert (o[:, 0:10:2] == float("inf")).all() and (o[:, 1:10:2] == -float("inf")).all()
     assert torch.isnan(o[:, 20:22]).all() and (o[:, 10:20] == 1).all() and (o[:, 22:] == 1).all()
     assert torch.isfinite(lse).all()
+
+
+# ---- rope: far positions, two heads per lane ---------------------------------------------
+
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_rope_far_positions_keep_fp32(interleaved):
+    """Turns of (1, 0) and (0, 1) are cosines and sines alone.  Theirs may be off by the
+    function's 4 ulp (4 * 2^-24 of at most 1) and two more roundings of what is turned
+    back and of the output (2^-24 each): 6 * 2^-24, whatever the position."""
+    d, n = 128, 4096
+    rng = np.random.default_rng(1)
+    freqs = rng.uniform(0.3, 1.0, d // 2)
+    pos = np.concatenate([rng.integers(2 ** 30, 2 ** 31, n - 6), [2 ** 31 - 1, -2 ** 31, 0, 1, -1, 2 ** 27]]).astype(np.int32)
+    x = torch.zeros((1, 2, n, d))
+    first = torch.arange(0, d, 2) if interleaved else torch.arange(d // 2)
+    x[0, 0, :, first] = 1
+    x[0, 1, :, first + (1 if interleaved else d // 2)] = 1
+    f = torch.as_tensor(freqs, device="cuda")
+    for fn, sign in ((bf1.rope, 1), (bf1.rope_bwd, -1)):
+        y, _ = fn(x.cuda(), None, i32(pos), f, interleaved=interleaved)
+        off = np.abs(f64(y) - co.rope(f64(x), pos, freqs, interleaved, 1.0, sign))
+        assert off.max() <= 6 * 2.0 ** -24, off.max()
