@@ -66,6 +66,17 @@ Tensor empty(IntArrayRef sizes, ScalarType type, int device) {
 
 void* stream_of(int device) { return c10::hip::getCurrentHIPStream((c10::DeviceIndex)device).stream(); }
 
+// The result of fn() with the interpreter's lock released: a launch waits while the
+// device's queue is full, and other Python threads go on.
+template <class F>
+int unlocked(F fn) {
+    struct Lock {
+        PyThreadState* state = PyEval_SaveThread();
+        ~Lock() { PyEval_RestoreThread(state); }
+    } lock;
+    return fn();
+}
+
 PyObject* status(int st) { return PyLong_FromLong(st); }
 
 // The tensors as a tuple.
@@ -100,11 +111,14 @@ PyObject* page_step(PyObject*, PyObject* const* a, Py_ssize_t n) {
     // one allocation, slots (8 bytes) first
     auto out = empty({3 * rows + 3 * batch + 3}, I32, dev)
                    .unsafe_split_with_sizes({2 * rows, batch, batch + 1, batch + 1, rows, 1});
-    const int st = bf1_page_step(
-        (int32_t)batch, lens->const_data_ptr<int32_t>(), more->const_data_ptr<int32_t>(), (int32_t*)table->data_ptr(),
-        (int32_t)table->size(1), free->const_data_ptr<int32_t>(), (int32_t)free->numel(), head->const_data_ptr<int32_t>(),
-        (int32_t)B, rows, (int32_t*)out[1].data_ptr(), (int32_t*)out[2].data_ptr(), (int32_t*)out[3].data_ptr(),
-        (int32_t*)out[4].data_ptr(), (int64_t*)out[0].data_ptr(), (int32_t*)out[5].data_ptr(), stream_of(dev));
+    const int st = unlocked([&] {
+        return bf1_page_step(
+            (int32_t)batch, lens->const_data_ptr<int32_t>(), more->const_data_ptr<int32_t>(), (int32_t*)table->data_ptr(),
+            (int32_t)table->size(1), free->const_data_ptr<int32_t>(), (int32_t)free->numel(),
+            head->const_data_ptr<int32_t>(), (int32_t)B, rows, (int32_t*)out[1].data_ptr(), (int32_t*)out[2].data_ptr(),
+            (int32_t*)out[3].data_ptr(), (int32_t*)out[4].data_ptr(), (int64_t*)out[0].data_ptr(),
+            (int32_t*)out[5].data_ptr(), stream_of(dev));
+    });
     if (st != BF1_OK) return status(st);
     return tuple({out[1], out[2], out[3], out[4], out[0].view(I64), out[5]});
     END_HANDLE_TH_ERRORS
@@ -150,10 +164,14 @@ PyObject* rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
     }
     if (heads[0] > INT32_MAX || heads[1] > INT32_MAX) Py_RETURN_NONE;
     const int32_t t = type == BF16 ? BF1_TYPE_BF16 : BF1_TYPE_F32;
-    const int st = bf1_rope(q->data_ptr(), k->data_ptr(), pos->const_data_ptr<int32_t>(), own ? rows : 0,
-                            freqs->const_data_ptr<double>(), qo.data_ptr(), ko.data_ptr(), (int32_t)batch, rows,
-                            (int32_t)heads[0], (int32_t)heads[1], (int32_t)d, (int32_t)(2 * freqs->numel()), t, t,
-                            a[4] == Py_True, (float)PyFloat_AS_DOUBLE(a[5]), (int32_t)transposed, strides, stream_of(dev));
+    const int32_t interleaved = a[4] == Py_True;
+    const float amplitude = (float)PyFloat_AS_DOUBLE(a[5]);
+    const int st = unlocked([&] {
+        return bf1_rope(q->data_ptr(), k->data_ptr(), pos->const_data_ptr<int32_t>(), own ? rows : 0,
+                        freqs->const_data_ptr<double>(), qo.data_ptr(), ko.data_ptr(), (int32_t)batch, rows,
+                        (int32_t)heads[0], (int32_t)heads[1], (int32_t)d, (int32_t)(2 * freqs->numel()), t, t, interleaved,
+                        amplitude, (int32_t)transposed, strides, stream_of(dev));
+    });
     return st == BF1_OK ? tuple({qo, ko}) : status(st);
     END_HANDLE_TH_ERRORS
 }
@@ -178,10 +196,12 @@ PyObject* kv_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (!vp || !step_rows(a[0], a[1], kp->size(1), kp->size(3), &dev, &k, &v)) Py_RETURN_NONE;
     const Tensor* slots = exact(a[2], I64, {k->size(0)}, &dev);
     if (!slots || kp->size(0) > INT32_MAX || kp->size(1) > INT32_MAX || kp->size(2) > INT32_MAX) Py_RETURN_NONE;
-    return status(bf1_kv_append(k->data_ptr(), v->data_ptr(), k->stride(0), k->stride(1), v->stride(0), v->stride(1),
-                                slots->const_data_ptr<int64_t>(), kp->data_ptr(), vp->data_ptr(), k->size(0),
-                                (int32_t)kp->size(0), (int32_t)kp->size(1), (int32_t)kp->size(3), (int32_t)kp->size(2),
-                                stream_of(dev)));
+    return status(unlocked([&] {
+        return bf1_kv_append(k->data_ptr(), v->data_ptr(), k->stride(0), k->stride(1), v->stride(0), v->stride(1),
+                             slots->const_data_ptr<int64_t>(), kp->data_ptr(), vp->data_ptr(), k->size(0),
+                             (int32_t)kp->size(0), (int32_t)kp->size(1), (int32_t)kp->size(3), (int32_t)kp->size(2),
+                             stream_of(dev));
+    }));
     END_HANDLE_TH_ERRORS
 }
 
@@ -228,12 +248,15 @@ PyObject* kv_append_q8(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const Tensor *before = exact(a[2], I32, {batch}, &dev), *after = exact(a[3], I32, {batch}, &dev);
     const Tensor *first = exact(a[4], I32, {batch + 1}, &dev), *blocks = exact(a[5], I32, {batch + 1}, &dev);
     if (!before || !after || !first || !blocks) Py_RETURN_NONE;
-    return status(bf1_kv_append_q8(
-        k->data_ptr(), v->data_ptr(), k->stride(0), k->stride(1), v->stride(0), v->stride(1), k->size(0), (int32_t)batch,
-        before->const_data_ptr<int32_t>(), after->const_data_ptr<int32_t>(), first->const_data_ptr<int32_t>(),
-        blocks->const_data_ptr<int32_t>(), table->const_data_ptr<int32_t>(), (int32_t)table->size(1), (int32_t)c.pages,
-        c.kp->data_ptr(), c.vp->data_ptr(), (float*)c.ks->data_ptr(), (float*)c.vs->data_ptr(), c.kt->data_ptr(),
-        c.vt->data_ptr(), (int32_t)c.Hkv, (int32_t)c.d, (int32_t)c.B, c.format, stream_of(dev)));
+    return status(unlocked([&] {
+        return bf1_kv_append_q8(
+            k->data_ptr(), v->data_ptr(), k->stride(0), k->stride(1), v->stride(0), v->stride(1), k->size(0),
+            (int32_t)batch, before->const_data_ptr<int32_t>(), after->const_data_ptr<int32_t>(),
+            first->const_data_ptr<int32_t>(), blocks->const_data_ptr<int32_t>(), table->const_data_ptr<int32_t>(),
+            (int32_t)table->size(1), (int32_t)c.pages, c.kp->data_ptr(), c.vp->data_ptr(), (float*)c.ks->data_ptr(),
+            (float*)c.vs->data_ptr(), c.kt->data_ptr(), c.vt->data_ptr(), (int32_t)c.Hkv, (int32_t)c.d, (int32_t)c.B,
+            c.format, stream_of(dev));
+    }));
     END_HANDLE_TH_ERRORS
 }
 
@@ -259,12 +282,14 @@ PyObject* attn_decode_q8(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (st != BF1_OK) return status(st);
     Tensor out = empty(q->sizes(), BF16, dev), lse = empty({batch, Hq}, F32, dev), ws;
     if (need > 0) ws = empty({need}, at::kByte, dev);
-    st = bf1_decode_attn_q8(q->data_ptr(), c.kp->data_ptr(), c.vp->data_ptr(), (const float*)c.ks->data_ptr(),
-                            (const float*)c.vs->data_ptr(), c.kt->data_ptr(), c.vt->data_ptr(),
-                            lens->const_data_ptr<int32_t>(), (int32_t)c.pages, plan->const_data_ptr<int32_t>(),
-                            (int32_t)plan->size(1), out.data_ptr(), (float*)lse.data_ptr(), (int32_t)batch, (int32_t)Hq,
-                            (int32_t)c.Hkv, (int32_t)c.d, (int32_t)B, c.format, need > 0 ? ws.data_ptr() : nullptr, need,
-                            stream_of(dev));
+    st = unlocked([&] {
+        return bf1_decode_attn_q8(
+            q->data_ptr(), c.kp->data_ptr(), c.vp->data_ptr(), (const float*)c.ks->data_ptr(),
+            (const float*)c.vs->data_ptr(), c.kt->data_ptr(), c.vt->data_ptr(), lens->const_data_ptr<int32_t>(),
+            (int32_t)c.pages, plan->const_data_ptr<int32_t>(), (int32_t)plan->size(1), out.data_ptr(),
+            (float*)lse.data_ptr(), (int32_t)batch, (int32_t)Hq, (int32_t)c.Hkv, (int32_t)c.d, (int32_t)B, c.format,
+            need > 0 ? ws.data_ptr() : nullptr, need, stream_of(dev));
+    });
     return st == BF1_OK ? tuple({out, lse}) : status(st);
     END_HANDLE_TH_ERRORS
 }

@@ -3,13 +3,20 @@ path: precision of the decode's weights, searches over many sequences, lanes tha
 two heads, far positions, guards around every buffer.  Against the plain definitions
 (oracle/cache_oracle.py); helpers and bars are tests/test_gpu_cache.py's."""
 
+import gc
+import operator
+import sys
+import threading
+import time
+from functools import partial
+
 import numpy as np
 import pytest
 import torch
 
 import paper_2608_20427_amd as bf1
 from oracle import cache_oracle as co
-from test_gpu_cache import CODES, f64, i32
+from test_gpu_cache import CODES, f64, i32, normal
 
 pytestmark = pytest.mark.gpu
 
@@ -111,3 +118,53 @@ def test_rope_far_positions_keep_fp32(interleaved):
         y, _ = fn(x.cuda(), None, i32(pos), f, interleaved=interleaved)
         off = np.abs(f64(y) - co.rope(f64(x), pos, freqs, interleaved, 1.0, sign))
         assert off.max() <= 6 * 2.0 ** -24, off.max()
+
+
+# ---- binding: other threads ----------------------------------------------------------------
+
+def _calls():
+    """The usual call of each operator that is marshalled natively, as a function of no
+    arguments."""
+    m = bf1._native()
+    k, pages = normal(1, 3, 2, 64), normal(2, 3, 2, 64, 64)
+    lens, new, table = i32([0, 0, 0]), i32([1, 1, 1]), i32([[0], [1], [2]])
+    start = i32([0, 1, 2, 3])
+    cache = bf1.cache_q8(3, 3, 2, 64)
+    freqs = torch.ones(32, dtype=torch.float64, device="cuda")
+    return {"page_step": partial(m.page_step, lens, new, table, i32(range(9)), i32([0]), 3, 64),
+            "rope": partial(m.rope, k, k, lens, freqs, False, 1.0, 0),
+            "kv_append": partial(m.kv_append, k, k, torch.arange(3, device="cuda"), pages, pages.clone()),
+            "kv_append_q8": partial(m.kv_append_q8, k, k, lens, new, start, start, table, cache),
+            "attn_decode_q8": partial(m.attn_decode_q8, normal(3, 3, 4, 64), cache, new, i32(np.zeros((3, 4))), 64)}
+
+
+@pytest.mark.parametrize("name", ["page_step", "rope", "kv_append", "kv_append_q8", "attn_decode_q8"])
+def test_other_threads_run_during_a_native_call(name):
+    """A row of calls with no Python code between them: another thread gets ahead only
+    where a call releases the interpreter's lock."""
+    call = _calls()[name]
+    assert call() is not None
+    ticks, stop = [], threading.Event()
+
+    def tick():
+        while not stop.is_set():
+            ticks.append(None)
+            time.sleep(0)
+
+    other = threading.Thread(target=tick)
+    interval = sys.getswitchinterval()
+    gc.disable()
+    sys.setswitchinterval(1e-5)
+    try:
+        other.start()
+        while not ticks:
+            time.sleep(0.001)
+        row = [ticks.__len__] + [call] * 1000 + [ticks.__len__]
+        got = list(map(operator.methodcaller("__call__"), row))
+    finally:
+        stop.set()
+        sys.setswitchinterval(interval)
+        gc.enable()
+        other.join()
+    torch.cuda.synchronize()
+    assert got[-1] > got[0]
