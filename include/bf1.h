@@ -379,7 +379,8 @@ int bf1_page_step(int32_t batch, const int32_t* seq_lens, const int32_t* new_len
  *   freqs     : [rot_dim / 2] double, radians per position
  *   Q_out, K_out : out_type: in_type, or bf16 of fp32; may be the inputs themselves
  *               (same type and strides), otherwise they overlap neither them nor each other
- *   strides   : HOST int64[12], in elements: batch, head, token of Q, Q_out, K, K_out
+ *   strides   : HOST int64[12], in elements: batch, head, token of Q, Q_out, K, K_out;
+ *               that of a dimension with one entry is not used
  * Angles are exact products, reduced to a part of a turn in double precision for any
  * position; cosine, sine and the turn are fp32, rounded once.  Even
  * head_dim <= 1024 and rot_dim; sixteen bytes at a time where strides, addresses and
@@ -395,7 +396,7 @@ int bf1_rope(const void* Q, const void* K, const int32_t* positions, int64_t pos
 /*
  * A step's keys and values into the bf16 cache of bf1_decode_attn.
  *   K, V  : rows [tokens, Hkv, head_dim] bf16, 16-byte aligned, strides of token and
- *           head in elements (multiples of 8)
+ *           head in elements (multiples of 8; that of a single row or head is not used)
  *   slots : [tokens] int64; a row whose slot is negative or past the cache is left
  *           out.  The slots of one call are distinct.
  *   K_pages, V_pages : [num_pages, Hkv, B, head_dim] bf16

@@ -610,6 +610,8 @@ __global__ __launch_bounds__((APPEND_THREADS<D, PW>)) void kv_append_q8_kernel(
     }
 }
 
+// A dimension's stride where it is used: one with a single entry may have any.
+int64_t used(int64_t stride, int64_t entries) { return entries > 1 ? stride : 0; }
 bool strides16(int64_t a, int64_t b) { return a >= 0 && b >= 0 && a % 8 == 0 && b % 8 == 0; }
 
 template <typename TI, typename TO>
@@ -716,11 +718,14 @@ int bf1_rope(const void* Q, const void* K, const int32_t* positions, int64_t pos
     if (Hq + (int64_t)Hkv > 65535) return BF1_ERR_UNSUPPORTED;
     const int64_t esize = in_type == BF1_TYPE_BF16 ? 2 : 4, osize = out_type == BF1_TYPE_BF16 ? 2 : 4;
     if (!bf1::aligned(positions, 4) || !bf1::aligned(freqs, 8)) return BF1_ERR_INVALID_ARG;
-    for (int i = 0; i < 12; ++i)
-        if (strides[i] < 0) return BF1_ERR_INVALID_ARG;
+    int64_t st[12];
+    for (int i = 0; i < 12; ++i) {
+        st[i] = bf1::used(strides[i], i % 3 == 0 ? batch : i % 3 == 2 ? n : i < 6 ? Hq : Hkv);
+        if (st[i] < 0) return BF1_ERR_INVALID_ARG;
+    }
     // every element is within reach of a 64-bit byte offset
     for (int i = 0; i < 12; i += 3)
-        if ((double)batch * strides[i] + (double)std::max(Hq, Hkv) * strides[i + 1] + (double)n * strides[i + 2] > 1e18)
+        if ((double)batch * st[i] + (double)std::max(Hq, Hkv) * st[i + 1] + (double)n * st[i + 2] > 1e18)
             return BF1_ERR_INVALID_ARG;
     // a side's output is read by no other lane: it is not the other side's input or output
     if (Hq > 0 && Hkv > 0 && (Q_out == K_out || Q_out == K || K_out == Q)) return BF1_ERR_INVALID_ARG;
@@ -736,13 +741,13 @@ int bf1_rope(const void* Q, const void* K, const int32_t* positions, int64_t pos
         if (in == out) {
             if (in_type != out_type) return BF1_ERR_INVALID_ARG;
             for (int i = 0; i < 3; ++i)
-                if (strides[6 * side + i] != strides[6 * side + 3 + i]) return BF1_ERR_INVALID_ARG;
+                if (st[6 * side + i] != st[6 * side + 3 + i]) return BF1_ERR_INVALID_ARG;
         }
         wide = wide && bf1::aligned(in, 16) && bf1::aligned(out, vec * osize);
-        for (int i = 0; i < 6; ++i) wide = wide && strides[6 * side + i] % vec == 0;
+        for (int i = 0; i < 6; ++i) wide = wide && st[6 * side + i] % vec == 0;
     }
-    const bf1::RopeSide q{Q, Q_out, strides[0], strides[1], strides[2], strides[3], strides[4], strides[5], Hq};
-    const bf1::RopeSide k{K, K_out, strides[6], strides[7], strides[8], strides[9], strides[10], strides[11], Hkv};
+    const bf1::RopeSide q{Q, Q_out, st[0], st[1], st[2], st[3], st[4], st[5], Hq};
+    const bf1::RopeSide k{K, K_out, st[6], st[7], st[8], st[9], st[10], st[11], Hkv};
     const float sign = transposed ? -1.f : 1.f;
     bool fits = false;
     hipStream_t s = (hipStream_t)stream;
@@ -771,6 +776,10 @@ int bf1_kv_append(const void* K, const void* V, int64_t k_token_stride, int64_t 
     if (!bf1::aligned(K, 16) || !bf1::aligned(V, 16) || !bf1::aligned(K_pages, 16) || !bf1::aligned(V_pages, 16) ||
         !bf1::aligned(slots, 8))
         return BF1_ERR_INVALID_ARG;
+    k_token_stride = bf1::used(k_token_stride, tokens);
+    v_token_stride = bf1::used(v_token_stride, tokens);
+    k_head_stride = bf1::used(k_head_stride, Hkv);
+    v_head_stride = bf1::used(v_head_stride, Hkv);
     if (!bf1::strides16(k_token_stride, k_head_stride) || !bf1::strides16(v_token_stride, v_head_stride))
         return BF1_ERR_INVALID_ARG;
     if (tokens >= (int64_t(1) << 31) || (double)tokens * Hkv * (head_dim / 8) >= 4294967296.0) return BF1_ERR_UNSUPPORTED;
@@ -801,6 +810,10 @@ int bf1_kv_append_q8(const void* K, const void* V, int64_t k_token_stride, int64
                           (const void*)block_start, (const void*)page_table, (const void*)K_scale,
                           (const void*)V_scale})
         if (!bf1::aligned(p, 4)) return BF1_ERR_INVALID_ARG;
+    k_token_stride = bf1::used(k_token_stride, tokens);
+    v_token_stride = bf1::used(v_token_stride, tokens);
+    k_head_stride = bf1::used(k_head_stride, Hkv);
+    v_head_stride = bf1::used(v_head_stride, Hkv);
     if (!bf1::strides16(k_token_stride, k_head_stride) || !bf1::strides16(v_token_stride, v_head_stride))
         return BF1_ERR_INVALID_ARG;
     if (tokens >= (int64_t(1) << 31) || Hkv > 65535 || batch > (1 << 22)) return BF1_ERR_UNSUPPORTED;

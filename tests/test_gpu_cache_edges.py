@@ -168,3 +168,26 @@ def test_other_threads_run_during_a_native_call(name):
         other.join()
     torch.cuda.synchronize()
     assert got[-1] > got[0]
+
+
+# ---- strides that nothing uses ---------------------------------------------------------------
+
+@pytest.mark.parametrize("shape,strides", [((1, 2, 64), (131, 64, 1)), ((5, 1, 64), (64, 33, 1)), ((1, 1, 128), (1, 7, 1))])
+def test_strides_of_a_single_row_or_head_are_not_used(shape, strides):
+    """One row, or one kv-head, whose stride is no multiple of what a load takes."""
+    T, Hkv, d = shape
+    x, y = normal(1, 2048), normal(2, 2048)
+    odd = [t.as_strided(shape, strides) for t in (x, y)]
+    even = [t.as_strided(shape, strides).clone(memory_format=torch.contiguous_format).view(shape) for t in (x, y)]
+    pos, freqs = i32(range(100, 100 + T)), torch.linspace(0.01, 1.0, d // 2, dtype=torch.float64, device="cuda")
+    got = []
+    for k, v in (odd, even):
+        pages = [normal(3, 2, Hkv, 64, d) for _ in range(2)]
+        bf1.kv_append(k, v, torch.arange(60, 60 + T, device="cuda"), *pages)
+        cache = bf1.cache_q8(2, 1, Hkv, d)
+        bf1.kv_append_q8(k, v, i32([64 - T]), i32([64]), i32([0, T]), i32([0, 1]), i32([[1]]), cache)
+        turned = bf1.rope(k, v, pos, freqs)
+        heads = bf1.rope(k.transpose(0, 1)[None], v.transpose(0, 1)[None], pos, freqs)
+        got.append([*pages, *cache, *turned, *heads])
+    for a, b in zip(*got):
+        assert torch.equal(a.contiguous().view(torch.uint8), b.contiguous().view(torch.uint8))
