@@ -429,6 +429,13 @@ int bf1_kv_append(const void* K, const void* V, int64_t k_token_stride, int64_t 
  * sequence's newest token go to its tail; tails of sequences without new tokens, and
  * all other pages, are left as they were.  Rows behind the last sequence are not read.
  * The pages that a step completes are distinct.
+ *
+ * The tail is state that a step consumes.  A step that begins inside a block and ends
+ * in a later one writes the later block's rows over the earlier one's, so the same step
+ * again (a pass before a capture, a retry) would quantise wrong rows, unless K_tail and
+ * V_tail are put back as they were before it; they are all that has to be.  Every
+ * other step can be repeated.  For the same reason tokens can be taken back (by
+ * smaller lengths) only as far as the first token of the newest block.
  */
 typedef enum { BF1_Q8_E4M3 = 0, BF1_Q8_INT8 = 1 } bf1_q8_format;
 

@@ -836,7 +836,12 @@ def kv_append_q8(k, v, lens_before, seq_lens, token_start, block_start, page_tab
     """Write a step's rows k, v [tokens, Hkv, d] bf16 into a CacheQ8: blocks that the
     step completes are quantised into their pages, the rows of each sequence's newest
     block go to its tail.  lens_before: the lengths page_step was given; seq_lens,
-    token_start and block_start: what it returned; page_table: what it updated."""
+    token_start and block_start: what it returned; page_table: what it updated.
+
+    A step that begins inside a block and ends in a later one overwrites the tail rows
+    that it quantised: to run it again (a warm-up before a capture, a retry), put
+    cache.k_tail and cache.v_tail back as they were first.  Other steps can be repeated
+    as they are.  Tokens can be taken back only as far as the newest block's first."""
     if stream is None:
         r = (_MARSHAL or _native()).kv_append_q8(k, v, lens_before, seq_lens, token_start, block_start, page_table, cache)
         if r is not None:

@@ -16,7 +16,7 @@ import torch
 
 import paper_2608_20427_amd as bf1
 from oracle import cache_oracle as co
-from test_gpu_cache import CODES, f64, i32, normal
+from test_gpu_cache import CODES, f64, filled_cache, i32, normal, plan_step
 
 pytestmark = pytest.mark.gpu
 
@@ -191,3 +191,40 @@ def test_strides_of_a_single_row_or_head_are_not_used(shape, strides):
         got.append([*pages, *cache, *turned, *heads])
     for a, b in zip(*got):
         assert torch.equal(a.contiguous().view(torch.uint8), b.contiguous().view(torch.uint8))
+
+
+# ---- kv_append_q8: what a repeated step needs ------------------------------------------------
+
+def _bytes(cache):
+    return [t.view(torch.uint8).clone() for t in cache]
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+@pytest.mark.parametrize("before,new", [(3, 20), (0, 64), (64, 200), (10, 54), (128, 1), (63, 1)])
+def test_append_q8_repeats_inside_a_block_or_from_its_start(fmt, before, new):
+    d, B, Hkv = 64, 64, 2
+    k, v = normal(1, new, Hkv, d), normal(2, new, Hkv, d)
+    cache = filled_cache(fmt, 6, 1, Hkv, d, B)
+    touched = (before + new - 1) // B - before // B + 1
+    args = (k, v, i32([before]), i32([before + new]), i32([0, new]), i32([0, touched]), i32([[4, 1, 0, 5, 2]]), cache)
+    bf1.kv_append_q8(*args)
+    once = _bytes(cache)
+    bf1.kv_append_q8(*args)
+    assert all(torch.equal(a, b) for a, b in zip(once, _bytes(cache)))
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+@pytest.mark.parametrize("before,new", [([50], [40]), ([63, 5, 100], [2, 300, 27]), ([20], [64])])
+def test_append_q8_repeats_across_blocks_with_its_tails_put_back(fmt, before, new):
+    d, B, Hkv = 64, 64, 2
+    k, v = normal(1, sum(new), Hkv, d), normal(2, sum(new), Hkv, d)
+    table, after, ts, bs, P = plan_step(before, new, B)
+    cache = filled_cache(fmt, P, len(before), Hkv, d, B)
+    tails = [t.clone() for t in cache[4:]]
+    args = (k, v, i32(before), i32(after), i32(ts), i32(bs), i32(table), cache)
+    bf1.kv_append_q8(*args)
+    once = _bytes(cache)
+    for t, x in zip(cache[4:], tails):
+        t.copy_(x)
+    bf1.kv_append_q8(*args)
+    assert all(torch.equal(a, b) for a, b in zip(once, _bytes(cache)))
