@@ -331,8 +331,10 @@ __global__ __launch_bounds__(THREADS) void rope_kernel(RopeSide q, RopeSide k, c
             for (int i = 0; i < P; ++i) {
                 constexpr int step = INTER ? 2 : 1, far = INTER ? 1 : P;
                 const float x0 = v[j][step * i], x1 = v[j][step * i + far];
-                y[step * i] = x0 * c[i] - x1 * s[i];
-                y[step * i + far] = x1 * c[i] + x0 * s[i];
+                // written out, so that every instance rounds the same way: a token's bits
+                // do not go by how many others the call has
+                y[step * i] = fmaf(x0, c[i], -(x1 * s[i]));
+                y[step * i + far] = fmaf(x1, c[i], x0 * s[i]);
             }
         } else {
 #pragma unroll

@@ -16,7 +16,8 @@ import torch
 
 import paper_2608_20427_amd as bf1
 from oracle import cache_oracle as co
-from test_gpu_cache import CODES, f64, filled_cache, i32, normal, plan_step
+from test_gpu_cache import (CODES, check_rope, decode_case, f64, filled_cache, host, i32, normal, plan_step,
+                            run_decode)
 
 pytestmark = pytest.mark.gpu
 
@@ -228,3 +229,43 @@ def test_append_q8_repeats_across_blocks_with_its_tails_put_back(fmt, before, ne
         t.copy_(x)
     bf1.kv_append_q8(*args)
     assert all(torch.equal(a, b) for a, b in zip(once, _bytes(cache)))
+
+
+# ---- rope: two heads per lane ----------------------------------------------------------------
+
+# the lanes of these calls own two heads each (256 workgroups and more with one), the last
+# of an odd number of heads one
+TWO_HEADS = [(1, 1700, 3, 2, 128, 128, torch.bfloat16), (1, 1200, 7, 0, 128, 128, torch.bfloat16),
+             (1, 1200, 3, 2, 128, 64, torch.bfloat16), (2, 500, 3, 2, 128, 128, torch.float32),
+             (1, 330, 2, 1, 80, 20, torch.bfloat16), (1, 800, 1, 2, 36, 12, torch.float32),
+             (3, 300, 4, 3, 64, 32, torch.float32)]
+
+
+@pytest.mark.parametrize("batch,n,Hq,Hkv,d,r,dtype", TWO_HEADS)
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_rope_two_heads_per_lane(batch, n, Hq, Hkv, d, r, dtype, interleaved):
+    """Against the oracle, and the same bits as calls on few tokens (a head per lane)."""
+    rng = np.random.default_rng(n)
+    freqs = list(1e6 ** (-np.arange(0, r, 2) / r))
+    pos = rng.integers(-5, 200000, (batch, n)).astype(np.int32)
+    q = normal(1, batch, Hq, n, d, dtype=dtype)
+    k = normal(2, batch, Hkv, n, d, dtype=dtype) if Hkv else None
+    f = torch.tensor(freqs, dtype=torch.float64, device="cuda")
+    for bwd, out in ((False, None), (True, None)) + (((True, torch.bfloat16),) if dtype is torch.float32 else ()):
+        big = check_rope(q, k, pos, freqs, interleaved, 1.139, bwd=bwd, dtype=out)
+        fn = bf1.rope_bwd if bwd else bf1.rope
+        for a in (0, n // 2, n - 17):
+            part = [None if x is None else x[:, :, a:a + 17] for x in (q, k)]
+            small = fn(*part, i32(pos[:, a:a + 17]), f, interleaved=interleaved, amplitude=1.139, dtype=out)
+            for x, y in zip(big, small):
+                assert x is None or torch.equal(x[:, :, a:a + 17], y)
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_rope_two_heads_per_lane_in_place(interleaved, dtype):
+    q, k, pos = normal(1, 1, 3, 1700, 128, dtype=dtype), normal(2, 1, 2, 1700, 128, dtype=dtype), i32(range(1700))
+    freqs, amp = bf1.rope_freqs(64, scaling="bands", factor=4.0)
+    a = bf1.rope(q, k, pos, freqs, interleaved, amp)
+    b = bf1.rope(q, k, pos, freqs, interleaved, amp, q_out=q, k_out=k)
+    assert b[0] is q and b[1] is k and torch.equal(a[0], q) and torch.equal(a[1], k)
