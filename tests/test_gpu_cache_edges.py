@@ -231,6 +231,40 @@ def test_append_q8_repeats_across_blocks_with_its_tails_put_back(fmt, before, ne
     assert all(torch.equal(a, b) for a, b in zip(once, _bytes(cache)))
 
 
+# ---- kv_append_q8: many sequences ------------------------------------------------------------
+
+@pytest.mark.parametrize("fmt,batch,active", [("int8", 256, 200), ("e4m3", 257, 257), ("int8", 513, 300),
+                                              ("e4m3", 3000, 900), ("int8", 66000, 150)])
+def test_append_q8_finds_its_sequence_among_many(fmt, batch, active):
+    """A block's sequence is searched 256 table entries at a time: one pass, two, and for
+    more than 65536 sequences three.  Places without rows, rows that complete a block or
+    none, blocks on both sides of every 256.  Against the oracle over the active places;
+    the others keep what they had."""
+    d, B = 64, 64
+    rng = np.random.default_rng(batch)
+    edges = [i for i in (0, 255, 256, 257, 511, 512, batch - 2, batch - 1) if i < batch]
+    at = np.unique(np.concatenate([edges, rng.permutation(batch)[:active]]))
+    before, new = np.zeros(batch, dtype=np.int64), np.zeros(batch, dtype=np.int64)
+    before[rng.random(batch) < 0.3] = 70  # also of places without rows
+    before[at] = rng.choice([0, 10, 63, 64, 127], len(at))
+    new[at] = rng.choice([1, 1, 54, 64, 65, 130], len(at))
+    new[edges], before[edges] = 1, 63  # each completes a block
+    table, after, ts, bs, P = plan_step(before, new, B)
+    T = int(ts[-1])
+    k, v = normal(1, T, 1, d), normal(2, T, 1, d)
+    cache = filled_cache(fmt, P, batch, 1, d, B)
+    first = cache._replace(k_tail=cache.k_tail[at], v_tail=cache.v_tail[at])
+    ref = co.append_q8(f64(k), f64(v), before[at], after[at], ts[:-1][at], table[at], host(first, fmt), fmt, B)
+    rest = torch.ones(batch, dtype=torch.bool)
+    rest[at] = False
+    old = [t[rest.cuda()] for t in cache[4:]]
+    bf1.kv_append_q8(k, v, i32(before), i32(after), i32(ts), i32(bs), i32(table), cache)
+    got = host(cache._replace(k_tail=cache.k_tail[at], v_tail=cache.v_tail[at]), fmt)
+    for n in got:
+        assert np.array_equal(got[n], ref[n]), n
+    assert all(torch.equal(t[rest.cuda()], x) for t, x in zip(cache[4:], old))
+
+
 # ---- rope: two heads per lane ----------------------------------------------------------------
 
 # the lanes of these calls own two heads each (256 workgroups and more with one), the last
@@ -269,3 +303,77 @@ def test_rope_two_heads_per_lane_in_place(interleaved, dtype):
     a = bf1.rope(q, k, pos, freqs, interleaved, amp)
     b = bf1.rope(q, k, pos, freqs, interleaved, amp, q_out=q, k_out=k)
     assert b[0] is q and b[1] is k and torch.equal(a[0], q) and torch.equal(a[1], k)
+
+
+# ---- guards around the buffers ---------------------------------------------------------------
+
+GUARD = 1 << 16
+
+
+def guarded(t):
+    """A copy of t between two guards; (copy, all of its memory)."""
+    raw = torch.full((2 * GUARD + t.numel() * t.element_size(),), 0xa5, dtype=torch.uint8, device="cuda")
+    inner = raw[GUARD:GUARD + t.numel() * t.element_size()].view(t.dtype).view(t.shape)
+    inner.copy_(t)
+    return inner, raw
+
+
+def untouched(raw):
+    return bool((raw[:GUARD] == 0xa5).all()) and bool((raw[-GUARD:] == 0xa5).all())
+
+
+FOREIGN = [([0], [64], [0, 64], [0, 1], [[6]]), ([0], [64], [0, 64], [0, 1], [[-1]]), ([0], [64], [0, 64], [0, 1], [[7]]),
+           ([0], [128], [1000, 64], [0, 2], [[0, 1]]), ([0], [64], [-70, 64], [0, 1], [[2]]),
+           ([5], [-5], [0, 64], [0, 1], [[0]]), ([0, 0], [64, 64], [0, 64, 128], [5, 2, 1], [[0], [1]]),
+           ([0], [2 ** 31 - 1], [0, 64], [0, 2 ** 31 - 1], [[1]]), ([-9], [64], [0, 64], [-4, 1], [[3]]),
+           ([30, 0], [70, 64], [0, 40, 64], [0, 2, 3], [[6, 4], [5, 6]])]
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+@pytest.mark.parametrize("case", range(len(FOREIGN)))
+def test_append_q8_foreign_tables_change_nothing_else(fmt, case):
+    """Six pages; tables that name others, rows past the tensors, sums that are none.
+    Around every buffer nothing is written, pages that no table names keep codes and
+    scales, and a row of a tail keeps what it held or takes the row that the tables
+    give it."""
+    before, after, ts, bs, table = FOREIGN[case]
+    B, d, Hkv, P, T = 64, 64, 2, 6, 64
+    k, v = normal(1, T, Hkv, d), normal(2, T, Hkv, d)
+    old = filled_cache(fmt, P, len(before), Hkv, d, B)
+    both = [guarded(t) for t in old]
+    cache = bf1.CacheQ8(*(t for t, _ in both))
+    bf1.kv_append_q8(k, v, i32(before), i32(after), i32(ts), i32(bs), i32(table), cache)
+    assert all(untouched(raw) for _, raw in both)
+    named = {p for r in table for p in r if 0 <= p < P}
+    for p in set(range(P)) - named:
+        for x, y in zip(old[:4], cache[:4]):
+            assert torch.equal(x[p].view(torch.uint8), y[p].view(torch.uint8))
+    for x, was, now in ((k, old.k_tail, cache.k_tail), (v, old.v_tail, cache.v_tail)):
+        for b in range(len(before)):
+            start = max(before[b], 0)
+            end = max(after[b], start)
+            last = (end - 1) // B * B
+            for r in range(B):
+                row = ts[b] + last + r - start
+                given = start <= last + r < end and 0 <= row < T
+                assert torch.equal(now[b, :, r], was[b, :, r]) or (given and torch.equal(now[b, :, r], x[row]))
+
+
+@pytest.mark.parametrize("lens,splits", [([200, 70], False), ([9000, 70], True)])
+def test_decode_q8_without_an_lse(lens, splits):
+    """O alone, with one split and with several, between guards: the same bits, and
+    nothing beside them or behind the workspace."""
+    q, cache, table = decode_case("int8", lens, 4, 2, 64, 64, 2, True, 9)
+    (want, _), plan = run_decode(q, cache, table, lens, 64, 2, True)
+    need = bf1.decode_q8_workspace_size(2, 4, 2, 64, 64, plan.shape[1])
+    assert (need > 0) == splits
+    o, o_raw = guarded(torch.zeros_like(want))
+    ws, ws_raw = guarded(torch.zeros(need, dtype=torch.uint8, device="cuda"))
+    lens = i32(lens)
+    status = bf1.load().bf1_decode_attn_q8(
+        q.data_ptr(), *(t.data_ptr() for t in cache), lens.data_ptr(), cache.k_pages.shape[0], plan.data_ptr(),
+        plan.shape[1], o.data_ptr(), None, 2, 4, 2, 64, 64, 1, ws.data_ptr() if need else None, need,
+        torch.cuda.current_stream().cuda_stream)
+    assert status == bf1.BF1_OK
+    torch.cuda.synchronize()
+    assert torch.equal(o, want) and untouched(o_raw) and untouched(ws_raw)
