@@ -70,9 +70,10 @@ __device__ __forceinline__ uint32_t group_scan(uint32_t x, uint32_t* part, uint3
 // writes the table entry, and no row reads an entry that this launch writes.
 //
 // Bound by latency: 20 bytes per sequence and 12 per row.  Every workgroup sums the
-// batch for itself (SEQS sequences at a time), so that one launch does it.  32 sequences
-// of a row each 4.4 us, 48 of 84K rows 4.6, 2000 of a row 7.5 (two rounds); an empty
-// kernel takes 2.2.  Four rows per thread and scans through LDS moves: 5.4 and 8.4.
+// batch for itself (SEQS sequences at a time), so that one launch does it.  Replays of a
+// graph: 32 sequences of a row each 4.3 us, 48 of 84K rows 4.6, 2000 of a row 7.5 (two
+// rounds); an empty kernel takes 2.2.  Four rows per thread and scans through LDS moves:
+// 5.4 and 8.4 for the first and the last.
 constexpr int SPT = 4;                   // sequences per thread and round
 constexpr int SEQS = THREADS * SPT;
 constexpr int ROWS_PER_GROUP = THREADS;  // a row per thread
@@ -208,13 +209,14 @@ __global__ __launch_bounds__(THREADS) void page_step_kernel(
 // fp32 part and turned by what that leaves, so that fp32 holds them to the function's
 // own few ulp.  With one 64-bit product each and no turn back they were up to 3.8e-7 off
 // at positions of 2^31 (2-norm of the error of float32 gradients, positions below 8191:
-// 3.4e-8, now 2.8e-8), in the same time: 32768 rows of 24 heads of 128 81.3 us, now
-// 80.3; those gradients 14.1 and 14.1.
+// 3.4e-8, now 2.7e-8), in the same time: 32768 rows of 24 heads of 128 81.3 us, now
+// 80.6; those gradients 14.1 and 14.4.
 //
 // A lane owns P pairs of one token, 16 bytes of each half of the head, in HB heads.
 // Workgroups follow each other over the heads of the same tokens, so that rows of joined
-// projections are read where they lie: 32768 rows, 16 + 8 heads of 128, 83 us (403 MB,
-// 4.8 TB/s; a large copy reaches 5.0), 93 with the heads' workgroups far apart.
+// projections are read where they lie: 32768 rows, 16 + 8 heads of 128, 80.6 us a call
+// (403 MB, 5.0 TB/s; a large copy reaches 5.1), 10 us more with the heads' workgroups far
+// apart.
 struct RopeSide {
     const void* in;
     void* out;
@@ -350,8 +352,8 @@ __global__ __launch_bounds__(THREADS) void rope_kernel(RopeSide q, RopeSide k, c
 // Rows into bf16 pages
 // ---------------------------------------------------------------------------
 // One lane per 16 bytes of a row of K and of V; a row without a slot is left out.  Bound
-// by memory: 16294 rows of 8 heads of 128 27 us for 134 MB (4.9 TB/s; a large copy reaches
-// 5.1).
+// by memory: 16294 rows of 8 heads of 128 27.3 us for 134 MB (4.9 TB/s; a large copy
+// reaches 5.1).
 __global__ __launch_bounds__(THREADS) void kv_append_kernel(
     const __bf16* __restrict__ k, const __bf16* __restrict__ v, int64_t kt, int64_t kh, int64_t vt, int64_t vh,
     const int64_t* __restrict__ slots, __bf16* __restrict__ k_pages, __bf16* __restrict__ v_pages, int64_t items,
@@ -389,8 +391,9 @@ __global__ __launch_bounds__(THREADS) void kv_append_kernel(
 // read it.  Neighbouring workgroups take the heads of the same rows.
 //
 // Bound by memory, a block's load, scale and code behind each other: 36585 rows of 8 heads
-// of 128 49 us (e4m3) and 51 (int8) for 225 MB (4.6 and 4.4 TB/s).  A row each for 64
-// sequences 5.4 us: where the sequence is, its lengths, its rows, one after the other.
+// of 128 49 us (e4m3) and 51 (int8) for 225 MB (4.6 and 4.4 TB/s); with heads of 64 31.6
+// (int8) for 112 MB: half the bytes of a workgroup behind the same chain.  A row each for
+// 64 sequences 5.4 us: where the sequence is, its lengths, its rows, one after the other.
 struct QuantE4m3 {
     static constexpr bool INT8 = false;
 };
@@ -626,8 +629,9 @@ hipError_t launch_rope(const RopeSide& q, const RopeSide& k, const int32_t* posi
     const int64_t groups = (rows * lanes + THREADS - 1) / THREADS;
     const int32_t heads = q.heads + k.heads;
     // Two heads per lane share its cosines and sines; one where that leaves compute units
-    // without a workgroup.  us, one / two / four: 32 rows of 24 heads of 128 3.2 / 3.6 /
-    // 4.1, 4096 14.2 / 12.7 / 11.7, 32768 107 / 84 / 88.
+    // without a workgroup.  us in replays of a graph, one / two / four: 32 rows of 24 heads
+    // of 128 3.3 / 3.7 / 4.3, 512 4.5 / 4.2 / 4.7, 4096 16.9 / 13.2 / 12.1, 32768 118 / 85 /
+    // 87.
     const int32_t hb = groups * heads < 256 ? 1 : 2;
     const int32_t hsplit = (heads + hb - 1) / hb;
     *fits = rows * lanes < (int64_t(1) << 31) && launchable(groups * hsplit);

@@ -16,10 +16,11 @@
 // instructions and the scales multiply fp32 numbers: the scores' sums, and the
 // weights before they are split in three bf16 parts (all 24 bits of them).
 //
-// Bound by memory (the vector unit is busy a fifth of a long list's time): one dense
-// list of 64K, 16/8 heads of 128 27.0 us with its merge for 134 MB, 12 ragged ones of up to
-// 32K with groups of 8 60 us for 293 MB, 32 sequences of 64K on the BF1 route 12.6 us for 51
-// MB (the bf16 decode 19.6 for 101), one sequence 8.1 us: 4.7 for a launch and a single
+// Bound by memory (the vector unit is busy a fifth of a long list's time).  Replays of a
+// graph: one dense list of 64K, 16/8 heads of 128 26.7 us with its merge for 134 MB, 12
+// ragged ones of up to 32K with groups of 8, int8 in pages of 128, 64.5 us with theirs
+// for 293 MB, 32 sequences of 64K on the BF1 route 12.2 us for 51 MB, partly cached (the
+// bf16 decode of 32 full ones 21.2), one sequence 8.2 us: 4.8 for a launch and a single
 // unit, the rest what one compute unit takes to fetch eleven.
 #include <hip/hip_runtime.h>
 #include <float.h>
@@ -543,8 +544,12 @@ hipError_t launch_d(const Args& a, int32_t G, int32_t B, hipStream_t st) {
 // of 512 units 218 / 60 / 56; 64 rows of 512 (heads of 64) 129 / 41 / 41.
 //
 // Shorter lists: at most 256 workgroups, and a list is cut only where that saves three
-// rounds.  A round takes some 1.5 us, the merge 2 to 3 and a launch more.  us, uncut /
-// cut: 12 units, 8 rows 8.1 / 7.7, 160 rows 11.7 / 12.6; 33 units, 8 rows 17.5 / 8.5.
+// rounds.  A round takes some 1.5 us, the merge 2 to 3, and from the host its launch 3.8
+// more: the rule is for calls from the host.  In replays of a graph, where no launch
+// costs that, cutting would win a little for few rows: us, uncut / cut, 12 units, 8 rows 8.2
+// / 7.9, 64 rows 9.7 / 8.6, 128 rows of groups of 8 10.7 / 11.5, 256 rows not cut; 33 units, 8
+// rows 17.5 / 8.5 (cut).  One sequence is then behind the bf16 decode, which spreads it over
+// more compute units (7.3 for twice the bytes).
 //
 // More than 32 splits cost the merge more than they save: 256 units, 2 rows 16 for 14.
 constexpr int64_t PLACES = 256, MANY_ROWS = 2048;
