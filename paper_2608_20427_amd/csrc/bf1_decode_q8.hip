@@ -193,9 +193,10 @@ __global__ __launch_bounds__(THREADS, 3) void decode_q8_kernel(
     // the third; nothing reads them), and groups of 8 the first two; the third is a product
     // of its own there, added to the columns of the first.  With two parts an output that
     // is a small difference of large weights lost bits, and 12 dense lists of 32K were 1.2e-4
-    // (2-norm, mostly bf16 steps) from the same in fp32, 6.6e-5 with three; us, two / three:
-    // those lists, groups of 8, 70.6 / 71.5, 32 sequences of 64K on the BF1 route 11.65 /
-    // 11.71, one sequence 8.06 / 8.20.
+    // (2-norm, bf16 steps) from a form in fp32 throughout; with three 7e-5, most of it that
+    // form's: 19 of 49152 outputs differ from the rounded 64-bit result, 84 of its own.  us,
+    // two / three: those lists, groups of 8, 70.6 / 71.5, 32 sequences of 64K on the BF1
+    // route 11.65 / 11.71, one sequence 8.06 / 8.20.
     constexpr bool OWN3 = 3 * G > 16;
     constexpr uint32_t FIRST = 0xffff0000u, TWO = 0xffffff00u;  // where a weight holds them
     const uint32_t upto = OWN3 || col < 2 * G ? TWO : ~0u, from = col < G ? 0 : OWN3 || col < 2 * G ? FIRST : TWO;
