@@ -464,6 +464,140 @@ int bf1_decode_attn_q8(const void* Q, const void* K_pages, const void* V_pages, 
                        int64_t workspace_bytes, void* stream);
 
 /*
+ * RMSNorm of every head of queries and keys with the rotary positions in the same pass,
+ * and its gradient.  For a head's row x of head_dim elements, r = (mean x^2 + eps)^-1/2:
+ *     forward   y = turn(x r gain)                 turn as bf1_rope's, with `amplitude`
+ *     gradient  dn = the transposed turn of dy, u = dn gain,
+ *               dx = r (u - x r mean(u x r)),  dgain = sum over rows of dn x r
+ * Sums, the norm and the turn are fp32 (squares too: a row's elements lie below 2^60),
+ * results are rounded once.
+ *   Q, K, positions, freqs, Q_out, K_out, interleaved, amplitude: as bf1_rope's; outputs
+ *               may have any strides that write no element twice
+ *   q_gain, k_gain : [head_dim] of gain_type, shared by the heads of a side; NULL: ones
+ *   dQ, dK    : gradients of the outputs, of grad_type: fp32, or bf16 with bf16 Q and K
+ *   dQ_in, dK_in : gradients of Q and K, of out_type, any type; may be dQ and dK, or Q and
+ *               K, where type and strides are the same
+ *   dq_gain, dk_gain : [head_dim] fp32, the sums over batch, heads and tokens; either may
+ *               be NULL.  The order of the sums goes by the sizes alone: deterministic
+ *   strides   : HOST int64, in elements: forward [12] as bf1_rope's; gradient [18]: batch,
+ *               head, token of dQ, Q, dQ_in, dK, K, dK_in
+ *   workspace : at least bf1_qk_norm_rope_bwd_workspace_size() bytes, 16-byte aligned; none
+ *               where that is 0, or without dq_gain and dk_gain
+ * eps > 0; even head_dim <= 512 and rot_dim.  Sixteen bytes at a time where strides,
+ * addresses and the two parts of a head allow it, element by element otherwise, with the
+ * same bits.
+ */
+int bf1_qk_norm_rope(const void* Q, const void* K, const void* q_gain, const void* k_gain, int32_t gain_type,
+                     const int32_t* positions, int64_t positions_batch_stride, const double* freqs, void* Q_out,
+                     void* K_out, int32_t batch, int64_t n, int32_t Hq, int32_t Hkv, int32_t head_dim, int32_t rot_dim,
+                     int32_t in_type, int32_t out_type, int32_t interleaved, float eps, float amplitude,
+                     const int64_t* strides, void* stream);
+int bf1_qk_norm_rope_bwd_workspace_size(int32_t batch, int64_t n, int32_t Hq, int32_t Hkv, int32_t head_dim,
+                                        int32_t rot_dim, int32_t in_type, int64_t* bytes);
+int bf1_qk_norm_rope_bwd(const void* dQ, const void* dK, int32_t grad_type, const void* Q, const void* K,
+                         const void* q_gain, const void* k_gain, int32_t gain_type, const int32_t* positions,
+                         int64_t positions_batch_stride, const double* freqs, void* dQ_in, void* dK_in, float* dq_gain,
+                         float* dk_gain, int32_t batch, int64_t n, int32_t Hq, int32_t Hkv, int32_t head_dim,
+                         int32_t rot_dim, int32_t in_type, int32_t out_type, int32_t interleaved, float eps,
+                         float amplitude, const int64_t* strides, void* workspace, int64_t workspace_bytes, void* stream);
+
+/*
+ * Drafted tokens over the bf16 cache.  Behind sequence b, which holds seq_lens_before[b]
+ * tokens, lies a tree of up to 64 drafted nodes, its rows packed as bf1_page_step's:
+ * rows token_start[b] .. token_start[b + 1] - 1.  Node i follows an earlier node, or the
+ * newest token.  Its position is the length plus its depth; bf1_page_step (with the
+ * nodes as new tokens) and bf1_kv_append put its key and value at the length plus i.
+ *
+ * bf1_tree_step: masks and positions, in one launch.
+ *   parents   : [rows] int32, the parent's number in its own tree; a number that is not
+ *               an earlier node's means none (the node follows the newest token)
+ *   seq_lens  : [batch] int32, the lengths with the drafted tokens (bf1_page_step's): nodes
+ *               past them have no place
+ *   masks     : [rows] int64, bit k of a row: node k is the node or one before it
+ *   positions : [rows] int32, for bf1_rope or bf1_qk_norm_rope, too
+ * Rows behind the last tree, of nodes without a place and past the 64th: mask 0, position -1.
+ *
+ * bf1_attn_tree: attention of all nodes, one kernel, or two with workspace.  The node at
+ * position p, block j = p / B, reads the committed keys of the blocks of P(j) (Eq. 1; with
+ * `dense` of every block up to j) and the drafted keys of its mask (where L = 0 keeps block
+ * j from reading block j - 1, only those in block j).  A chain of nodes reads what its tokens
+ * would read one after the other.
+ *   Q, O      : [rows, Hq, head_dim] bf16, packed; LSE [rows, Hq] fp32, may be NULL
+ *   masks     : any; bits of nodes without a place do nothing
+ *   K_pages, V_pages, page_table : bf1_decode_attn's and bf1_decode_plan's
+ *   max_nodes : largest tree of the call, at most 64
+ * A row whose position is not within 64 from its sequence's length on (also -1), whose
+ * number is max_nodes or more, or whose sequence lacks a page that some node of it reads,
+ * gets NaN; a row that reads nothing 0 and LSE -infinity.  Rows behind the last tree are
+ * left as they are.  What a row does not read does nothing, whatever it holds.  Weights
+ * are applied with 16 bits, sums are fp32; deterministic.  head_dim and B in {64, 128},
+ * Hq / Hkv in {1, 2, 4, 8}, L <= 32.
+ */
+int bf1_tree_step(const int32_t* parents, const int32_t* token_start, const int32_t* seq_lens_before,
+                  const int32_t* seq_lens, int32_t batch, int64_t rows, int64_t* masks, int32_t* positions, void* stream);
+int bf1_attn_tree_workspace_size(int32_t batch, int32_t max_nodes, int32_t Hq, int32_t Hkv, int32_t head_dim, int32_t B,
+                                 int32_t max_pages_per_seq, int32_t L, int32_t dense, int64_t* bytes);
+int bf1_attn_tree(const void* Q, const void* K_pages, const void* V_pages, const int64_t* masks, const int32_t* positions,
+                  const int32_t* seq_lens_before, const int32_t* token_start, const int32_t* page_table,
+                  int32_t max_pages_per_seq, int32_t num_pages, void* O, float* LSE, int32_t batch, int64_t rows,
+                  int32_t max_nodes, int32_t Hq, int32_t Hkv, int32_t head_dim, int32_t B, int32_t L, int32_t dense,
+                  void* workspace, int64_t workspace_bytes, void* stream);
+
+/*
+ * The accepted nodes' rows of one layer's cache move together: node accepted[b, k] of
+ * sequence b goes to position seq_lens_before[b] + k.
+ *   accepted     : [batch, accepted_width <= 64] int32: numbers of a path, ascending; the
+ *                  first one that is not above the one before it, or is no node's, ends it
+ *   seq_lens     : the lengths with the drafted tokens
+ *   seq_lens_out : [batch] int32, seq_lens_before plus the nodes accepted; neither input
+ * Rows may lie where others go.  A row from or to a page that is none is left out.  The
+ * same call again moves other rows: seq_lens_out is for the step's next.
+ */
+int bf1_kv_compact(void* K_pages, void* V_pages, const int32_t* accepted, int32_t accepted_width,
+                   const int32_t* seq_lens_before, const int32_t* seq_lens, const int32_t* page_table, int32_t batch,
+                   int32_t max_pages_per_seq, int32_t num_pages, int32_t Hkv, int32_t head_dim, int32_t B,
+                   int32_t* seq_lens_out, void* stream);
+
+/*
+ * Pages held by several sequences.  bf1_page_fork: every place b of the batch goes on with
+ * the first keep_lens[b] tokens of the sequence that place sources[b] holds (none where
+ * sources[b] is no place): forks, beams that change places, tokens taken back, ends.
+ *   seq_lens, sources, keep_lens : [batch] int32; keep_lens below 0 counts as 0 and past the
+ *                    source's length as that
+ *   page_table     : [batch, max_pages_per_seq] int32, read; page_table_out gets the new one,
+ *                    -1 behind each sequence's last block
+ *   shares         : [num_pages] int32, updated: holders of a page beyond the first, 0 or more
+ *                    (bf1_page_step's pages have one holder).  A caller that holds pages
+ *                    itself, as a cache of prefixes does, adds 1 to theirs
+ *   free_pages     : [num_free] int32, updated: bf1_page_step's list, with room for every page.
+ *                    Pages that nobody holds any more are put back below the head, ascending
+ *   free_head, free_head_out : [1] int32; may be the same
+ *   seq_lens_out   : [batch] int32; neither of the three inputs
+ *   copy_from, copy_to, copy_rows : [batch] int32, distinct buffers: see below
+ * Full blocks are shared.  A block that goes on being written has one holder: the first
+ * place that continues it keeps its page, if no other sequence and no caller holds that;
+ * for the others it is to be copied, the first copy_rows[b] tokens of page copy_from[b] to
+ * the new page copy_to[b] (-1, -1 and 0 where nothing is).  bf1_kv_copy does it, for each
+ * layer's cache.  Without a free page the sequence goes on without that block's tokens:
+ * the caller sees it in seq_lens_out.
+ * Table entries outside [0, num_pages) are no pages; they are taken over as they are.
+ * shares and free_pages are state that the call consumes: to run it again (a pass before a
+ * capture, a retry), put them back first.  Two kernels; deterministic.  B in {64, 128}.
+ *
+ * bf1_kv_copy: rows 0 .. copy_rows[i] - 1 (B at most) of K and V page copy_from[i] to page
+ * copy_to[i], all heads, for i < count; entries outside the cache are left out.  No page is
+ * copied to twice, or both to and from.  The tails of the 8-bit cache are such pages, too
+ * (num_pages = batch).
+ */
+int bf1_page_fork(int32_t batch, const int32_t* seq_lens, const int32_t* sources, const int32_t* keep_lens,
+                  const int32_t* page_table, int32_t max_pages_per_seq, int32_t* shares, int32_t num_pages,
+                  int32_t* free_pages, int32_t num_free, const int32_t* free_head, int32_t B, int32_t* page_table_out,
+                  int32_t* seq_lens_out, int32_t* free_head_out, int32_t* copy_from, int32_t* copy_to, int32_t* copy_rows,
+                  void* stream);
+int bf1_kv_copy(void* K_pages, void* V_pages, const int32_t* copy_from, const int32_t* copy_to, const int32_t* copy_rows,
+                int32_t count, int32_t num_pages, int32_t Hkv, int32_t head_dim, int32_t B, void* stream);
+
+/*
  * Key split of the forward kernels (bf1_attn_fwd, bf1_attn_fwd_noalloc,
  * bf1_attn_fwd_csr, bf1_dense_causal_fwd), process-wide:
  *   0  automatic (the default): when a launch has at most one work item (one

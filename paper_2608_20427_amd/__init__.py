@@ -25,6 +25,8 @@ __all__ = [
     "set_forward_key_split",
     "PageStep", "page_step", "rope_freqs", "rope", "rope_bwd", "kv_append", "CacheQ8", "cache_q8", "kv_append_q8",
     "decode_q8_workspace_size", "attn_decode_q8",
+    "qk_norm_rope", "qk_norm_rope_bwd_workspace_size", "qk_norm_rope_bwd", "tree_step", "attn_tree_workspace_size",
+    "attn_tree", "kv_compact", "PageFork", "page_fork", "kv_copy",
 ]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -128,6 +130,28 @@ def load():
     lib.bf1_decode_attn_q8.restype = ctypes.c_int
     lib.bf1_decode_attn_q8.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, i32, vp, i32, vp, vp, i32, i32, i32, i32, i32,
                                        i32, vp, i64, vp]
+    pi64 = ctypes.POINTER(i64)
+    lib.bf1_qk_norm_rope.restype = ctypes.c_int
+    lib.bf1_qk_norm_rope.argtypes = [vp, vp, vp, vp, i32, vp, i64, vp, vp, vp, i32, i64, i32, i32, i32, i32, i32, i32, i32,
+                                     f32, f32, pi64, vp]
+    lib.bf1_qk_norm_rope_bwd_workspace_size.restype = ctypes.c_int
+    lib.bf1_qk_norm_rope_bwd_workspace_size.argtypes = [i32, i64, i32, i32, i32, i32, i32, pi64]
+    lib.bf1_qk_norm_rope_bwd.restype = ctypes.c_int
+    lib.bf1_qk_norm_rope_bwd.argtypes = [vp, vp, i32, vp, vp, vp, vp, i32, vp, i64, vp, vp, vp, vp, vp, i32, i64, i32, i32,
+                                         i32, i32, i32, i32, i32, f32, f32, pi64, vp, i64, vp]
+    lib.bf1_tree_step.restype = ctypes.c_int
+    lib.bf1_tree_step.argtypes = [vp, vp, vp, vp, i32, i64, vp, vp, vp]
+    lib.bf1_attn_tree_workspace_size.restype = ctypes.c_int
+    lib.bf1_attn_tree_workspace_size.argtypes = [i32, i32, i32, i32, i32, i32, i32, i32, i32, pi64]
+    lib.bf1_attn_tree.restype = ctypes.c_int
+    lib.bf1_attn_tree.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, i32, i32, vp, vp, i32, i64, i32, i32, i32, i32, i32, i32,
+                                  i32, vp, i64, vp]
+    lib.bf1_kv_compact.restype = ctypes.c_int
+    lib.bf1_kv_compact.argtypes = [vp, vp, vp, i32, vp, vp, vp, i32, i32, i32, i32, i32, i32, vp, vp]
+    lib.bf1_page_fork.restype = ctypes.c_int
+    lib.bf1_page_fork.argtypes = [i32, vp, vp, vp, vp, i32, vp, i32, vp, i32, vp, i32, vp, vp, vp, vp, vp, vp, vp]
+    lib.bf1_kv_copy.restype = ctypes.c_int
+    lib.bf1_kv_copy.argtypes = [vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, vp]
     _LIB = lib
     return lib
 
@@ -912,3 +936,353 @@ def attn_decode_q8(q, cache, seq_lens, plan, B=64, out=None, lse=None, workspace
           ks.data_ptr(), vs.data_ptr(), kt.data_ptr(), vt.data_ptr(), seq_lens.data_ptr(), num_pages, plan.data_ptr(),
           stride, out.data_ptr(), lse.data_ptr(), batch, Hq, Hkv, d, int(B), fmt, _ptr(workspace), ws_bytes)
     return out, lse
+
+
+# ---- norms of queries and keys with their rotary positions -----------------------
+
+def _strided(t, name, shape, dtype, dev):
+    """Raise ValueError unless `t` is a tensor of `shape` and `dtype` on `dev` with the
+    elements of a head side by side; returns its strides over batch, heads and tokens."""
+    import torch
+    if not isinstance(t, torch.Tensor) or t.device != dev or t.dtype != dtype or t.shape != shape:
+        raise ValueError(f"{name} must be a {dtype} tensor of shape {tuple(shape)} on {dev}")
+    s = t.stride()
+    if s[-1] != 1 and shape[-1] > 1:
+        raise ValueError(f"{name} must have the elements of a head side by side")
+    return (0, s[1], s[0]) if len(shape) == 3 else s[:3]
+
+
+def _norm_rope_sides(q, k, q_gain, k_gain, positions, freqs):
+    """Check what forward and gradient have in common; returns (device, type, gains' type,
+    sizes)."""
+    import torch
+    x = q if q is not None else k
+    if x is None:
+        raise ValueError("qk_norm_rope needs q or k")
+    dev = _cuda_device(x, "q" if q is not None else "k")
+    dim = x.dim()
+    if dim not in (3, 4) or x.dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError("q and k must be bf16 or float32, [batch, heads, n, d] or rows [tokens, heads, d]")
+    d = x.shape[-1]
+    batch, n = lead = (1, x.shape[0]) if dim == 3 else (x.shape[0], x.shape[2])
+    heads = []
+    for name, t in (("q", q), ("k", k)):
+        if t is None:
+            heads.append(0)
+            continue
+        if not isinstance(t, torch.Tensor) or t.dim() != dim or t.shape[-1] != d \
+                or ((1, t.shape[0]) if dim == 3 else (t.shape[0], t.shape[2])) != lead:
+            raise ValueError(f"{name} must agree with the other operand in every size but the heads")
+        heads.append(t.shape[1])
+    gains = [g for g in (q_gain, k_gain) if g is not None]
+    gtype = torch.float32
+    if gains:
+        gtype = getattr(gains[0], "dtype", None)
+        if gtype not in (torch.bfloat16, torch.float32):
+            raise ValueError("gains must be bf16 or float32 tensors")
+        for name, g in (("q_gain", q_gain), ("k_gain", k_gain)):
+            if g is not None:
+                check_buffer(g, name, (d,), gtype, dev)
+    if not isinstance(positions, torch.Tensor) or (positions.shape != (n,) and (dim == 3 or positions.shape != lead)):
+        raise ValueError(f"positions must have shape ({n},)" + (f" or ({batch}, {n})" if dim == 4 else ""))
+    check_buffer(positions, "positions", positions.shape, torch.int32, dev)
+    if not isinstance(freqs, torch.Tensor) or freqs.dim() != 1 or not 1 <= freqs.shape[0] <= d // 2:
+        raise ValueError("freqs must be a 1-D tensor of at most d / 2 entries")
+    check_buffer(freqs, "freqs", freqs.shape, torch.float64, dev)
+    return dev, x.dtype, gtype, (batch, n, *heads, d)
+
+
+def _type(dtype):
+    import torch
+    return 0 if dtype is torch.bfloat16 else 1
+
+
+def qk_norm_rope(q, k, q_gain, k_gain, positions, freqs, eps=1e-6, interleaved=False, amplitude=1.0, q_out=None,
+                 k_out=None, dtype=None, stream=None):
+    """RMSNorm of every head of queries and keys, times q_gain and k_gain [d] (bf16 or
+    float32; None: ones), and rope in one launch; returns (q_out, k_out).
+
+    q, k, positions, freqs, interleaved and amplitude as rope's; either of q, k may be
+    None.  Outputs are contiguous tensors of the inputs' shapes, or q_out and k_out: any
+    strides with the elements of a head side by side, the inputs themselves among them.
+    dtype=torch.bfloat16 rounds float32 inputs on the way."""
+    if stream is None and q_out is None and k_out is None and dtype is None:
+        r = (_MARSHAL or _native()).qk_norm_rope(q, k, q_gain, k_gain, positions, freqs, eps, interleaved, amplitude)
+        if r is not None:
+            return _done(r, "bf1_qk_norm_rope")
+    dev, xtype, gtype, (batch, n, Hq, Hkv, d) = _norm_rope_sides(q, k, q_gain, k_gain, positions, freqs)
+    dtype = xtype if dtype is None else dtype
+    strides, outs = [], []
+    for name, x, out in (("q", q, q_out), ("k", k, k_out)):
+        if x is None:
+            strides += [0] * 6
+            outs.append(None)
+            continue
+        strides += _strided(x, name, x.shape, xtype, dev)
+        out = _empty(x.shape, dtype, dev, stream) if out is None else out
+        strides += _strided(out, name + "_out", x.shape, dtype, dev)
+        outs.append(out)
+    _call(load().bf1_qk_norm_rope, "bf1_qk_norm_rope", dev, stream, _ptr(q), _ptr(k), _ptr(q_gain), _ptr(k_gain),
+          _type(gtype), _ptr(positions), n if positions.dim() == 2 else 0, _ptr(freqs), _ptr(outs[0]), _ptr(outs[1]), batch,
+          n, Hq, Hkv, d, 2 * freqs.shape[0], _type(xtype), _type(dtype), int(bool(interleaved)), float(eps),
+          float(amplitude), (ctypes.c_int64 * 12)(*strides))
+    return tuple(outs)
+
+
+def qk_norm_rope_bwd_workspace_size(batch, n, Hq, Hkv, d, rot_dim, dtype):
+    """Bytes of workspace of qk_norm_rope_bwd; dtype: q's and k's."""
+    out = ctypes.c_int64(0)
+    _check(load().bf1_qk_norm_rope_bwd_workspace_size(int(batch), int(n), int(Hq), int(Hkv), int(d), int(rot_dim),
+                                                      _type(dtype), ctypes.byref(out)), "bf1_qk_norm_rope_bwd_workspace_size")
+    return out.value
+
+
+def qk_norm_rope_bwd(dq, dk, q, k, q_gain, k_gain, positions, freqs, eps=1e-6, interleaved=False, amplitude=1.0,
+                     dq_out=None, dk_out=None, dtype=None, workspace=None, stream=None):
+    """Gradients of qk_norm_rope: of q, k (dtype: theirs by default, or bf16 or float32)
+    and, in float32, of q_gain and k_gain (None where that is None), from those of its
+    outputs, dq and dk: float32, or q's type.  q and k are the forward's inputs; any
+    strides with the elements of a head side by side.  Outputs are contiguous, or dq_out
+    and dk_out with any such strides, dq and dk themselves or q and k among them."""
+    import torch
+    if stream is None and dq_out is None and dk_out is None and dtype is None and workspace is None:
+        r = (_MARSHAL or _native()).qk_norm_rope_bwd(dq, dk, q, k, q_gain, k_gain, positions, freqs, eps, interleaved,
+                                                     amplitude)
+        if r is not None:
+            return _done(r, "bf1_qk_norm_rope_bwd")
+    dev, xtype, gtype, (batch, n, Hq, Hkv, d) = _norm_rope_sides(q, k, q_gain, k_gain, positions, freqs)
+    dtype = xtype if dtype is None else dtype
+    if dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError("dtype must be bfloat16 or float32")
+    ytype = getattr(dq if q is not None else dk, "dtype", None)
+    if ytype is not torch.float32 and ytype is not xtype:
+        raise ValueError(f"dq and dk must be float32 or {xtype}")
+    strides, outs, gains = [], [], []
+    for name, x, dy, out, gain in (("q", q, dq, dq_out, q_gain), ("k", k, dk, dk_out, k_gain)):
+        if x is None:
+            if dy is not None:
+                raise ValueError(f"d{name} without {name}")
+            strides += [0] * 9
+            outs.append(None)
+            gains.append(None)
+            continue
+        strides += _strided(dy, "d" + name, x.shape, ytype, dev)
+        strides += _strided(x, name, x.shape, xtype, dev)
+        out = _empty(x.shape, dtype, dev, stream) if out is None else out
+        strides += _strided(out, f"d{name}_out", x.shape, dtype, dev)
+        outs.append(out)
+        gains.append(None if gain is None else _empty((d,), torch.float32, dev, stream))
+    rot = 2 * freqs.shape[0]
+    need = qk_norm_rope_bwd_workspace_size(batch, n, Hq, Hkv, d, rot, xtype) if any(g is not None for g in gains) else 0
+    if workspace is not None:
+        check_workspace(workspace, "workspace", need, dev)
+    elif need:
+        workspace = _empty((need,), torch.uint8, dev, stream)
+    _call(load().bf1_qk_norm_rope_bwd, "bf1_qk_norm_rope_bwd", dev, stream, _ptr(dq), _ptr(dk), _type(ytype), _ptr(q),
+          _ptr(k), _ptr(q_gain), _ptr(k_gain), _type(gtype), _ptr(positions), n if positions.dim() == 2 else 0, _ptr(freqs),
+          _ptr(outs[0]), _ptr(outs[1]), _ptr(gains[0]), _ptr(gains[1]), batch, n, Hq, Hkv, d, rot, _type(xtype),
+          _type(dtype), int(bool(interleaved)), float(eps), float(amplitude), (ctypes.c_int64 * 18)(*strides),
+          _ptr(workspace), need)
+    return (*outs, *gains)
+
+
+# ---- drafted tokens over the cache, and pages of several sequences -----------------
+#
+# A step that verifies drafts: page_step and kv_append place the trees' nodes as new
+# tokens, tree_step makes their masks and positions (for rope or qk_norm_rope too),
+# attn_tree is their attention, kv_compact keeps the accepted ones.  page_fork and
+# kv_copy continue sequences from others and free what nobody holds any more.
+
+def tree_step(parents, token_start, lens_before, seq_lens, masks=None, positions=None, stream=None):
+    """(masks, positions) of the nodes of drafted trees, packed as page_step's rows.
+
+    parents: int32 [rows], each node's parent in its own tree (an earlier node; anything
+    else: none, the node follows the sequence's newest token).  token_start and seq_lens:
+    page_step's for this step; lens_before: the lengths it was given.  masks: int64 [rows],
+    bit k of a row set where node k is the node or one before it; positions: int32 [rows],
+    the length plus the depth.  A tree has up to 64 nodes; those past the 64th or past
+    seq_lens, and rows behind the last tree, get mask 0 and position -1."""
+    if masks is None and positions is None and stream is None:
+        r = (_MARSHAL or _native()).tree_step(parents, token_start, lens_before, seq_lens)
+        if r is not None:
+            return _done(r, "bf1_tree_step")
+    import torch
+    dev = _cuda_device(parents, "parents")
+    _i32_cuda(parents, "parents", 1)
+    _i32_cuda(lens_before, "lens_before", 1, dev)
+    rows, batch = parents.shape[0], lens_before.shape[0]
+    check_buffer(token_start, "token_start", (batch + 1,), torch.int32, dev)
+    check_buffer(seq_lens, "seq_lens", (batch,), torch.int32, dev)
+    masks = _empty((rows,), torch.int64, dev, stream) if masks is None \
+        else check_buffer(masks, "masks", (rows,), torch.int64, dev)
+    positions = _empty((rows,), torch.int32, dev, stream) if positions is None \
+        else check_buffer(positions, "positions", (rows,), torch.int32, dev)
+    _call(load().bf1_tree_step, "bf1_tree_step", dev, stream, _ptr(parents), _ptr(token_start), _ptr(lens_before),
+          _ptr(seq_lens), batch, rows, _ptr(masks), _ptr(positions))
+    return masks, positions
+
+
+def _bf16_pages(k_pages, v_pages):
+    """Check bf16 pages [num_pages, Hkv, B, d]; returns (device, sizes)."""
+    import torch
+    dev = _cuda_device(k_pages, "k_pages")
+    if k_pages.dim() != 4:
+        raise ValueError("k_pages must be a 4-D tensor [num_pages, Hkv, B, d]")
+    check_buffer(k_pages, "k_pages", k_pages.shape, torch.bfloat16, dev)
+    check_buffer(v_pages, "v_pages", k_pages.shape, torch.bfloat16, dev)
+    return dev, tuple(k_pages.shape)
+
+
+def attn_tree_workspace_size(batch, max_nodes, Hq, Hkv, head_dim, B, max_pages, L=2, dense=False):
+    out = ctypes.c_int64(0)
+    _check(load().bf1_attn_tree_workspace_size(int(batch), int(max_nodes), int(Hq), int(Hkv), int(head_dim), int(B),
+                                               int(max_pages), int(L), int(bool(dense)), ctypes.byref(out)),
+           "bf1_attn_tree_workspace_size")
+    return out.value
+
+
+def attn_tree(q, k_pages, v_pages, masks, positions, lens_before, token_start, page_table, B=64, L=2, dense=False,
+              max_nodes=64, out=None, lse=None, workspace=None, stream=None):
+    """Attention of all nodes of drafted trees over the paged cache that holds them (at
+    page_step's slots); returns (O [rows, Hq, d] bf16, LSE [rows, Hq] fp32).
+
+    q: [rows, Hq, d] bf16, packed; masks, positions: tree_step's, or any masks; lens_before:
+    the lengths without the drafted tokens; token_start: page_step's.  A node at position
+    p reads the committed keys of the blocks on the BF1 route of block p // B (dense: of
+    every block up to it) and the drafted ones of its mask.  max_nodes: the largest tree of
+    the call, at most 64; rows past it get NaN, as do those without a place and those of a
+    sequence that lacks a page.  Rows behind the last tree are left as they are."""
+    if out is None and lse is None and workspace is None and stream is None:
+        r = (_MARSHAL or _native()).attn_tree(q, k_pages, v_pages, masks, positions, lens_before, token_start, page_table, B,
+                                              L, dense, max_nodes)
+        if r is not None:
+            return _done(r, "bf1_attn_tree")
+    import torch
+    dev, (num_pages, Hkv, pw, d) = _bf16_pages(k_pages, v_pages)
+    if not isinstance(q, torch.Tensor) or q.dim() != 3 or q.shape[2] != d or pw != B:
+        raise ValueError("q must be [rows, Hq, d] with the cache's head size, and its pages hold B tokens")
+    rows, Hq, _ = q.shape
+    check_buffer(q, "q", q.shape, torch.bfloat16, dev)
+    check_buffer(masks, "masks", (rows,), torch.int64, dev)
+    check_buffer(positions, "positions", (rows,), torch.int32, dev)
+    if not isinstance(page_table, torch.Tensor) or page_table.dim() != 2:
+        raise ValueError("page_table must be a 2-D tensor [batch, max_pages]")
+    batch, max_pages = page_table.shape
+    check_buffer(page_table, "page_table", page_table.shape, torch.int32, dev)
+    check_buffer(lens_before, "lens_before", (batch,), torch.int32, dev)
+    check_buffer(token_start, "token_start", (batch + 1,), torch.int32, dev)
+    out = _empty(q.shape, torch.bfloat16, dev, stream) if out is None \
+        else check_buffer(out, "out", q.shape, torch.bfloat16, dev)
+    lse = _empty((rows, Hq), torch.float32, dev, stream) if lse is None \
+        else check_buffer(lse, "lse", (rows, Hq), torch.float32, dev)
+    need = attn_tree_workspace_size(batch, max_nodes, Hq, Hkv, d, B, max_pages, L, dense)
+    if workspace is not None:
+        check_workspace(workspace, "workspace", need, dev)
+    elif need:
+        workspace = _empty((need,), torch.uint8, dev, stream)
+    _call(load().bf1_attn_tree, "bf1_attn_tree", dev, stream, _ptr(q), _ptr(k_pages), _ptr(v_pages), _ptr(masks),
+          _ptr(positions), _ptr(lens_before), _ptr(token_start), _ptr(page_table), max_pages, num_pages, _ptr(out), _ptr(lse),
+          batch, rows, int(max_nodes), Hq, Hkv, d, int(B), int(L), int(bool(dense)), _ptr(workspace), need)
+    return out, lse
+
+
+def kv_compact(k_pages, v_pages, accepted, lens_before, seq_lens, page_table, out=None, stream=None):
+    """Move the rows of the accepted nodes of every tree together in one layer's bf16
+    cache: node accepted[b, k] goes to position lens_before[b] + k.  Returns the new lengths
+    int32 [batch] (`out`, if given; another tensor than the two it is made of).
+
+    accepted: int32 [batch, up to 64], a path's nodes, ascending; the first entry that is
+    not above the one before it, or is no node (-1), ends it.  seq_lens: with the drafted
+    tokens, as page_step returned it."""
+    if out is None and stream is None:
+        r = (_MARSHAL or _native()).kv_compact(k_pages, v_pages, accepted, lens_before, seq_lens, page_table)
+        if r is not None:
+            return _done(r, "bf1_kv_compact")
+    import torch
+    dev, (num_pages, Hkv, B, d) = _bf16_pages(k_pages, v_pages)
+    if not isinstance(page_table, torch.Tensor) or page_table.dim() != 2:
+        raise ValueError("page_table must be a 2-D tensor [batch, max_pages]")
+    batch, max_pages = page_table.shape
+    check_buffer(page_table, "page_table", page_table.shape, torch.int32, dev)
+    if not isinstance(accepted, torch.Tensor) or accepted.dim() != 2:
+        raise ValueError("accepted must be a 2-D tensor [batch, up to 64]")
+    width = accepted.shape[1]
+    check_buffer(accepted, "accepted", (batch, width), torch.int32, dev)
+    check_buffer(lens_before, "lens_before", (batch,), torch.int32, dev)
+    check_buffer(seq_lens, "seq_lens", (batch,), torch.int32, dev)
+    out = _empty((batch,), torch.int32, dev, stream) if out is None else check_buffer(out, "out", (batch,), torch.int32, dev)
+    _call(load().bf1_kv_compact, "bf1_kv_compact", dev, stream, _ptr(k_pages), _ptr(v_pages), _ptr(accepted), width,
+          _ptr(lens_before), _ptr(seq_lens), _ptr(page_table), batch, max_pages, num_pages, Hkv, d, B, _ptr(out))
+    return out
+
+
+class PageFork(NamedTuple):
+    """What page_fork writes: the new page table [batch, max_pages], lengths [batch] and
+    head of the free list [1], and the copies to make, [batch] each: copy_rows[b] tokens of
+    page copy_from[b] to page copy_to[b] (-1, -1 and 0: none)."""
+    page_table: object
+    seq_lens: object
+    free_head: object
+    copy_from: object
+    copy_to: object
+    copy_rows: object
+
+
+def page_fork(seq_lens, sources, keep_lens, page_table, shares, free_pages, free_head, B=64, out=None, stream=None):
+    """Every place b of the batch goes on with the first keep_lens[b] tokens (at most all)
+    of the sequence that place sources[b] holds, or ends where sources[b] is no place: forks,
+    beams that change places, tokens taken back, ends.  Returns a PageFork (`out`, if given).
+
+    All are int32.  shares [num_pages] counts the holders of a page beyond the first
+    (zeros for a new cache; add 1 to the pages you hold yourself) and is updated, as is
+    free_pages, page_step's list with room for every page: pages that nobody holds any more
+    go back below the head.  Full blocks are shared; a block that goes on being written
+    stays with the first place that continues it, if nobody else holds its page, and is
+    copied for the others: kv_copy with the result's lists, for each layer's cache (for a
+    CacheQ8 move the tails instead).  Without a free page a sequence goes on without that
+    block's tokens.  To run the same call again (a warm-up before a capture, a retry), put
+    shares and free_pages back as they were first."""
+    if out is None and stream is None:
+        r = (_MARSHAL or _native()).page_fork(seq_lens, sources, keep_lens, page_table, shares, free_pages, free_head, B)
+        if r is not None:
+            return PageFork._make(_done(r, "bf1_page_fork"))
+    import torch
+    dev = _cuda_device(page_table, "page_table")
+    if page_table.dim() != 2:
+        raise ValueError("page_table must be a 2-D tensor [batch, max_pages]")
+    batch, max_pages = page_table.shape
+    check_buffer(page_table, "page_table", page_table.shape, torch.int32, dev)
+    for name, t in (("seq_lens", seq_lens), ("sources", sources), ("keep_lens", keep_lens)):
+        check_buffer(t, name, (batch,), torch.int32, dev)
+    _i32_cuda(shares, "shares", 1, dev)
+    _i32_cuda(free_pages, "free_pages", 1, dev)
+    check_buffer(free_head, "free_head", (1,), torch.int32, dev)
+    sizes = ((batch, max_pages), (batch,), (1,), (batch,), (batch,), (batch,))
+    if out is None:
+        out = PageFork(*(_empty(s, torch.int32, dev, stream) for s in sizes))
+    else:
+        out = PageFork(*out)
+        for name, t, s in zip(PageFork._fields, out, sizes):
+            check_buffer(t, name, s, torch.int32, dev)
+    _call(load().bf1_page_fork, "bf1_page_fork", dev, stream, batch, _ptr(seq_lens), _ptr(sources), _ptr(keep_lens),
+          _ptr(page_table), max_pages, _ptr(shares), shares.shape[0], _ptr(free_pages), free_pages.shape[0],
+          _ptr(free_head), int(B), *(_ptr(t) for t in out))
+    return out
+
+
+def kv_copy(k_pages, v_pages, copy_from, copy_to, copy_rows, stream=None):
+    """Copy the first copy_rows[i] tokens of K and V page copy_from[i] to page copy_to[i]
+    (int32 lists, page_fork's) in bf16 pages [num_pages, Hkv, B, d]; entries outside the
+    cache are left out.  No page is copied to twice, or both to and from."""
+    if stream is None:
+        r = (_MARSHAL or _native()).kv_copy(k_pages, v_pages, copy_from, copy_to, copy_rows)
+        if r is not None:
+            return _check(r, "bf1_kv_copy")
+    dev, (num_pages, Hkv, B, d) = _bf16_pages(k_pages, v_pages)
+    _i32_cuda(copy_from, "copy_from", 1, dev)
+    _i32_cuda(copy_to, "copy_to", 1, dev)
+    _i32_cuda(copy_rows, "copy_rows", 1, dev)
+    if not copy_from.shape == copy_to.shape == copy_rows.shape:
+        raise ValueError("copy_from, copy_to and copy_rows must have the same length")
+    _call(load().bf1_kv_copy, "bf1_kv_copy", dev, stream, _ptr(k_pages), _ptr(v_pages), _ptr(copy_from), _ptr(copy_to),
+          _ptr(copy_rows), copy_from.shape[0], num_pages, Hkv, d, B)

@@ -15,6 +15,7 @@ import shutil
 import subprocess
 import sys
 import sysconfig
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
@@ -23,6 +24,8 @@ LIB = os.path.join(HERE, "libbf1.so")
 MARSHAL = os.path.join(HERE, "_marshal.so")
 ROCM = os.environ.get("ROCM_PATH", "/opt/rocm")
 ARCH = "gfx950"
+HIP_SOURCES = ("bf1_tree", "bf1_decode", "bf1_decode_q8", "bf1_kernels", "bf1_bwd", "bf1_norm_rope", "bf1_cache",
+               "bf1_stack", "bf1_pages")
 
 HIP_FLAGS = [
     f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC",
@@ -48,30 +51,17 @@ def build(verbose=False, extra_hip_flags=()):
     hipcc = shutil.which("hipcc") or os.path.join(ROCM, "bin", "hipcc")
     gxx = shutil.which("g++") or "g++"
     os.makedirs(BUILD, exist_ok=True)
-    k_obj = os.path.join(BUILD, "bf1_kernels.o")
-    b_obj = os.path.join(BUILD, "bf1_bwd.o")
-    d_obj = os.path.join(BUILD, "bf1_decode.o")
-    s_obj = os.path.join(BUILD, "bf1_stack.o")
-    c_obj = os.path.join(BUILD, "bf1_cache.o")
-    q_obj = os.path.join(BUILD, "bf1_decode_q8.o")
-    a_obj = os.path.join(BUILD, "bf1_api.o")
-    _run([hipcc, *HIP_FLAGS, *extra_hip_flags, "-c", os.path.join(CSRC, "bf1_kernels.hip"),
-          "-o", k_obj], verbose)
-    _run([hipcc, *HIP_FLAGS, *extra_hip_flags, "-c", os.path.join(CSRC, "bf1_bwd.hip"),
-          "-o", b_obj], verbose)
-    _run([hipcc, *HIP_FLAGS, *extra_hip_flags, "-c", os.path.join(CSRC, "bf1_decode.hip"),
-          "-o", d_obj], verbose)
-    _run([hipcc, *HIP_FLAGS, *extra_hip_flags, "-c", os.path.join(CSRC, "bf1_stack.hip"),
-          "-o", s_obj], verbose)
-    _run([hipcc, *HIP_FLAGS, *extra_hip_flags, "-c", os.path.join(CSRC, "bf1_cache.hip"),
-          "-o", c_obj], verbose)
-    _run([hipcc, *HIP_FLAGS, *extra_hip_flags, "-c", os.path.join(CSRC, "bf1_decode_q8.hip"),
-          "-o", q_obj], verbose)
-    _run([gxx, *HOST_FLAGS, "-c", os.path.join(CSRC, "bf1_api.cpp"), "-o", a_obj], verbose)
+    objs, steps = [], []
+    for name in HIP_SOURCES:
+        objs.append(os.path.join(BUILD, name + ".o"))
+        steps.append([hipcc, *HIP_FLAGS, *extra_hip_flags, "-c", os.path.join(CSRC, name + ".hip"), "-o", objs[-1]])
+    objs.append(os.path.join(BUILD, "bf1_api.o"))
+    steps.append([gxx, *HOST_FLAGS, "-c", os.path.join(CSRC, "bf1_api.cpp"), "-o", objs[-1]])
+    with ThreadPoolExecutor(4) as pool:
+        list(pool.map(lambda cmd: _run(cmd, verbose), steps))
     tmp = LIB + ".tmp"
-    _run([hipcc, f"--offload-arch={ARCH}", "-shared", "-fPIC", k_obj, b_obj, d_obj, s_obj, c_obj, q_obj, a_obj,
-          "-o", tmp,
-          f"-L{ROCM}/lib", "-lamdhip64", f"-Wl,-rpath,{ROCM}/lib"], verbose)
+    _run([hipcc, f"--offload-arch={ARCH}", "-shared", "-fPIC", *objs, "-o", tmp, f"-L{ROCM}/lib", "-lamdhip64",
+          f"-Wl,-rpath,{ROCM}/lib"], verbose)
     os.replace(tmp, LIB)
     torch = importlib.util.find_spec("torch").submodule_search_locations[0]
     inc, lib = os.path.join(torch, "include"), os.path.join(torch, "lib")

@@ -11,6 +11,7 @@
 
 #include "../../include/bf1.h"
 #include "bf1_device.h"
+#include "bf1_rotary.h"
 
 namespace bf1 {
 namespace {
@@ -262,20 +263,6 @@ __device__ __forceinline__ void store_n(T* p, const float* f) {
 #pragma unroll
         for (int k = 0; k < N; ++k) p[k] = (T)f[k];
     }
-}
-
-// p * f radians without its whole turns: the nearest fp32 number of half turns, in
-// [-1, 1], and the radians left (below 2^-23).
-struct Turn {
-    float half_turns, rest;
-};
-__device__ __forceinline__ Turn turn_of(double p, double f) {
-    constexpr double INV = 0x1.45f306dc9c883p-3, INV_LOW = -0x1.6b01ec5417056p-57;  // 1 / (2 pi)
-    const double a = p * f, a_low = fma(p, f, -a);
-    const double t = a * INV, t_low = fma(a, INV, -t) + fma(a, INV_LOW, a_low * INV);
-    const double x = 2. * ((t - rint(t)) + t_low);
-    const float h = (float)x;
-    return {h, (float)((x - (double)h) * 3.141592653589793)};
 }
 
 template <typename TI, typename TO, bool INTER, int P, int HB>

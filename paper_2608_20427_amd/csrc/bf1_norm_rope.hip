@@ -1,0 +1,611 @@
+// Per-head RMSNorm of queries and keys with the rotary positions in the same pass,
+// and its gradient, for gfx950.
+//
+//   r = (mean x^2 + eps)^-1/2,  n = x r,  y = amplitude R(p f) (n g)
+//
+// over a head's d elements; R turns the first `rot` of them in pairs by the angle
+// p f_i (bf1_rotary.h: exact products, reduced in double), the others only get their
+// norm.  With the incoming gradient dy:
+//
+//   dn = amplitude R^T dy,  u = dn g,  dx = r (u - n mean(u n)),  dg = sum over rows of dn n
+//
+// All sums and the turn are fp32, the result is rounded once.  Both are bound by
+// memory: a row is read once and written once, 16 bytes a lane and load.
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include <algorithm>
+#include <type_traits>
+
+#include "../../include/bf1.h"
+#include "bf1_device.h"
+#include "bf1_rotary.h"
+
+// every instance rounds the same way: contraction only where it is written
+#pragma clang fp contract(off)
+
+namespace bf1 {
+namespace {
+
+constexpr int THREADS = 256;
+
+int status_of(hipError_t e) { return e == hipSuccess ? BF1_OK : BF1_ERR_HIP; }
+bool aligned(const void* p, uintptr_t a) { return p != nullptr && reinterpret_cast<uintptr_t>(p) % a == 0; }
+bool launchable(int64_t blocks) { return blocks < (int64_t(1) << 32) / THREADS; }
+
+// A row (one head of one token) belongs to a team of 1 << `lshift` lanes of one wave.  A
+// lane holds P elements from `a` and P from `b` on: the two halves of P pairs, 2 P
+// elements of pairs that lie side by side, or 2 P of the rest behind the pairs.  P is
+// what 16 bytes hold of x, also where rows are read element by element (na, nb: how
+// many there are), so that a row's sums do not go by its alignment.
+template <typename T>
+constexpr int PAIRS = 16 / sizeof(T);
+
+struct Lane {
+    int32_t a, b, na, nb;
+    bool turn;
+    int32_t pair, pairs;  // first pair and their number
+};
+template <bool INTER, int P>
+__device__ __forceinline__ Lane lane_of(int32_t l, int32_t d, int32_t half) {
+    const int32_t units = (half + P - 1) / P;
+    Lane x;
+    x.turn = l < units;
+    x.pair = l * P;
+    x.pairs = x.turn ? min(P, half - l * P) : 0;
+    if (x.turn && !INTER) {
+        x.a = l * P;
+        x.b = half + l * P;
+        x.na = x.nb = x.pairs;
+    } else {
+        x.a = x.turn ? 2 * l * P : 2 * half + 2 * (l - units) * P;
+        x.b = x.a + P;
+        const int32_t end = x.turn ? 2 * half : d;
+        x.na = min(max(end - x.a, 0), P);
+        x.nb = min(max(end - x.b, 0), P);
+    }
+    return x;
+}
+
+template <typename T, int P>
+__device__ __forceinline__ void load_vec(const T* p, float* f) {
+    if constexpr (sizeof(T) == 2) {
+        if constexpr (P == 8) {
+            const u32x4 w = *reinterpret_cast<const u32x4*>(p);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                f[2 * k] = __uint_as_float(w[k] << 16);
+                f[2 * k + 1] = __uint_as_float(w[k] & 0xffff0000u);
+            }
+        } else {
+            const u32x2 w = *reinterpret_cast<const u32x2*>(p);
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                f[2 * k] = __uint_as_float(w[k] << 16);
+                f[2 * k + 1] = __uint_as_float(w[k] & 0xffff0000u);
+            }
+        }
+    } else {
+#pragma unroll
+        for (int q = 0; q < P; q += 4) {
+            const f32x4 w = *reinterpret_cast<const f32x4*>(p + q);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) f[q + k] = w[k];
+        }
+    }
+}
+
+template <typename T, int P>
+__device__ __forceinline__ void store_vec(T* p, const float* f) {
+    if constexpr (sizeof(T) == 2) {
+        typedef __bf16 vec __attribute__((ext_vector_type(P)));
+        vec v;
+#pragma unroll
+        for (int k = 0; k < P; ++k) v[k] = (__bf16)f[k];
+        *reinterpret_cast<vec*>(p) = v;
+    } else {
+#pragma unroll
+        for (int q = 0; q < P; q += 4) *reinterpret_cast<f32x4*>(p + q) = f32x4{f[q], f[q + 1], f[q + 2], f[q + 3]};
+    }
+}
+
+// A lane's 2 P elements of a row; zeros where there are none.
+template <typename T, int P, bool WIDE>
+__device__ __forceinline__ void load_row(const T* row, const Lane& x, float* f) {
+    if constexpr (WIDE) {
+#pragma unroll
+        for (int k = 0; k < 2 * P; ++k) f[k] = 0.f;
+        if (x.na) load_vec<T, P>(row + x.a, f);
+        if (x.nb) load_vec<T, P>(row + x.b, f + P);
+    } else {
+#pragma unroll
+        for (int k = 0; k < P; ++k) {
+            f[k] = k < x.na ? (float)row[x.a + k] : 0.f;
+            f[P + k] = k < x.nb ? (float)row[x.b + k] : 0.f;
+        }
+    }
+}
+
+template <typename T, int P, bool WIDE>
+__device__ __forceinline__ void store_row(T* row, const Lane& x, const float* f) {
+    if constexpr (WIDE) {
+        if (x.na) store_vec<T, P>(row + x.a, f);
+        if (x.nb) store_vec<T, P>(row + x.b, f + P);
+    } else {
+#pragma unroll
+        for (int k = 0; k < P; ++k) {
+            if (k < x.na) row[x.a + k] = (T)f[k];
+            if (k < x.nb) row[x.b + k] = (T)f[P + k];
+        }
+    }
+}
+
+// A lane's elements of a gain vector (ones without one), bf16 or fp32 and of any
+// alignment; read once per workgroup's turn from the caches.
+template <int P>
+__device__ __forceinline__ void load_gain(const void* gain, int32_t f32, const Lane& x, float* g) {
+#pragma unroll
+    for (int k = 0; k < 2 * P; ++k) {
+        const int32_t e = (k < P ? x.a + k : x.b + k - P);
+        const bool in = k < P ? k < x.na : k - P < x.nb;
+        g[k] = gain == nullptr || !in ? 1.f : f32 ? ((const float*)gain)[e] : (float)((const __bf16*)gain)[e];
+    }
+}
+
+__device__ __forceinline__ float team_sum(float s, int32_t lshift) {
+    for (int32_t m = 1 << lshift >> 1; m > 0; m >>= 1) s += __shfl_xor(s, m);
+    return s;
+}
+
+// Turns a lane's pairs: e0 c - e1 s, e1 c + e0 s.
+template <bool INTER, int P>
+__device__ __forceinline__ void turn_pairs(float* y, const float* c, const float* s) {
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+        const int e0 = INTER ? 2 * i : i, e1 = INTER ? 2 * i + 1 : P + i;
+        const float x0 = y[e0], x1 = y[e1];
+        y[e0] = fmaf(x0, c[i], -(x1 * s[i]));
+        y[e1] = fmaf(x1, c[i], x0 * s[i]);
+    }
+}
+
+template <int P>
+__device__ __forceinline__ void turns(const Lane& x, int32_t position, const double* freqs, float amplitude, float sign,
+                                      float* c, float* s) {
+    if (!x.turn) return;
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+        const Turn t = turn_of((double)position, freqs[min(x.pair + i, x.pair + x.pairs - 1)]);
+        float cs, sn;
+        sincospif(t.half_turns, &sn, &cs);
+        c[i] = fmaf(-sn, t.rest, cs) * amplitude;
+        s[i] = fmaf(cs, t.rest, sn) * (sign * amplitude);
+    }
+}
+
+struct Rows {
+    const void* p;
+    int64_t b, h, t;  // strides of batch, head and token, in elements
+};
+struct Side {
+    Rows x, dy, out;
+    const void* gain;
+    int32_t heads;
+};
+struct Shape {
+    const int32_t* positions;
+    int64_t pos_batch;
+    const double* freqs;
+    uint32_t items;  // rows * lanes of a team
+    uint32_t n, hsplit;
+    int32_t d, half, lshift, gain_f32;
+    float eps, amplitude;
+};
+
+// 256 lanes: teams of neighbouring tokens, HB heads each, so that a lane's cosines and
+// sines serve them all; workgroups follow each other over the heads of the same tokens.
+template <typename T, typename TO, bool INTER, bool WIDE, int HB>
+__global__ __launch_bounds__(THREADS) void norm_rope_kernel(Side q, Side k, Shape z) {
+    constexpr int P = PAIRS<T>;
+    const uint32_t group = blockIdx.x / z.hsplit;
+    const uint32_t item = group * THREADS + threadIdx.x;
+    const bool live = item < z.items;
+    const uint32_t row = live ? item >> z.lshift : 0;
+    const uint32_t b = row / z.n, t = row - b * z.n;
+    const Lane x = lane_of<INTER, P>((int32_t)(item & ((1u << z.lshift) - 1)), z.d, z.half);
+    const int32_t heads = q.heads + k.heads;
+    const int32_t h0 = (int32_t)(blockIdx.x - group * z.hsplit) * HB;
+    float v[HB][2 * P];
+#pragma unroll
+    for (int j = 0; j < HB; ++j) {
+        const int32_t h = min(h0 + j, heads - 1);
+        const bool isk = h >= q.heads;
+        const Rows& r = isk ? k.x : q.x;
+        load_row<T, P, WIDE>((const T*)r.p + b * r.b + (isk ? h - q.heads : h) * r.h + t * r.t, x, v[j]);
+    }
+    float c[P], s[P];
+    turns<P>(x, z.positions[b * z.pos_batch + t], z.freqs, z.amplitude, 1.f, c, s);
+#pragma unroll
+    for (int j = 0; j < HB; ++j) {
+        const int32_t h = h0 + j;
+        if (h >= heads) break;
+        const bool isk = h >= q.heads;
+        float sum = 0.f;
+#pragma unroll
+        for (int e = 0; e < 2 * P; ++e) sum = fmaf(v[j][e], v[j][e], sum);
+        const float r = 1.0f / sqrtf(team_sum(sum, z.lshift) / (float)z.d + z.eps);
+        float g[2 * P];
+        load_gain<P>(isk ? k.gain : q.gain, z.gain_f32, x, g);
+#pragma unroll
+        for (int e = 0; e < 2 * P; ++e) v[j][e] = v[j][e] * r * g[e];
+        if (x.turn) turn_pairs<INTER, P>(v[j], c, s);
+        if (live) {
+            const Rows& o = isk ? k.out : q.out;
+            store_row<TO, P, WIDE>((TO*)const_cast<void*>(o.p) + b * o.b + (isk ? h - q.heads : h) * o.h + t * o.t, x,
+                                   v[j]);
+        }
+    }
+}
+
+// The gradient.  A workgroup goes over tiles of THREADS / team tokens and HB heads,
+// gridDim.x apart, and keeps its sums of the gains' gradients in registers; at the end
+// its teams meet (lane moves, then LDS) and write one record [2][d], which the next
+// kernel sums over the workgroups, in their order.  The records go by the call's sizes
+// alone, so the result is the same each time.
+template <typename T, typename TD, typename TO, bool INTER, bool WIDE, int HB>
+__global__ __launch_bounds__(THREADS) void norm_rope_bwd_kernel(Side q, Side k, Shape z, uint32_t tiles,
+                                                                float* __restrict__ q_dgain, float* __restrict__ k_dgain,
+                                                                float* __restrict__ records) {
+    constexpr int P = PAIRS<T>;
+    __shared__ float part[THREADS / 64][2][64 * 2 * P];  // [wave][side][lane of a team, element]
+    const Lane x = lane_of<INTER, P>((int32_t)(threadIdx.x & ((1u << z.lshift) - 1)), z.d, z.half);
+    const int32_t heads = q.heads + k.heads;
+    float acc[2][2 * P];
+#pragma unroll
+    for (int e = 0; e < 2 * P; ++e) acc[0][e] = acc[1][e] = 0.f;
+    for (uint32_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+        const uint32_t group = tile / z.hsplit;
+        const uint32_t item = group * THREADS + threadIdx.x;
+        const bool live = item < z.items;
+        const uint32_t row = live ? item >> z.lshift : 0;
+        const uint32_t b = row / z.n, t = row - b * z.n;
+        const int32_t h0 = (int32_t)(tile - group * z.hsplit) * HB;
+        float v[HB][2 * P], dy[HB][2 * P];
+#pragma unroll
+        for (int j = 0; j < HB; ++j) {
+            const int32_t h = min(h0 + j, heads - 1);
+            const bool isk = h >= q.heads;
+            const int32_t hh = isk ? h - q.heads : h;
+            const Rows &r = isk ? k.x : q.x, &y = isk ? k.dy : q.dy;
+            load_row<T, P, WIDE>((const T*)r.p + b * r.b + hh * r.h + t * r.t, x, v[j]);
+            load_row<TD, P, WIDE>((const TD*)y.p + b * y.b + hh * y.h + t * y.t, x, dy[j]);
+        }
+        float c[P], s[P];
+        turns<P>(x, z.positions[b * z.pos_batch + t], z.freqs, z.amplitude, -1.f, c, s);
+#pragma unroll
+        for (int j = 0; j < HB; ++j) {
+            const int32_t h = h0 + j;
+            if (h >= heads) break;
+            const bool isk = h >= q.heads;
+            float g[2 * P];
+            load_gain<P>(isk ? k.gain : q.gain, z.gain_f32, x, g);
+            if (x.turn) turn_pairs<INTER, P>(dy[j], c, s);
+            float sum = 0.f;
+#pragma unroll
+            for (int e = 0; e < 2 * P; ++e) sum = fmaf(v[j][e], v[j][e], sum);
+            const float r = 1.0f / sqrtf(team_sum(sum, z.lshift) / (float)z.d + z.eps);
+            float along = 0.f;
+            float dg[2 * P];
+#pragma unroll
+            for (int e = 0; e < 2 * P; ++e) {
+                v[j][e] *= r;
+                dg[e] = live ? dy[j][e] * v[j][e] : 0.f;
+                dy[j][e] *= g[e];
+                along = fmaf(dy[j][e], v[j][e], along);
+            }
+            along = team_sum(along, z.lshift) / (float)z.d;
+#pragma unroll
+            for (int e = 0; e < 2 * P; ++e) dy[j][e] = r * fmaf(-v[j][e], along, dy[j][e]);
+            if (isk) {
+#pragma unroll
+                for (int e = 0; e < 2 * P; ++e) acc[1][e] += dg[e];
+            } else {
+#pragma unroll
+                for (int e = 0; e < 2 * P; ++e) acc[0][e] += dg[e];
+            }
+            if (live) {
+                const Rows& o = isk ? k.out : q.out;
+                store_row<TO, P, WIDE>((TO*)const_cast<void*>(o.p) + b * o.b + (isk ? h - q.heads : h) * o.h + t * o.t, x,
+                                       dy[j]);
+            }
+        }
+    }
+    if (q_dgain == nullptr && k_dgain == nullptr) return;
+    const int32_t team = 1 << z.lshift, l = threadIdx.x & (team - 1), wave = threadIdx.x >> 6;
+#pragma unroll
+    for (int side = 0; side < 2; ++side)
+#pragma unroll
+        for (int e = 0; e < 2 * P; ++e) {
+            float a = acc[side][e];
+            for (int32_t m = team; m < 64; m <<= 1) a += __shfl_xor(a, m);
+            if ((threadIdx.x & 63) < team) part[wave][side][l * 2 * P + e] = a;
+        }
+    __syncthreads();
+    if ((int32_t)threadIdx.x >= team) return;
+    // the first team's lanes write what the waves' teams of the same lane have
+#pragma unroll
+    for (int side = 0; side < 2; ++side)
+#pragma unroll
+        for (int e = 0; e < 2 * P; ++e) {
+            float a = 0.f;
+#pragma unroll
+            for (int w = 0; w < THREADS / 64; ++w) a += part[w][side][l * 2 * P + e];
+            const int32_t at = e < P ? x.a + e : x.b + e - P;
+            if (e < P ? e >= x.na : e - P >= x.nb) continue;
+            if (records != nullptr)
+                records[((int64_t)blockIdx.x * 2 + side) * z.d + at] = a;
+            else if (float* out = side ? k_dgain : q_dgain)
+                out[at] = a;
+        }
+}
+
+// The gains' gradients from the workgroups' records: 32 columns a workgroup, 32 threads
+// each.
+constexpr int SUM_THREADS = 1024, SUM_COLS = 32;
+__global__ __launch_bounds__(SUM_THREADS) void gain_sum_kernel(const float* __restrict__ records, int32_t count, int32_t d,
+                                                               float* __restrict__ q_dgain, float* __restrict__ k_dgain) {
+    constexpr int PER = SUM_THREADS / SUM_COLS;
+    __shared__ float part[PER][SUM_COLS];
+    const int32_t col = blockIdx.x * SUM_COLS + threadIdx.x % SUM_COLS, r0 = threadIdx.x / SUM_COLS;
+    float a = 0.f;
+    if (col < 2 * d) {
+#pragma unroll 8
+        for (int32_t r = r0; r < count; r += PER) a += records[(int64_t)r * 2 * d + col];
+    }
+    part[r0][threadIdx.x % SUM_COLS] = a;
+    __syncthreads();
+    if (r0 != 0 || col >= 2 * d) return;
+    a = 0.f;
+#pragma unroll
+    for (int r = 0; r < PER; ++r) a += part[r][threadIdx.x];
+    float* out = col < d ? q_dgain : k_dgain;
+    if (out != nullptr) out[col < d ? col : col - d] = a;
+}
+
+// A dimension's stride where it is used: one with a single entry may have any.
+int64_t used(int64_t stride, int64_t entries) { return entries > 1 ? stride : 0; }
+
+int32_t team_shift(int32_t d, int32_t half, int32_t P) {
+    const int32_t units = (half + P - 1) / P + (d - 2 * half + 2 * P - 1) / (2 * P);
+    int32_t s = 0;
+    while ((1 << s) < units) ++s;
+    return s;
+}
+
+constexpr int BWD_HEADS = 2;
+constexpr int64_t MOST_RECORDS = 1024;
+int64_t bwd_tiles(int64_t rows, int32_t heads, int32_t lshift) {
+    return ((rows << lshift) + THREADS - 1) / THREADS * ((heads + BWD_HEADS - 1) / BWD_HEADS);
+}
+
+// Sizes that forward, backward and workspace refuse the same way; BF1_OK with *rows == 0
+// where there is nothing to do.
+int check_sizes(int64_t batch, int64_t n, int32_t Hq, int32_t Hkv, int32_t d, int32_t rot, int32_t type, int64_t* rows) {
+    *rows = 0;
+    if (batch < 0 || n < 0 || Hq < 0 || Hkv < 0 || type < 0 || type > 1) return BF1_ERR_INVALID_ARG;
+    if (d < 2 || d > 512 || d % 2 || rot < 2 || rot > d || rot % 2) return BF1_ERR_UNSUPPORTED;
+    if (n >= (int64_t(1) << 31) || Hq + (int64_t)Hkv > 65535) return BF1_ERR_UNSUPPORTED;
+    if (batch == 0 || n == 0 || Hq + Hkv == 0) return BF1_OK;
+    const int32_t P = type == BF1_TYPE_BF16 ? 8 : 4, lshift = team_shift(d, rot / 2, P);
+    if ((double)batch * n * (1 << lshift) >= 2147483648.0) return BF1_ERR_UNSUPPORTED;
+    if (!launchable((((batch * n) << lshift) / THREADS + 1) * (Hq + Hkv))) return BF1_ERR_UNSUPPORTED;
+    *rows = batch * n;
+    return BF1_OK;
+}
+
+// The used strides of one tensor, 0 where an element is out of a 64-bit byte offset's
+// reach or a stride is negative.
+bool rows_of(const void* p, const int64_t* st, int32_t batch, int32_t heads, int64_t n, Rows* r) {
+    *r = Rows{p, used(st[0], batch), used(st[1], heads), used(st[2], n)};
+    return r->b >= 0 && r->h >= 0 && r->t >= 0 && (double)batch * r->b + (double)heads * r->h + (double)n * r->t <= 1e18;
+}
+// Whether no element of [batch, heads, n, d] rows is written twice: every dimension
+// steps over all that the closer ones cover.
+bool distinct(const Rows& r, int32_t batch, int32_t heads, int64_t n, int32_t d) {
+    struct Dim {
+        int64_t stride, size;
+    } dims[3] = {{r.b, batch}, {r.h, heads}, {r.t, n}};
+    std::sort(dims, dims + 3, [](const Dim& x, const Dim& y) { return x.stride < y.stride; });
+    int64_t extent = d;
+    for (const Dim& x : dims) {
+        if (x.size <= 1) continue;
+        if (x.stride < extent) return false;
+        extent = x.stride * (x.size - 1) + extent;
+    }
+    return true;
+}
+bool multiples(const Rows& r, int64_t vec) { return r.b % vec == 0 && r.h % vec == 0 && r.t % vec == 0; }
+
+// Alignment of a lane's vector of P elements: 16 bytes, or what P elements have if less.
+bool wide_rows(const Rows& r, int64_t P, int64_t esize) {
+    const int64_t vec = std::min<int64_t>(P, 16 / esize);
+    return aligned(r.p, vec * esize) && multiples(r, vec);
+}
+
+}  // namespace
+}  // namespace bf1
+
+extern "C" {
+
+int bf1_qk_norm_rope(const void* Q, const void* K, const void* q_gain, const void* k_gain, int32_t gain_type,
+                     const int32_t* positions, int64_t positions_batch_stride, const double* freqs, void* Q_out,
+                     void* K_out, int32_t batch, int64_t n, int32_t Hq, int32_t Hkv, int32_t head_dim, int32_t rot_dim,
+                     int32_t in_type, int32_t out_type, int32_t interleaved, float eps, float amplitude,
+                     const int64_t* strides, void* stream) {
+    int64_t rows;
+    const int bad = bf1::check_sizes(batch, n, Hq, Hkv, head_dim, rot_dim, in_type, &rows);
+    if (bad != BF1_OK) return bad;
+    if (!strides || (interleaved & ~1) || !(eps > 0.f) || out_type < 0 || out_type > 1 || gain_type < 0 || gain_type > 1)
+        return BF1_ERR_INVALID_ARG;
+    if (in_type == BF1_TYPE_BF16 && out_type != BF1_TYPE_BF16) return BF1_ERR_UNSUPPORTED;
+    if (positions_batch_stride != 0 && positions_batch_stride < n) return BF1_ERR_INVALID_ARG;
+    if (rows == 0) return BF1_OK;
+    if (!bf1::aligned(positions, 4) || !bf1::aligned(freqs, 8)) return BF1_ERR_INVALID_ARG;
+    const int64_t esize = in_type == BF1_TYPE_BF16 ? 2 : 4, osize = out_type == BF1_TYPE_BF16 ? 2 : 4;
+    const int64_t gsize = gain_type == BF1_TYPE_BF16 ? 2 : 4, P = 16 / esize;
+    if ((q_gain && !bf1::aligned(q_gain, gsize)) || (k_gain && !bf1::aligned(k_gain, gsize))) return BF1_ERR_INVALID_ARG;
+    // a side's output is read by no other row's lanes: it is not the other side's input or output
+    if (Hq > 0 && Hkv > 0 && (Q_out == K_out || Q_out == K || K_out == Q)) return BF1_ERR_INVALID_ARG;
+    const int32_t half = rot_dim / 2;
+    bool wide = half % P == 0 && (head_dim - rot_dim) % P == 0;
+    bf1::Side side[2];
+    for (int i = 0; i < 2; ++i) {
+        const int32_t heads = i ? Hkv : Hq;
+        const void *in = i ? K : Q, *out = i ? K_out : Q_out;
+        side[i] = bf1::Side{};
+        side[i].heads = heads;
+        side[i].gain = i ? k_gain : q_gain;
+        if (heads == 0) continue;
+        if (!bf1::aligned(in, esize) || !bf1::aligned(out, osize)) return BF1_ERR_INVALID_ARG;
+        if (!bf1::rows_of(in, strides + 6 * i, batch, heads, n, &side[i].x) ||
+            !bf1::rows_of(out, strides + 6 * i + 3, batch, heads, n, &side[i].out) ||
+            !bf1::distinct(side[i].out, batch, heads, n, head_dim))
+            return BF1_ERR_INVALID_ARG;
+        const bf1::Rows &x = side[i].x, &o = side[i].out;
+        if (in == out && (in_type != out_type || x.b != o.b || x.h != o.h || x.t != o.t)) return BF1_ERR_INVALID_ARG;
+        wide = wide && bf1::wide_rows(x, P, esize) && bf1::wide_rows(o, P, osize);
+    }
+    const int32_t lshift = bf1::team_shift(head_dim, half, (int32_t)P);
+    const int64_t groups = ((rows << lshift) + bf1::THREADS - 1) / bf1::THREADS;
+    const int32_t heads = Hq + Hkv;
+    const int32_t hb = !wide || groups * heads < 256 ? 1 : 2;
+    const int32_t hsplit = (heads + hb - 1) / hb;
+    const bf1::Shape z{positions, positions_batch_stride, freqs, (uint32_t)(rows << lshift), (uint32_t)n, (uint32_t)hsplit,
+                       head_dim, half, lshift, gain_type == BF1_TYPE_F32, eps, amplitude};
+    auto go = [&](auto kern) {
+        hipLaunchKernelGGL(kern, dim3((unsigned)(groups * hsplit)), dim3(bf1::THREADS), 0, (hipStream_t)stream, side[0],
+                           side[1], z);
+        return bf1::status_of(hipGetLastError());
+    };
+    auto pick = [&](auto in_c, auto out_c, auto inter_c) {
+        using T = decltype(in_c);
+        using TO = decltype(out_c);
+        constexpr bool I = decltype(inter_c)::value;
+        if (!wide) return go(bf1::norm_rope_kernel<T, TO, I, false, 1>);
+        return hb == 1 ? go(bf1::norm_rope_kernel<T, TO, I, true, 1>) : go(bf1::norm_rope_kernel<T, TO, I, true, 2>);
+    };
+    auto types = [&](auto inter_c) {
+        if (in_type == BF1_TYPE_BF16) return pick((__bf16)0, (__bf16)0, inter_c);
+        return out_type == BF1_TYPE_BF16 ? pick(0.f, (__bf16)0, inter_c) : pick(0.f, 0.f, inter_c);
+    };
+    return interleaved ? types(std::true_type{}) : types(std::false_type{});
+}
+
+int bf1_qk_norm_rope_bwd_workspace_size(int32_t batch, int64_t n, int32_t Hq, int32_t Hkv, int32_t head_dim,
+                                        int32_t rot_dim, int32_t in_type, int64_t* bytes) {
+    if (!bytes) return BF1_ERR_INVALID_ARG;
+    int64_t rows;
+    const int bad = bf1::check_sizes(batch, n, Hq, Hkv, head_dim, rot_dim, in_type, &rows);
+    if (bad != BF1_OK) return bad;
+    *bytes = 0;
+    if (rows == 0) return BF1_OK;
+    const int32_t lshift = bf1::team_shift(head_dim, rot_dim / 2, in_type == BF1_TYPE_BF16 ? 8 : 4);
+    const int64_t records = std::min(bf1::bwd_tiles(rows, Hq + Hkv, lshift), bf1::MOST_RECORDS);
+    if (records > 1) *bytes = records * 2 * head_dim * 4;
+    return BF1_OK;
+}
+
+int bf1_qk_norm_rope_bwd(const void* dQ, const void* dK, int32_t grad_type, const void* Q, const void* K,
+                         const void* q_gain, const void* k_gain, int32_t gain_type, const int32_t* positions,
+                         int64_t positions_batch_stride, const double* freqs, void* dQ_in, void* dK_in, float* dq_gain,
+                         float* dk_gain, int32_t batch, int64_t n, int32_t Hq, int32_t Hkv, int32_t head_dim,
+                         int32_t rot_dim, int32_t in_type, int32_t out_type, int32_t interleaved, float eps,
+                         float amplitude, const int64_t* strides, void* workspace, int64_t workspace_bytes, void* stream) {
+    int64_t rows;
+    const int bad = bf1::check_sizes(batch, n, Hq, Hkv, head_dim, rot_dim, in_type, &rows);
+    if (bad != BF1_OK) return bad;
+    if (!strides || (interleaved & ~1) || !(eps > 0.f) || out_type < 0 || out_type > 1 || gain_type < 0 || gain_type > 1 ||
+        grad_type < 0 || grad_type > 1)
+        return BF1_ERR_INVALID_ARG;
+    if (in_type == BF1_TYPE_F32 && grad_type == BF1_TYPE_BF16) return BF1_ERR_UNSUPPORTED;
+    if (positions_batch_stride != 0 && positions_batch_stride < n) return BF1_ERR_INVALID_ARG;
+    if ((dq_gain && !bf1::aligned(dq_gain, 4)) || (dk_gain && !bf1::aligned(dk_gain, 4)) || (dq_gain && dq_gain == dk_gain))
+        return BF1_ERR_INVALID_ARG;
+    const int64_t esize = in_type == BF1_TYPE_BF16 ? 2 : 4, osize = out_type == BF1_TYPE_BF16 ? 2 : 4;
+    const int64_t dsize = grad_type == BF1_TYPE_BF16 ? 2 : 4, gsize = gain_type == BF1_TYPE_BF16 ? 2 : 4, P = 16 / esize;
+    const int32_t half = rot_dim / 2, heads = Hq + Hkv;
+    hipStream_t stm = (hipStream_t)stream;
+    const int sum_groups = (2 * head_dim + bf1::SUM_COLS - 1) / bf1::SUM_COLS;
+    if (rows == 0) {  // sums over nothing
+        if (!dq_gain && !dk_gain) return BF1_OK;
+        hipLaunchKernelGGL(bf1::gain_sum_kernel, dim3(sum_groups), dim3(bf1::SUM_THREADS), 0, stm, nullptr, 0, head_dim,
+                           dq_gain, dk_gain);
+        return bf1::status_of(hipGetLastError());
+    }
+    if (!bf1::aligned(positions, 4) || !bf1::aligned(freqs, 8)) return BF1_ERR_INVALID_ARG;
+    if ((q_gain && !bf1::aligned(q_gain, gsize)) || (k_gain && !bf1::aligned(k_gain, gsize))) return BF1_ERR_INVALID_ARG;
+    if (Hq > 0 && Hkv > 0 && (dQ_in == dK_in || dQ_in == dK || dK_in == dQ || dQ_in == K || dK_in == Q))
+        return BF1_ERR_INVALID_ARG;
+    bool wide = half % P == 0 && (head_dim - rot_dim) % P == 0;
+    bf1::Side side[2];
+    for (int i = 0; i < 2; ++i) {
+        const int32_t h = i ? Hkv : Hq;
+        const void *dy = i ? dK : dQ, *x = i ? K : Q, *out = i ? dK_in : dQ_in;
+        side[i] = bf1::Side{};
+        side[i].heads = h;
+        side[i].gain = i ? k_gain : q_gain;
+        if (h == 0) continue;
+        if (!bf1::aligned(dy, dsize) || !bf1::aligned(x, esize) || !bf1::aligned(out, osize)) return BF1_ERR_INVALID_ARG;
+        const int64_t* st = strides + 9 * i;
+        if (!bf1::rows_of(dy, st, batch, h, n, &side[i].dy) || !bf1::rows_of(x, st + 3, batch, h, n, &side[i].x) ||
+            !bf1::rows_of(out, st + 6, batch, h, n, &side[i].out) ||
+            !bf1::distinct(side[i].out, batch, h, n, head_dim))
+            return BF1_ERR_INVALID_ARG;
+        const bf1::Rows& o = side[i].out;
+        for (int j = 0; j < 2; ++j) {  // over dy or x only where an element keeps its place
+            const bf1::Rows& r = j ? side[i].x : side[i].dy;
+            if (r.p == out && ((j ? in_type : grad_type) != out_type || r.b != o.b || r.h != o.h || r.t != o.t))
+                return BF1_ERR_INVALID_ARG;
+        }
+        wide = wide && bf1::wide_rows(side[i].dy, P, dsize) && bf1::wide_rows(side[i].x, P, esize) &&
+               bf1::wide_rows(o, P, osize);
+    }
+    const int32_t lshift = bf1::team_shift(head_dim, half, (int32_t)P);
+    const int64_t tiles = bf1::bwd_tiles(rows, heads, lshift);
+    const int64_t records = std::min(tiles, bf1::MOST_RECORDS);
+    const bool sums = dq_gain || dk_gain;
+    if (sums && records > 1) {
+        if (!bf1::aligned(workspace, 16)) return BF1_ERR_INVALID_ARG;
+        if (workspace_bytes < records * 2 * head_dim * 4) return BF1_ERR_BUFFER_TOO_SMALL;
+    }
+    const bf1::Shape z{positions, positions_batch_stride, freqs, (uint32_t)(rows << lshift), (uint32_t)n,
+                       (uint32_t)((heads + bf1::BWD_HEADS - 1) / bf1::BWD_HEADS), head_dim, half, lshift,
+                       gain_type == BF1_TYPE_F32, eps, amplitude};
+    auto go = [&](auto kern) {
+        hipLaunchKernelGGL(kern, dim3((unsigned)records), dim3(bf1::THREADS), 0, stm, side[0], side[1], z, (uint32_t)tiles,
+                           dq_gain, dk_gain, records > 1 ? (float*)workspace : nullptr);
+        if (sums && records > 1)
+            hipLaunchKernelGGL(bf1::gain_sum_kernel, dim3(sum_groups), dim3(bf1::SUM_THREADS), 0, stm,
+                               (const float*)workspace, (int32_t)records, head_dim, dq_gain, dk_gain);
+        return bf1::status_of(hipGetLastError());
+    };
+    auto pick = [&](auto x_c, auto d_c, auto out_c) {
+        using T = decltype(x_c);
+        using TD = decltype(d_c);
+        using TO = decltype(out_c);
+        constexpr int HB = bf1::BWD_HEADS;
+        if (interleaved)
+            return wide ? go(bf1::norm_rope_bwd_kernel<T, TD, TO, true, true, HB>)
+                        : go(bf1::norm_rope_bwd_kernel<T, TD, TO, true, false, HB>);
+        return wide ? go(bf1::norm_rope_bwd_kernel<T, TD, TO, false, true, HB>)
+                    : go(bf1::norm_rope_bwd_kernel<T, TD, TO, false, false, HB>);
+    };
+    auto outs = [&](auto x_c, auto d_c) {
+        return out_type == BF1_TYPE_BF16 ? pick(x_c, d_c, (__bf16)0) : pick(x_c, d_c, 0.f);
+    };
+    if (in_type == BF1_TYPE_F32) return outs(0.f, 0.f);
+    return grad_type == BF1_TYPE_BF16 ? outs((__bf16)0, (__bf16)0) : outs((__bf16)0, 0.f);
+}
+
+}  // extern "C"

@@ -124,55 +124,71 @@ PyObject* page_step(PyObject*, PyObject* const* a, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
+// What rope and norm + rope have in common.
+struct Turning {
+    int dims, token;                       // 3: rows [tokens, heads, d]; 4: [batch, heads, n, d]
+    int64_t batch, rows, d, heads[2];
+    const Tensor *x[2], *pos, *freqs;
+    bool own;  // positions of each batch entry
+};
+bool turning(PyObject* qo, PyObject* ko, PyObject* po, PyObject* fo, int* dev, Turning* t) {
+    if (!THPVariable_CheckExact(qo)) return false;
+    t->dims = (int)THPVariable_Unpack(qo).dim();
+    if (t->dims != 3 && t->dims != 4) return false;
+    t->x[0] = tensor(qo, t->dims, dev);
+    t->x[1] = tensor(ko, t->dims, dev);
+    if (!t->x[0] || !t->x[1]) return false;
+    const Tensor &q = *t->x[0], &k = *t->x[1];
+    t->token = t->dims == 3 ? 0 : 2;
+    t->batch = t->dims == 3 ? 1 : q.size(0);
+    t->rows = q.size(t->token);
+    t->d = q.size(t->dims - 1);
+    if (q.scalar_type() != k.scalar_type() || (q.scalar_type() != BF16 && q.scalar_type() != F32) ||
+        k.size(t->token) != t->rows || k.size(t->dims - 1) != t->d || (t->dims == 4 && k.size(0) != t->batch) ||
+        q.stride(t->dims - 1) != 1 || k.stride(t->dims - 1) != 1)
+        return false;
+    t->freqs = row(fo, F64, dev);
+    if (!t->freqs || t->freqs->numel() < 1 || t->freqs->numel() > t->d / 2) return false;
+    t->pos = exact(po, I32, {t->rows}, dev);
+    t->own = t->pos == nullptr && t->dims == 4;
+    if (t->own) t->pos = exact(po, I32, {t->batch, t->rows}, dev);
+    t->heads[0] = q.size(1);
+    t->heads[1] = k.size(1);
+    return t->pos && t->batch <= INT32_MAX && t->d <= INT32_MAX && t->heads[0] <= INT32_MAX && t->heads[1] <= INT32_MAX;
+}
+// Strides over batch, heads and tokens.
+void strides_of(const Tensor& x, const Turning& t, int64_t* s) {
+    s[0] = t.dims == 4 ? x.stride(0) : 0;
+    s[1] = x.stride(1);
+    s[2] = x.stride(t.token);
+}
 // rope(q, k, positions, freqs, interleaved, amplitude, transposed): q and k
 PyObject* rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
     HANDLE_TH_ERRORS
-    if (n != 7 || !THPVariable_CheckExact(a[0]) || !PyBool_Check(a[4]) || !PyFloat_CheckExact(a[5])) Py_RETURN_NONE;
     int64_t transposed;
-    if (!integer(a[6], &transposed)) Py_RETURN_NONE;
     int dev = -1;
-    const int dims = (int)THPVariable_Unpack(a[0]).dim();
-    if (dims != 3 && dims != 4) Py_RETURN_NONE;
-    const Tensor *q = tensor(a[0], dims, &dev), *k = tensor(a[1], dims, &dev);
-    if (!q || !k || q->scalar_type() != k->scalar_type() || (q->scalar_type() != BF16 && q->scalar_type() != F32))
+    Turning t;
+    if (n != 7 || !PyBool_Check(a[4]) || !PyFloat_CheckExact(a[5]) || !integer(a[6], &transposed) ||
+        !turning(a[0], a[1], a[2], a[3], &dev, &t))
         Py_RETURN_NONE;
-    const int token = dims == 3 ? 0 : 2;  // rows [tokens, heads, d] or [batch, heads, n, d]
-    const int64_t batch = dims == 3 ? 1 : q->size(0), rows = q->size(token), d = q->size(dims - 1);
-    if (k->size(token) != rows || k->size(dims - 1) != d || (dims == 4 && k->size(0) != batch) || q->stride(dims - 1) != 1 ||
-        k->stride(dims - 1) != 1)
-        Py_RETURN_NONE;
-    const Tensor* freqs = row(a[3], F64, &dev);
-    if (!freqs || freqs->numel() < 1 || freqs->numel() > d / 2) Py_RETURN_NONE;
-    const Tensor* pos = exact(a[2], I32, {rows}, &dev);
-    const bool own = pos == nullptr && dims == 4;  // positions of each batch entry
-    if (own) pos = exact(a[2], I32, {batch, rows}, &dev);
-    if (!pos || batch > INT32_MAX || d > INT32_MAX) Py_RETURN_NONE;
-    const ScalarType type = q->scalar_type();
-    Tensor qo = empty(q->sizes(), type, dev), ko = empty(k->sizes(), type, dev);
+    const ScalarType type = t.x[0]->scalar_type();
+    Tensor out[2];
     int64_t strides[12];
-    int64_t heads[2];
-    for (int side = 0; side < 2; ++side) {
-        const Tensor& x = side ? *k : *q;
-        const int64_t h = heads[side] = x.size(1);
-        int64_t* s = strides + 6 * side;
-        s[0] = dims == 4 ? x.stride(0) : 0;
-        s[1] = x.stride(1);
-        s[2] = x.stride(token);
-        s[3] = dims == 4 ? h * rows * d : 0;
-        s[4] = dims == 4 ? rows * d : d;
-        s[5] = dims == 4 ? d : h * d;
+    for (int i = 0; i < 2; ++i) {
+        out[i] = empty(t.x[i]->sizes(), type, dev);
+        strides_of(*t.x[i], t, strides + 6 * i);
+        strides_of(out[i], t, strides + 6 * i + 3);
     }
-    if (heads[0] > INT32_MAX || heads[1] > INT32_MAX) Py_RETURN_NONE;
-    const int32_t t = type == BF16 ? BF1_TYPE_BF16 : BF1_TYPE_F32;
+    const int32_t ty = type == BF16 ? BF1_TYPE_BF16 : BF1_TYPE_F32;
     const int32_t interleaved = a[4] == Py_True;
     const float amplitude = (float)PyFloat_AS_DOUBLE(a[5]);
     const int st = unlocked([&] {
-        return bf1_rope(q->data_ptr(), k->data_ptr(), pos->const_data_ptr<int32_t>(), own ? rows : 0,
-                        freqs->const_data_ptr<double>(), qo.data_ptr(), ko.data_ptr(), (int32_t)batch, rows,
-                        (int32_t)heads[0], (int32_t)heads[1], (int32_t)d, (int32_t)(2 * freqs->numel()), t, t, interleaved,
-                        amplitude, (int32_t)transposed, strides, stream_of(dev));
+        return bf1_rope(t.x[0]->data_ptr(), t.x[1]->data_ptr(), t.pos->const_data_ptr<int32_t>(), t.own ? t.rows : 0,
+                        t.freqs->const_data_ptr<double>(), out[0].data_ptr(), out[1].data_ptr(), (int32_t)t.batch, t.rows,
+                        (int32_t)t.heads[0], (int32_t)t.heads[1], (int32_t)t.d, (int32_t)(2 * t.freqs->numel()), ty, ty,
+                        interleaved, amplitude, (int32_t)transposed, strides, stream_of(dev));
     });
-    return st == BF1_OK ? tuple({qo, ko}) : status(st);
+    return st == BF1_OK ? tuple({out[0], out[1]}) : status(st);
     END_HANDLE_TH_ERRORS
 }
 
@@ -294,12 +310,260 @@ PyObject* attn_decode_q8(PyObject*, PyObject* const* a, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
+// Gains [d], bf16 or fp32, or None.
+bool gains_of(PyObject* qo, PyObject* ko, int64_t d, int* dev, const Tensor** q, const Tensor** k, int32_t* type) {
+    *q = *k = nullptr;
+    ScalarType st = F32;
+    for (int i = 0; i < 2; ++i) {
+        PyObject* o = i ? ko : qo;
+        if (o == Py_None) continue;
+        const Tensor* g = tensor(o, 1, dev);
+        if (!g || (g->scalar_type() != BF16 && g->scalar_type() != F32) || !g->is_contiguous() || g->numel() != d) return false;
+        if (i && *q && g->scalar_type() != st) return false;
+        st = g->scalar_type();
+        *(i ? k : q) = g;
+    }
+    *type = st == BF16 ? BF1_TYPE_BF16 : BF1_TYPE_F32;
+    return true;
+}
+void* ptr(const Tensor* t) { return t ? t->data_ptr() : nullptr; }
+
+// qk_norm_rope(q, k, q_gain, k_gain, positions, freqs, eps, interleaved, amplitude): q and k
+PyObject* qk_norm_rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    int dev = -1;
+    Turning t;
+    const Tensor *qg, *kg;
+    int32_t gtype;
+    if (n != 9 || !PyFloat_CheckExact(a[6]) || !PyBool_Check(a[7]) || !PyFloat_CheckExact(a[8]) ||
+        !turning(a[0], a[1], a[4], a[5], &dev, &t) || !gains_of(a[2], a[3], t.d, &dev, &qg, &kg, &gtype))
+        Py_RETURN_NONE;
+    const ScalarType type = t.x[0]->scalar_type();
+    Tensor out[2];
+    int64_t strides[12];
+    for (int i = 0; i < 2; ++i) {
+        out[i] = empty(t.x[i]->sizes(), type, dev);
+        strides_of(*t.x[i], t, strides + 6 * i);
+        strides_of(out[i], t, strides + 6 * i + 3);
+    }
+    const int32_t ty = type == BF16 ? BF1_TYPE_BF16 : BF1_TYPE_F32, interleaved = a[7] == Py_True;
+    const float eps = (float)PyFloat_AS_DOUBLE(a[6]), amplitude = (float)PyFloat_AS_DOUBLE(a[8]);
+    const int st = unlocked([&] {
+        return bf1_qk_norm_rope(t.x[0]->data_ptr(), t.x[1]->data_ptr(), ptr(qg), ptr(kg), gtype,
+                                t.pos->const_data_ptr<int32_t>(), t.own ? t.rows : 0, t.freqs->const_data_ptr<double>(),
+                                out[0].data_ptr(), out[1].data_ptr(), (int32_t)t.batch, t.rows, (int32_t)t.heads[0],
+                                (int32_t)t.heads[1], (int32_t)t.d, (int32_t)(2 * t.freqs->numel()), ty, ty, interleaved, eps,
+                                amplitude, strides, stream_of(dev));
+    });
+    return st == BF1_OK ? tuple({out[0], out[1]}) : status(st);
+    END_HANDLE_TH_ERRORS
+}
+
+// qk_norm_rope_bwd(dq, dk, q, k, q_gain, k_gain, positions, freqs, eps, interleaved, amplitude):
+// the gradients of q, k and both gains
+PyObject* qk_norm_rope_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    int dev = -1;
+    Turning t;
+    const Tensor *qg, *kg;
+    int32_t gtype;
+    if (n != 11 || !PyFloat_CheckExact(a[8]) || !PyBool_Check(a[9]) || !PyFloat_CheckExact(a[10]) ||
+        !turning(a[2], a[3], a[6], a[7], &dev, &t) || !gains_of(a[4], a[5], t.d, &dev, &qg, &kg, &gtype) || !qg || !kg)
+        Py_RETURN_NONE;
+    const Tensor* dy[2] = {tensor(a[0], t.dims, &dev), tensor(a[1], t.dims, &dev)};
+    const ScalarType type = t.x[0]->scalar_type();
+    for (int i = 0; i < 2; ++i)
+        if (!dy[i] || dy[i]->sizes() != t.x[i]->sizes() || dy[i]->stride(t.dims - 1) != 1 ||
+            (dy[i]->scalar_type() != F32 && dy[i]->scalar_type() != type) || dy[i]->scalar_type() != dy[0]->scalar_type())
+            Py_RETURN_NONE;
+    const int32_t ty = type == BF16 ? BF1_TYPE_BF16 : BF1_TYPE_F32;
+    const int32_t rot = (int32_t)(2 * t.freqs->numel());
+    int64_t need = 0;
+    int st = bf1_qk_norm_rope_bwd_workspace_size((int32_t)t.batch, t.rows, (int32_t)t.heads[0], (int32_t)t.heads[1],
+                                                 (int32_t)t.d, rot, ty, &need);
+    if (st != BF1_OK) return status(st);
+    Tensor out[2], gain[2], ws;
+    int64_t strides[18];
+    for (int i = 0; i < 2; ++i) {
+        out[i] = empty(t.x[i]->sizes(), type, dev);
+        gain[i] = empty({t.d}, F32, dev);
+        strides_of(*dy[i], t, strides + 9 * i);
+        strides_of(*t.x[i], t, strides + 9 * i + 3);
+        strides_of(out[i], t, strides + 9 * i + 6);
+    }
+    if (need > 0) ws = empty({need}, at::kByte, dev);
+    const int32_t interleaved = a[9] == Py_True;
+    const float eps = (float)PyFloat_AS_DOUBLE(a[8]), amplitude = (float)PyFloat_AS_DOUBLE(a[10]);
+    st = unlocked([&] {
+        return bf1_qk_norm_rope_bwd(
+            dy[0]->data_ptr(), dy[1]->data_ptr(), dy[0]->scalar_type() == BF16 ? BF1_TYPE_BF16 : BF1_TYPE_F32,
+            t.x[0]->data_ptr(), t.x[1]->data_ptr(), ptr(qg), ptr(kg), gtype, t.pos->const_data_ptr<int32_t>(),
+            t.own ? t.rows : 0, t.freqs->const_data_ptr<double>(), out[0].data_ptr(), out[1].data_ptr(),
+            (float*)gain[0].data_ptr(), (float*)gain[1].data_ptr(), (int32_t)t.batch, t.rows, (int32_t)t.heads[0],
+            (int32_t)t.heads[1], (int32_t)t.d, rot, ty, ty, interleaved, eps, amplitude, strides,
+            need > 0 ? ws.data_ptr() : nullptr, need, stream_of(dev));
+    });
+    return st == BF1_OK ? tuple({out[0], out[1], gain[0], gain[1]}) : status(st);
+    END_HANDLE_TH_ERRORS
+}
+
+// tree_step(parents, token_start, lens_before, seq_lens): masks and positions
+PyObject* tree_step(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    int dev = -1;
+    if (n != 4) Py_RETURN_NONE;
+    const Tensor *parents = row(a[0], I32, &dev), *before = row(a[2], I32, &dev);
+    if (!parents || !before) Py_RETURN_NONE;
+    const int64_t rows = parents->numel(), batch = before->numel();
+    const Tensor *start = exact(a[1], I32, {batch + 1}, &dev), *after = exact(a[3], I32, {batch}, &dev);
+    if (!start || !after || batch > INT32_MAX) Py_RETURN_NONE;
+    Tensor masks = empty({rows}, I64, dev), pos = empty({rows}, I32, dev);
+    const int st = unlocked([&] {
+        return bf1_tree_step(parents->const_data_ptr<int32_t>(), start->const_data_ptr<int32_t>(),
+                             before->const_data_ptr<int32_t>(), after->const_data_ptr<int32_t>(), (int32_t)batch, rows,
+                             (int64_t*)masks.data_ptr(), (int32_t*)pos.data_ptr(), stream_of(dev));
+    });
+    return st == BF1_OK ? tuple({masks, pos}) : status(st);
+    END_HANDLE_TH_ERRORS
+}
+
+// The bf16 pages [num_pages, Hkv, B, d] of a cache.
+bool bf16_pages(PyObject* ko, PyObject* vo, int* dev, const Tensor** k, const Tensor** v) {
+    *k = tensor(ko, 4, dev);
+    if (!*k || (*k)->scalar_type() != BF16 || !(*k)->is_contiguous()) return false;
+    *v = exact(vo, BF16, (*k)->sizes(), dev);
+    for (int i = 0; i < 4; ++i)
+        if ((*k)->size(i) > INT32_MAX) return false;
+    return *v != nullptr;
+}
+
+// attn_tree(q, k_pages, v_pages, masks, positions, lens_before, token_start, page_table, B, L, dense, max_nodes)
+PyObject* attn_tree(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    int64_t B, L, most;
+    int dev = -1;
+    if (n != 12 || !integer(a[8], &B) || !integer(a[9], &L) || !PyBool_Check(a[10]) || !integer(a[11], &most) ||
+        L > INT32_MAX || L < INT32_MIN || most > INT32_MAX || most < INT32_MIN)
+        Py_RETURN_NONE;
+    const Tensor *q = tensor(a[0], 3, &dev), *k, *v;
+    if (!q || q->scalar_type() != BF16 || !q->is_contiguous() || !bf16_pages(a[1], a[2], &dev, &k, &v)) Py_RETURN_NONE;
+    const int64_t rows = q->size(0), Hq = q->size(1), d = q->size(2);
+    const Tensor* table = tensor(a[7], 2, &dev);
+    if (k->size(2) != B || k->size(3) != d || Hq > INT32_MAX || !table || table->scalar_type() != I32 ||
+        !table->is_contiguous() || table->size(0) > INT32_MAX || table->size(1) > INT32_MAX)
+        Py_RETURN_NONE;
+    const int64_t batch = table->size(0);
+    const Tensor *masks = exact(a[3], I64, {rows}, &dev), *pos = exact(a[4], I32, {rows}, &dev);
+    const Tensor *before = exact(a[5], I32, {batch}, &dev), *start = exact(a[6], I32, {batch + 1}, &dev);
+    if (!masks || !pos || !before || !start) Py_RETURN_NONE;
+    const int32_t dense = a[10] == Py_True;
+    int64_t need = 0;
+    int st = bf1_attn_tree_workspace_size((int32_t)batch, (int32_t)most, (int32_t)Hq, (int32_t)k->size(1), (int32_t)d,
+                                          (int32_t)B, (int32_t)table->size(1), (int32_t)L, dense, &need);
+    if (st != BF1_OK) return status(st);
+    Tensor out = empty(q->sizes(), BF16, dev), lse = empty({rows, Hq}, F32, dev), ws;
+    if (need > 0) ws = empty({need}, at::kByte, dev);
+    st = unlocked([&] {
+        return bf1_attn_tree(q->data_ptr(), k->data_ptr(), v->data_ptr(), masks->const_data_ptr<int64_t>(),
+                             pos->const_data_ptr<int32_t>(), before->const_data_ptr<int32_t>(),
+                             start->const_data_ptr<int32_t>(), table->const_data_ptr<int32_t>(), (int32_t)table->size(1),
+                             (int32_t)k->size(0), out.data_ptr(), (float*)lse.data_ptr(), (int32_t)batch, rows, (int32_t)most,
+                             (int32_t)Hq, (int32_t)k->size(1), (int32_t)d, (int32_t)B, (int32_t)L, dense,
+                             need > 0 ? ws.data_ptr() : nullptr, need, stream_of(dev));
+    });
+    return st == BF1_OK ? tuple({out, lse}) : status(st);
+    END_HANDLE_TH_ERRORS
+}
+
+// kv_compact(k_pages, v_pages, accepted, lens_before, seq_lens, page_table): the new lengths
+PyObject* kv_compact(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    int dev = -1;
+    const Tensor *k, *v;
+    if (n != 6 || !bf16_pages(a[0], a[1], &dev, &k, &v)) Py_RETURN_NONE;
+    const Tensor *table = tensor(a[5], 2, &dev), *accepted = tensor(a[2], 2, &dev);
+    if (!table || table->scalar_type() != I32 || !table->is_contiguous() || !accepted || accepted->scalar_type() != I32 ||
+        !accepted->is_contiguous() || accepted->size(0) != table->size(0) || accepted->size(1) > INT32_MAX ||
+        table->size(0) > INT32_MAX || table->size(1) > INT32_MAX)
+        Py_RETURN_NONE;
+    const int64_t batch = table->size(0);
+    const Tensor *before = exact(a[3], I32, {batch}, &dev), *after = exact(a[4], I32, {batch}, &dev);
+    if (!before || !after) Py_RETURN_NONE;
+    Tensor out = empty({batch}, I32, dev);
+    const int st = unlocked([&] {
+        return bf1_kv_compact(k->data_ptr(), v->data_ptr(), accepted->const_data_ptr<int32_t>(), (int32_t)accepted->size(1),
+                              before->const_data_ptr<int32_t>(), after->const_data_ptr<int32_t>(),
+                              table->const_data_ptr<int32_t>(), (int32_t)batch, (int32_t)table->size(1), (int32_t)k->size(0),
+                              (int32_t)k->size(1), (int32_t)k->size(3), (int32_t)k->size(2), (int32_t*)out.data_ptr(),
+                              stream_of(dev));
+    });
+    return st == BF1_OK ? THPVariable_Wrap(out) : status(st);
+    END_HANDLE_TH_ERRORS
+}
+
+// page_fork(seq_lens, sources, keep_lens, page_table, shares, free_pages, free_head, B)
+PyObject* page_fork(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    int64_t B;
+    int dev = -1;
+    if (n != 8 || !integer(a[7], &B)) Py_RETURN_NONE;
+    const Tensor* table = tensor(a[3], 2, &dev);
+    if (!table || table->scalar_type() != I32 || !table->is_contiguous() || table->size(0) > INT32_MAX ||
+        table->size(1) > INT32_MAX)
+        Py_RETURN_NONE;
+    const int64_t batch = table->size(0), width = table->size(1);
+    const Tensor *lens = exact(a[0], I32, {batch}, &dev), *src = exact(a[1], I32, {batch}, &dev);
+    const Tensor *keep = exact(a[2], I32, {batch}, &dev), *shares = row(a[4], I32, &dev), *free = row(a[5], I32, &dev);
+    const Tensor* head = exact(a[6], I32, {1}, &dev);
+    if (!lens || !src || !keep || !shares || !free || !head || shares->numel() > INT32_MAX || free->numel() > INT32_MAX)
+        Py_RETURN_NONE;
+    // one allocation
+    auto out = empty({batch * width + 4 * batch + 1}, I32, dev)
+                   .unsafe_split_with_sizes({batch * width, batch, batch, batch, batch, 1});
+    const int st = unlocked([&] {
+        return bf1_page_fork((int32_t)batch, lens->const_data_ptr<int32_t>(), src->const_data_ptr<int32_t>(),
+                             keep->const_data_ptr<int32_t>(), table->const_data_ptr<int32_t>(), (int32_t)width,
+                             (int32_t*)shares->data_ptr(), (int32_t)shares->numel(), (int32_t*)free->data_ptr(),
+                             (int32_t)free->numel(), head->const_data_ptr<int32_t>(), (int32_t)B, (int32_t*)out[0].data_ptr(),
+                             (int32_t*)out[1].data_ptr(), (int32_t*)out[5].data_ptr(), (int32_t*)out[2].data_ptr(),
+                             (int32_t*)out[3].data_ptr(), (int32_t*)out[4].data_ptr(), stream_of(dev));
+    });
+    if (st != BF1_OK) return status(st);
+    return tuple({out[0].view({batch, width}), out[1], out[5], out[2], out[3], out[4]});
+    END_HANDLE_TH_ERRORS
+}
+
+// kv_copy(k_pages, v_pages, copy_from, copy_to, copy_rows)
+PyObject* kv_copy(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    int dev = -1;
+    const Tensor *k, *v;
+    if (n != 5 || !bf16_pages(a[0], a[1], &dev, &k, &v)) Py_RETURN_NONE;
+    const Tensor* from = row(a[2], I32, &dev);
+    if (!from || from->numel() > INT32_MAX) Py_RETURN_NONE;
+    const Tensor *to = exact(a[3], I32, {from->numel()}, &dev), *rows = exact(a[4], I32, {from->numel()}, &dev);
+    if (!to || !rows) Py_RETURN_NONE;
+    return status(unlocked([&] {
+        return bf1_kv_copy(k->data_ptr(), v->data_ptr(), from->const_data_ptr<int32_t>(), to->const_data_ptr<int32_t>(),
+                           rows->const_data_ptr<int32_t>(), (int32_t)from->numel(), (int32_t)k->size(0), (int32_t)k->size(1),
+                           (int32_t)k->size(3), (int32_t)k->size(2), stream_of(dev));
+    }));
+    END_HANDLE_TH_ERRORS
+}
+
 PyMethodDef methods[] = {
     {"page_step", (PyCFunction)(void (*)())page_step, METH_FASTCALL, nullptr},
     {"rope", (PyCFunction)(void (*)())rope, METH_FASTCALL, nullptr},
     {"kv_append", (PyCFunction)(void (*)())kv_append, METH_FASTCALL, nullptr},
     {"kv_append_q8", (PyCFunction)(void (*)())kv_append_q8, METH_FASTCALL, nullptr},
     {"attn_decode_q8", (PyCFunction)(void (*)())attn_decode_q8, METH_FASTCALL, nullptr},
+    {"qk_norm_rope", (PyCFunction)(void (*)())qk_norm_rope, METH_FASTCALL, nullptr},
+    {"qk_norm_rope_bwd", (PyCFunction)(void (*)())qk_norm_rope_bwd, METH_FASTCALL, nullptr},
+    {"tree_step", (PyCFunction)(void (*)())tree_step, METH_FASTCALL, nullptr},
+    {"attn_tree", (PyCFunction)(void (*)())attn_tree, METH_FASTCALL, nullptr},
+    {"kv_compact", (PyCFunction)(void (*)())kv_compact, METH_FASTCALL, nullptr},
+    {"page_fork", (PyCFunction)(void (*)())page_fork, METH_FASTCALL, nullptr},
+    {"kv_copy", (PyCFunction)(void (*)())kv_copy, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", "Native marshalling of the cache's operators.", -1, methods,
