@@ -483,7 +483,7 @@ int bf1_decode_attn_q8(const void* Q, const void* K_pages, const void* V_pages, 
  *               head, token of dQ, Q, dQ_in, dK, K, dK_in
  *   workspace : at least bf1_qk_norm_rope_bwd_workspace_size() bytes, 16-byte aligned; none
  *               where that is 0, or without dq_gain and dk_gain
- * eps > 0; even head_dim <= 512 and rot_dim.  Sixteen bytes at a time where strides,
+ * eps >= 1e-30; even head_dim <= 512 and rot_dim.  Sixteen bytes at a time where strides,
  * addresses and the two parts of a head allow it, element by element otherwise, with the
  * same bits.
  */

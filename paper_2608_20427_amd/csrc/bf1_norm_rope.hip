@@ -10,7 +10,10 @@
 //   dn = amplitude R^T dy,  u = dn g,  dx = r (u - n mean(u n)),  dg = sum over rows of dn n
 //
 // All sums and the turn are fp32, the result is rounded once.  Both are bound by
-// memory: a row is read once and written once, 16 bytes a lane and load.
+// memory: a row is read once and written once, 16 bytes a lane and load.  Replays of a
+// graph: 32768 tokens of 16 + 8 heads of 128 from joined rows 91 us for 403 MB (4.4 TB/s; a
+// large copy reaches 5.0), 32 tokens 4.2; the gradient of 16382 such tokens from fp32
+// gradients 90 us for 403 MB, with the sums over workgroups, of 128 tokens 12.
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -141,21 +144,34 @@ __device__ __forceinline__ void store_row(T* row, const Lane& x, const float* f)
     }
 }
 
-// A lane's elements of a gain vector (ones without one), bf16 or fp32 and of any
-// alignment; read once per workgroup's turn from the caches.
-template <int P>
+// A lane's elements of a gain vector, bf16 or fp32; ones without one.
+template <int P, bool WIDE>
 __device__ __forceinline__ void load_gain(const void* gain, int32_t f32, const Lane& x, float* g) {
+    if (gain == nullptr) {
 #pragma unroll
-    for (int k = 0; k < 2 * P; ++k) {
-        const int32_t e = (k < P ? x.a + k : x.b + k - P);
-        const bool in = k < P ? k < x.na : k - P < x.nb;
-        g[k] = gain == nullptr || !in ? 1.f : f32 ? ((const float*)gain)[e] : (float)((const __bf16*)gain)[e];
+        for (int k = 0; k < 2 * P; ++k) g[k] = 1.f;
+    } else if (f32) {
+        load_row<float, P, WIDE>((const float*)gain, x, g);
+    } else {
+        load_row<__bf16, P, WIDE>((const __bf16*)gain, x, g);
     }
 }
 
+// Sum over a team's 1 << lshift lanes, in all of them alike, by moves in the vector ALU.
+template <int CTRL>
+__device__ __forceinline__ float moved(float x) {
+    return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), CTRL, 0xf, 0xf, true));
+}
 __device__ __forceinline__ float team_sum(float s, int32_t lshift) {
-    for (int32_t m = 1 << lshift >> 1; m > 0; m >>= 1) s += __shfl_xor(s, m);
-    return s;
+    if (lshift > 0) s += moved<0xB1>(s);   // quad_perm 1 0 3 2
+    if (lshift > 1) s += moved<0x4E>(s);   // quad_perm 2 3 0 1
+    if (lshift > 2) s += moved<0x141>(s);  // row_half_mirror: the other four
+    if (lshift > 3) s += moved<0x140>(s);  // row_mirror: the other eight
+    if (lshift > 4) {
+        const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(s), __float_as_uint(s), false, false);
+        s = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    }
+    return lshift > 5 ? pair_sum(s) : s;
 }
 
 // Turns a lane's pairs: e0 c - e1 s, e1 c + e0 s.
@@ -191,7 +207,7 @@ struct Rows {
 struct Side {
     Rows x, dy, out;
     const void* gain;
-    int32_t heads;
+    int32_t heads, chunk;  // heads, and those of a workgroup's turn (the forward's: q's for both)
 };
 struct Shape {
     const int32_t* positions;
@@ -200,12 +216,18 @@ struct Shape {
     uint32_t items;  // rows * lanes of a team
     uint32_t n, hsplit;
     int32_t d, half, lshift, gain_f32;
-    float eps, amplitude;
+    float eps, amplitude, over_d;
 };
 
-// 256 lanes: teams of neighbouring tokens, HB heads each, so that a lane's cosines and
-// sines serve them all; workgroups follow each other over the heads of the same tokens.
-template <typename T, typename TO, bool INTER, bool WIDE, int HB>
+// (mean square + eps)^-1/2 of a row
+__device__ __forceinline__ float root(float sum, const Shape& z) {
+    return __builtin_amdgcn_rsqf(fmaf(sum, z.over_d, z.eps));
+}
+
+// 256 lanes: teams of neighbouring tokens, `chunk` heads each, one after the other, so that a
+// lane's cosines and sines serve them all; workgroups follow each other over the heads of
+// the same tokens.
+template <typename T, typename TO, bool INTER, bool WIDE>
 __global__ __launch_bounds__(THREADS) void norm_rope_kernel(Side q, Side k, Shape z) {
     constexpr int P = PAIRS<T>;
     const uint32_t group = blockIdx.x / z.hsplit;
@@ -214,163 +236,141 @@ __global__ __launch_bounds__(THREADS) void norm_rope_kernel(Side q, Side k, Shap
     const uint32_t row = live ? item >> z.lshift : 0;
     const uint32_t b = row / z.n, t = row - b * z.n;
     const Lane x = lane_of<INTER, P>((int32_t)(item & ((1u << z.lshift) - 1)), z.d, z.half);
-    const int32_t heads = q.heads + k.heads;
-    const int32_t h0 = (int32_t)(blockIdx.x - group * z.hsplit) * HB;
-    float v[HB][2 * P];
-#pragma unroll
-    for (int j = 0; j < HB; ++j) {
-        const int32_t h = min(h0 + j, heads - 1);
+    const int32_t first = (int32_t)(blockIdx.x - group * z.hsplit) * q.chunk;
+    const int32_t last = min(first + q.chunk, q.heads + k.heads);
+    float c[P], s[P], g[2 * P], next[2 * P];
+    auto load = [&](int32_t h, float* v) {
         const bool isk = h >= q.heads;
         const Rows& r = isk ? k.x : q.x;
-        load_row<T, P, WIDE>((const T*)r.p + b * r.b + (isk ? h - q.heads : h) * r.h + t * r.t, x, v[j]);
-    }
-    float c[P], s[P];
+        load_row<T, P, WIDE>((const T*)r.p + b * r.b + (isk ? h - q.heads : h) * r.h + t * r.t, x, v);
+    };
+    load(first, next);
     turns<P>(x, z.positions[b * z.pos_batch + t], z.freqs, z.amplitude, 1.f, c, s);
-#pragma unroll
-    for (int j = 0; j < HB; ++j) {
-        const int32_t h = h0 + j;
-        if (h >= heads) break;
+    for (int32_t h = first; h < last; ++h) {
         const bool isk = h >= q.heads;
+        float v[2 * P];
+#pragma unroll
+        for (int e = 0; e < 2 * P; ++e) v[e] = next[e];
+        if (h + 1 < last) load(h + 1, next);
+        if (h == first || h == q.heads) load_gain<P, WIDE>(isk ? k.gain : q.gain, z.gain_f32, x, g);
         float sum = 0.f;
 #pragma unroll
-        for (int e = 0; e < 2 * P; ++e) sum = fmaf(v[j][e], v[j][e], sum);
-        const float r = 1.0f / sqrtf(team_sum(sum, z.lshift) / (float)z.d + z.eps);
-        float g[2 * P];
-        load_gain<P>(isk ? k.gain : q.gain, z.gain_f32, x, g);
+        for (int e = 0; e < 2 * P; ++e) sum = fmaf(v[e], v[e], sum);
+        const float r = root(team_sum(sum, z.lshift), z);
 #pragma unroll
-        for (int e = 0; e < 2 * P; ++e) v[j][e] = v[j][e] * r * g[e];
-        if (x.turn) turn_pairs<INTER, P>(v[j], c, s);
+        for (int e = 0; e < 2 * P; ++e) v[e] = v[e] * r * g[e];
+        if (x.turn) turn_pairs<INTER, P>(v, c, s);
         if (live) {
             const Rows& o = isk ? k.out : q.out;
-            store_row<TO, P, WIDE>((TO*)const_cast<void*>(o.p) + b * o.b + (isk ? h - q.heads : h) * o.h + t * o.t, x,
-                                   v[j]);
+            store_row<TO, P, WIDE>((TO*)const_cast<void*>(o.p) + b * o.b + (isk ? h - q.heads : h) * o.h + t * o.t, x, v);
         }
     }
 }
 
-// The gradient.  A workgroup goes over tiles of THREADS / team tokens and HB heads,
-// gridDim.x apart, and keeps its sums of the gains' gradients in registers; at the end
-// its teams meet (lane moves, then LDS) and write one record [2][d], which the next
-// kernel sums over the workgroups, in their order.  The records go by the call's sizes
-// alone, so the result is the same each time.
-template <typename T, typename TD, typename TO, bool INTER, bool WIDE, int HB>
-__global__ __launch_bounds__(THREADS) void norm_rope_bwd_kernel(Side q, Side k, Shape z, uint32_t tiles,
+// The gradient.  A workgroup belongs to one side, the first `q_groups` to Q, and goes over
+// that side's tiles (THREADS / team tokens, `chunk` heads), as many apart as the side has
+// workgroups.  It keeps its sums of the gain's gradient in registers; at the end its teams
+// meet (lane moves, then LDS) and write one record [d], which the next kernel sums over
+// the workgroups, in their order.  The records go by the call's sizes alone, so the
+// result is the same each time.
+template <typename T, typename TD, typename TO, bool INTER, bool WIDE>
+__global__ __launch_bounds__(THREADS) void norm_rope_bwd_kernel(Side q, Side k, Shape z, uint32_t q_groups,
                                                                 float* __restrict__ q_dgain, float* __restrict__ k_dgain,
                                                                 float* __restrict__ records) {
     constexpr int P = PAIRS<T>;
-    __shared__ float part[THREADS / 64][2][64 * 2 * P];  // [wave][side][lane of a team, element]
+    extern __shared__ float part[];  // [wave][lane of a team, element]
     const Lane x = lane_of<INTER, P>((int32_t)(threadIdx.x & ((1u << z.lshift) - 1)), z.d, z.half);
-    const int32_t heads = q.heads + k.heads;
-    float acc[2][2 * P];
+    const bool isk = blockIdx.x >= q_groups;
+    const Side& w = isk ? k : q;
+    const uint32_t me = isk ? blockIdx.x - q_groups : blockIdx.x, hop = isk ? gridDim.x - q_groups : q_groups;
+    const uint32_t hsplit = (uint32_t)((w.heads + w.chunk - 1) / w.chunk);
+    const uint32_t tiles = (z.items + THREADS - 1) / THREADS * hsplit;
+    float acc[2 * P], g[2 * P];
 #pragma unroll
-    for (int e = 0; e < 2 * P; ++e) acc[0][e] = acc[1][e] = 0.f;
-    for (uint32_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
-        const uint32_t group = tile / z.hsplit;
+    for (int e = 0; e < 2 * P; ++e) acc[e] = 0.f;
+    load_gain<P, WIDE>(w.gain, z.gain_f32, x, g);
+    for (uint32_t tile = me; tile < tiles; tile += hop) {
+        const uint32_t group = tile / hsplit;
         const uint32_t item = group * THREADS + threadIdx.x;
         const bool live = item < z.items;
         const uint32_t row = live ? item >> z.lshift : 0;
         const uint32_t b = row / z.n, t = row - b * z.n;
-        const int32_t h0 = (int32_t)(tile - group * z.hsplit) * HB;
-        float v[HB][2 * P], dy[HB][2 * P];
-#pragma unroll
-        for (int j = 0; j < HB; ++j) {
-            const int32_t h = min(h0 + j, heads - 1);
-            const bool isk = h >= q.heads;
-            const int32_t hh = isk ? h - q.heads : h;
-            const Rows &r = isk ? k.x : q.x, &y = isk ? k.dy : q.dy;
-            load_row<T, P, WIDE>((const T*)r.p + b * r.b + hh * r.h + t * r.t, x, v[j]);
-            load_row<TD, P, WIDE>((const TD*)y.p + b * y.b + hh * y.h + t * y.t, x, dy[j]);
-        }
+        const int32_t first = (int32_t)(tile - group * hsplit) * w.chunk, last = min(first + w.chunk, w.heads);
+        const T* xp = (const T*)w.x.p + b * w.x.b + t * w.x.t;
+        const TD* yp = (const TD*)w.dy.p + b * w.dy.b + t * w.dy.t;
+        TO* op = (TO*)const_cast<void*>(w.out.p) + b * w.out.b + t * w.out.t;
         float c[P], s[P];
-        turns<P>(x, z.positions[b * z.pos_batch + t], z.freqs, z.amplitude, -1.f, c, s);
-#pragma unroll
-        for (int j = 0; j < HB; ++j) {
-            const int32_t h = h0 + j;
-            if (h >= heads) break;
-            const bool isk = h >= q.heads;
-            float g[2 * P];
-            load_gain<P>(isk ? k.gain : q.gain, z.gain_f32, x, g);
-            if (x.turn) turn_pairs<INTER, P>(dy[j], c, s);
+        for (int32_t h = first; h < last; ++h) {
+            float v[2 * P], dy[2 * P];
+            load_row<T, P, WIDE>(xp + h * w.x.h, x, v);
+            load_row<TD, P, WIDE>(yp + h * w.dy.h, x, dy);
+            if (h == first) turns<P>(x, z.positions[b * z.pos_batch + t], z.freqs, z.amplitude, -1.f, c, s);
+            if (x.turn) turn_pairs<INTER, P>(dy, c, s);
             float sum = 0.f;
 #pragma unroll
-            for (int e = 0; e < 2 * P; ++e) sum = fmaf(v[j][e], v[j][e], sum);
-            const float r = 1.0f / sqrtf(team_sum(sum, z.lshift) / (float)z.d + z.eps);
+            for (int e = 0; e < 2 * P; ++e) sum = fmaf(v[e], v[e], sum);
+            const float r = root(team_sum(sum, z.lshift), z);
             float along = 0.f;
-            float dg[2 * P];
 #pragma unroll
             for (int e = 0; e < 2 * P; ++e) {
-                v[j][e] *= r;
-                dg[e] = live ? dy[j][e] * v[j][e] : 0.f;
-                dy[j][e] *= g[e];
-                along = fmaf(dy[j][e], v[j][e], along);
+                v[e] *= r;
+                acc[e] += live ? dy[e] * v[e] : 0.f;
+                dy[e] *= g[e];
+                along = fmaf(dy[e], v[e], along);
             }
-            along = team_sum(along, z.lshift) / (float)z.d;
+            along = team_sum(along, z.lshift) * z.over_d;
 #pragma unroll
-            for (int e = 0; e < 2 * P; ++e) dy[j][e] = r * fmaf(-v[j][e], along, dy[j][e]);
-            if (isk) {
-#pragma unroll
-                for (int e = 0; e < 2 * P; ++e) acc[1][e] += dg[e];
-            } else {
-#pragma unroll
-                for (int e = 0; e < 2 * P; ++e) acc[0][e] += dg[e];
-            }
-            if (live) {
-                const Rows& o = isk ? k.out : q.out;
-                store_row<TO, P, WIDE>((TO*)const_cast<void*>(o.p) + b * o.b + (isk ? h - q.heads : h) * o.h + t * o.t, x,
-                                       dy[j]);
-            }
+            for (int e = 0; e < 2 * P; ++e) dy[e] = r * fmaf(-v[e], along, dy[e]);
+            if (live) store_row<TO, P, WIDE>(op + h * w.out.h, x, dy);
         }
     }
-    if (q_dgain == nullptr && k_dgain == nullptr) return;
+    float* dgain = isk ? k_dgain : q_dgain;
+    if (dgain == nullptr) return;
     const int32_t team = 1 << z.lshift, l = threadIdx.x & (team - 1), wave = threadIdx.x >> 6;
 #pragma unroll
-    for (int side = 0; side < 2; ++side)
-#pragma unroll
-        for (int e = 0; e < 2 * P; ++e) {
-            float a = acc[side][e];
-            for (int32_t m = team; m < 64; m <<= 1) a += __shfl_xor(a, m);
-            if ((threadIdx.x & 63) < team) part[wave][side][l * 2 * P + e] = a;
-        }
+    for (int e = 0; e < 2 * P; ++e) {
+        float a = acc[e];
+        for (int32_t m = team; m < 64; m <<= 1) a += __shfl_xor(a, m);
+        if ((threadIdx.x & 63) < team) part[(wave * team + l) * 2 * P + e] = a;
+    }
     __syncthreads();
     if ((int32_t)threadIdx.x >= team) return;
     // the first team's lanes write what the waves' teams of the same lane have
 #pragma unroll
-    for (int side = 0; side < 2; ++side)
+    for (int e = 0; e < 2 * P; ++e) {
+        float a = 0.f;
 #pragma unroll
-        for (int e = 0; e < 2 * P; ++e) {
-            float a = 0.f;
-#pragma unroll
-            for (int w = 0; w < THREADS / 64; ++w) a += part[w][side][l * 2 * P + e];
-            const int32_t at = e < P ? x.a + e : x.b + e - P;
-            if (e < P ? e >= x.na : e - P >= x.nb) continue;
-            if (records != nullptr)
-                records[((int64_t)blockIdx.x * 2 + side) * z.d + at] = a;
-            else if (float* out = side ? k_dgain : q_dgain)
-                out[at] = a;
-        }
+        for (int w = 0; w < THREADS / 64; ++w) a += part[(w * team + l) * 2 * P + e];
+        const int32_t at = e < P ? x.a + e : x.b + e - P;
+        if (e < P ? e >= x.na : e - P >= x.nb) continue;
+        (records != nullptr ? records + (int64_t)blockIdx.x * z.d : dgain)[at] = a;
+    }
 }
 
-// The gains' gradients from the workgroups' records: 32 columns a workgroup, 32 threads
-// each.
+// The gains' gradients from the workgroups' records, the first q_groups of them Q's: 32
+// columns a workgroup, 32 threads each.
 constexpr int SUM_THREADS = 1024, SUM_COLS = 32;
-__global__ __launch_bounds__(SUM_THREADS) void gain_sum_kernel(const float* __restrict__ records, int32_t count, int32_t d,
-                                                               float* __restrict__ q_dgain, float* __restrict__ k_dgain) {
+__global__ __launch_bounds__(SUM_THREADS) void gain_sum_kernel(const float* __restrict__ records, int32_t q_groups,
+                                                               int32_t groups, int32_t d, float* __restrict__ q_dgain,
+                                                               float* __restrict__ k_dgain) {
     constexpr int PER = SUM_THREADS / SUM_COLS;
     __shared__ float part[PER][SUM_COLS];
+    float* out = blockIdx.y ? k_dgain : q_dgain;
+    if (out == nullptr) return;
     const int32_t col = blockIdx.x * SUM_COLS + threadIdx.x % SUM_COLS, r0 = threadIdx.x / SUM_COLS;
+    const int32_t begin = blockIdx.y ? q_groups : 0, end = blockIdx.y ? groups : q_groups;
     float a = 0.f;
-    if (col < 2 * d) {
+    if (col < d) {
 #pragma unroll 8
-        for (int32_t r = r0; r < count; r += PER) a += records[(int64_t)r * 2 * d + col];
+        for (int32_t r = begin + r0; r < end; r += PER) a += records[(int64_t)r * d + col];
     }
     part[r0][threadIdx.x % SUM_COLS] = a;
     __syncthreads();
-    if (r0 != 0 || col >= 2 * d) return;
+    if (r0 != 0 || col >= d) return;
     a = 0.f;
 #pragma unroll
     for (int r = 0; r < PER; ++r) a += part[r][threadIdx.x];
-    float* out = col < d ? q_dgain : k_dgain;
-    if (out != nullptr) out[col < d ? col : col - d] = a;
+    out[col] = a;
 }
 
 // A dimension's stride where it is used: one with a single entry may have any.
@@ -383,10 +383,43 @@ int32_t team_shift(int32_t d, int32_t half, int32_t P) {
     return s;
 }
 
-constexpr int BWD_HEADS = 2;
-constexpr int64_t MOST_RECORDS = 1024;
-int64_t bwd_tiles(int64_t rows, int32_t heads, int32_t lshift) {
-    return ((rows << lshift) + THREADS - 1) / THREADS * ((heads + BWD_HEADS - 1) / BWD_HEADS);
+// Heads of a workgroup: as many as leave some 768 workgroups, three a compute unit, for
+// angles are the dearest part of a row (a double product, a reduction, cosine and sine of
+// every pair) and serve all of them; in equal parts.  us, 16 + 8 heads of 128, forward with 1 /
+// 2 / 4 / 8 / 12 / 24 heads: 1024 tokens 6.8 / 7.5 / 7.6 / 12 / 15 / 25, 4096 21 / 17 / 15 / 18 /
+// 21 / 35, 32768 152 / 118 / 99 / 91 / 89 / 93; gradient with 1 / 2 / 4 / 8 / 16 of a side: 2048
+// tokens 31 / 21 / 23 / 27 / 41, 16382 139 / 125 / 115 / 108 / 89.
+int32_t heads_each(int64_t groups, int32_t heads, int32_t all, int32_t most) {
+    if (heads == 0) return 1;
+    const int64_t c = std::min<int64_t>(std::max<int64_t>(groups * all / 768, 1), std::min(most, heads));
+    const int64_t parts = (heads + c - 1) / c;
+    return (int32_t)((heads + parts - 1) / parts);
+}
+
+// The gradient's workgroups: one a tile, or, past 2048 tiles, 1024 that go over all of
+// them, each side's in proportion.
+struct BwdPlan {
+    int32_t q_chunk, k_chunk, q_groups, groups;
+};
+BwdPlan bwd_plan(int64_t rows, int32_t Hq, int32_t Hkv, int32_t lshift) {
+    BwdPlan p;
+    const int64_t tg = ((rows << lshift) + THREADS - 1) / THREADS;
+    p.q_chunk = heads_each(tg, Hq, Hq + Hkv, 16);
+    p.k_chunk = heads_each(tg, Hkv, Hq + Hkv, 16);
+    int64_t qg = tg * ((Hq + p.q_chunk - 1) / p.q_chunk), kg = tg * ((Hkv + p.k_chunk - 1) / p.k_chunk);
+    if (qg + kg > 2048) {
+        const int64_t q = std::max<int64_t>(Hq > 0, 1024 * (int64_t)Hq / (Hq + Hkv));
+        kg = std::min(kg, std::max<int64_t>(Hkv > 0, 1024 - q));
+        qg = std::min(qg, q);
+    }
+    p.q_groups = (int32_t)qg;
+    p.groups = (int32_t)(qg + kg);
+    return p;
+}
+
+// None where each side is one workgroup, which then writes the result.
+int64_t record_bytes(const BwdPlan& p, int32_t d) {
+    return p.q_groups == 1 && p.groups == 2 ? 0 : (int64_t)p.groups * d * 4;
 }
 
 // Sizes that forward, backward and workspace refuse the same way; BF1_OK with *rows == 0
@@ -446,7 +479,7 @@ int bf1_qk_norm_rope(const void* Q, const void* K, const void* q_gain, const voi
     int64_t rows;
     const int bad = bf1::check_sizes(batch, n, Hq, Hkv, head_dim, rot_dim, in_type, &rows);
     if (bad != BF1_OK) return bad;
-    if (!strides || (interleaved & ~1) || !(eps > 0.f) || out_type < 0 || out_type > 1 || gain_type < 0 || gain_type > 1)
+    if (!strides || (interleaved & ~1) || !(eps >= 1e-30f) || out_type < 0 || out_type > 1 || gain_type < 0 || gain_type > 1)
         return BF1_ERR_INVALID_ARG;
     if (in_type == BF1_TYPE_BF16 && out_type != BF1_TYPE_BF16) return BF1_ERR_UNSUPPORTED;
     if (positions_batch_stride != 0 && positions_batch_stride < n) return BF1_ERR_INVALID_ARG;
@@ -459,6 +492,7 @@ int bf1_qk_norm_rope(const void* Q, const void* K, const void* q_gain, const voi
     if (Hq > 0 && Hkv > 0 && (Q_out == K_out || Q_out == K || K_out == Q)) return BF1_ERR_INVALID_ARG;
     const int32_t half = rot_dim / 2;
     bool wide = half % P == 0 && (head_dim - rot_dim) % P == 0;
+    for (const void* g : {q_gain, k_gain}) wide = wide && (!g || bf1::aligned(g, 16));
     bf1::Side side[2];
     for (int i = 0; i < 2; ++i) {
         const int32_t heads = i ? Hkv : Hq;
@@ -479,10 +513,11 @@ int bf1_qk_norm_rope(const void* Q, const void* K, const void* q_gain, const voi
     const int32_t lshift = bf1::team_shift(head_dim, half, (int32_t)P);
     const int64_t groups = ((rows << lshift) + bf1::THREADS - 1) / bf1::THREADS;
     const int32_t heads = Hq + Hkv;
-    const int32_t hb = !wide || groups * heads < 256 ? 1 : 2;
-    const int32_t hsplit = (heads + hb - 1) / hb;
+    const int32_t chunk = bf1::heads_each(groups, heads, heads, 12);
+    const int32_t hsplit = (heads + chunk - 1) / chunk;
+    side[0].chunk = chunk;
     const bf1::Shape z{positions, positions_batch_stride, freqs, (uint32_t)(rows << lshift), (uint32_t)n, (uint32_t)hsplit,
-                       head_dim, half, lshift, gain_type == BF1_TYPE_F32, eps, amplitude};
+                       head_dim, half, lshift, gain_type == BF1_TYPE_F32, eps, amplitude, 1.f / (float)head_dim};
     auto go = [&](auto kern) {
         hipLaunchKernelGGL(kern, dim3((unsigned)(groups * hsplit)), dim3(bf1::THREADS), 0, (hipStream_t)stream, side[0],
                            side[1], z);
@@ -492,8 +527,7 @@ int bf1_qk_norm_rope(const void* Q, const void* K, const void* q_gain, const voi
         using T = decltype(in_c);
         using TO = decltype(out_c);
         constexpr bool I = decltype(inter_c)::value;
-        if (!wide) return go(bf1::norm_rope_kernel<T, TO, I, false, 1>);
-        return hb == 1 ? go(bf1::norm_rope_kernel<T, TO, I, true, 1>) : go(bf1::norm_rope_kernel<T, TO, I, true, 2>);
+        return wide ? go(bf1::norm_rope_kernel<T, TO, I, true>) : go(bf1::norm_rope_kernel<T, TO, I, false>);
     };
     auto types = [&](auto inter_c) {
         if (in_type == BF1_TYPE_BF16) return pick((__bf16)0, (__bf16)0, inter_c);
@@ -511,8 +545,7 @@ int bf1_qk_norm_rope_bwd_workspace_size(int32_t batch, int64_t n, int32_t Hq, in
     *bytes = 0;
     if (rows == 0) return BF1_OK;
     const int32_t lshift = bf1::team_shift(head_dim, rot_dim / 2, in_type == BF1_TYPE_BF16 ? 8 : 4);
-    const int64_t records = std::min(bf1::bwd_tiles(rows, Hq + Hkv, lshift), bf1::MOST_RECORDS);
-    if (records > 1) *bytes = records * 2 * head_dim * 4;
+    *bytes = bf1::record_bytes(bf1::bwd_plan(rows, Hq, Hkv, lshift), head_dim);
     return BF1_OK;
 }
 
@@ -525,7 +558,7 @@ int bf1_qk_norm_rope_bwd(const void* dQ, const void* dK, int32_t grad_type, cons
     int64_t rows;
     const int bad = bf1::check_sizes(batch, n, Hq, Hkv, head_dim, rot_dim, in_type, &rows);
     if (bad != BF1_OK) return bad;
-    if (!strides || (interleaved & ~1) || !(eps > 0.f) || out_type < 0 || out_type > 1 || gain_type < 0 || gain_type > 1 ||
+    if (!strides || (interleaved & ~1) || !(eps >= 1e-30f) || out_type < 0 || out_type > 1 || gain_type < 0 || gain_type > 1 ||
         grad_type < 0 || grad_type > 1)
         return BF1_ERR_INVALID_ARG;
     if (in_type == BF1_TYPE_F32 && grad_type == BF1_TYPE_BF16) return BF1_ERR_UNSUPPORTED;
@@ -534,13 +567,13 @@ int bf1_qk_norm_rope_bwd(const void* dQ, const void* dK, int32_t grad_type, cons
         return BF1_ERR_INVALID_ARG;
     const int64_t esize = in_type == BF1_TYPE_BF16 ? 2 : 4, osize = out_type == BF1_TYPE_BF16 ? 2 : 4;
     const int64_t dsize = grad_type == BF1_TYPE_BF16 ? 2 : 4, gsize = gain_type == BF1_TYPE_BF16 ? 2 : 4, P = 16 / esize;
-    const int32_t half = rot_dim / 2, heads = Hq + Hkv;
+    const int32_t half = rot_dim / 2;
     hipStream_t stm = (hipStream_t)stream;
-    const int sum_groups = (2 * head_dim + bf1::SUM_COLS - 1) / bf1::SUM_COLS;
+    const dim3 sum_groups((unsigned)((head_dim + bf1::SUM_COLS - 1) / bf1::SUM_COLS), 2);
     if (rows == 0) {  // sums over nothing
         if (!dq_gain && !dk_gain) return BF1_OK;
-        hipLaunchKernelGGL(bf1::gain_sum_kernel, dim3(sum_groups), dim3(bf1::SUM_THREADS), 0, stm, nullptr, 0, head_dim,
-                           dq_gain, dk_gain);
+        hipLaunchKernelGGL(bf1::gain_sum_kernel, sum_groups, dim3(bf1::SUM_THREADS), 0, stm, nullptr, 0, 0, head_dim, dq_gain,
+                           dk_gain);
         return bf1::status_of(hipGetLastError());
     }
     if (!bf1::aligned(positions, 4) || !bf1::aligned(freqs, 8)) return BF1_ERR_INVALID_ARG;
@@ -548,6 +581,7 @@ int bf1_qk_norm_rope_bwd(const void* dQ, const void* dK, int32_t grad_type, cons
     if (Hq > 0 && Hkv > 0 && (dQ_in == dK_in || dQ_in == dK || dK_in == dQ || dQ_in == K || dK_in == Q))
         return BF1_ERR_INVALID_ARG;
     bool wide = half % P == 0 && (head_dim - rot_dim) % P == 0;
+    for (const void* g : {q_gain, k_gain}) wide = wide && (!g || bf1::aligned(g, 16));
     bf1::Side side[2];
     for (int i = 0; i < 2; ++i) {
         const int32_t h = i ? Hkv : Hq;
@@ -572,34 +606,35 @@ int bf1_qk_norm_rope_bwd(const void* dQ, const void* dK, int32_t grad_type, cons
                bf1::wide_rows(o, P, osize);
     }
     const int32_t lshift = bf1::team_shift(head_dim, half, (int32_t)P);
-    const int64_t tiles = bf1::bwd_tiles(rows, heads, lshift);
-    const int64_t records = std::min(tiles, bf1::MOST_RECORDS);
-    const bool sums = dq_gain || dk_gain;
-    if (sums && records > 1) {
+    const bf1::BwdPlan plan = bf1::bwd_plan(rows, Hq, Hkv, lshift);
+    side[0].chunk = plan.q_chunk;
+    side[1].chunk = plan.k_chunk;
+    const int64_t need = bf1::record_bytes(plan, head_dim);
+    const bool sums = (dq_gain || dk_gain) && need > 0;
+    if (sums) {
         if (!bf1::aligned(workspace, 16)) return BF1_ERR_INVALID_ARG;
-        if (workspace_bytes < records * 2 * head_dim * 4) return BF1_ERR_BUFFER_TOO_SMALL;
+        if (workspace_bytes < need) return BF1_ERR_BUFFER_TOO_SMALL;
     }
-    const bf1::Shape z{positions, positions_batch_stride, freqs, (uint32_t)(rows << lshift), (uint32_t)n,
-                       (uint32_t)((heads + bf1::BWD_HEADS - 1) / bf1::BWD_HEADS), head_dim, half, lshift,
-                       gain_type == BF1_TYPE_F32, eps, amplitude};
+    const bf1::Shape z{positions, positions_batch_stride, freqs, (uint32_t)(rows << lshift), (uint32_t)n, 0,
+                       head_dim, half, lshift, gain_type == BF1_TYPE_F32, eps, amplitude, 1.f / (float)head_dim};
+    const size_t lds = (size_t)bf1::THREADS / 64 * (1 << lshift) * 2 * P * 4;
     auto go = [&](auto kern) {
-        hipLaunchKernelGGL(kern, dim3((unsigned)records), dim3(bf1::THREADS), 0, stm, side[0], side[1], z, (uint32_t)tiles,
-                           dq_gain, dk_gain, records > 1 ? (float*)workspace : nullptr);
-        if (sums && records > 1)
-            hipLaunchKernelGGL(bf1::gain_sum_kernel, dim3(sum_groups), dim3(bf1::SUM_THREADS), 0, stm,
-                               (const float*)workspace, (int32_t)records, head_dim, dq_gain, dk_gain);
+        hipLaunchKernelGGL(kern, dim3((unsigned)plan.groups), dim3(bf1::THREADS), lds, stm, side[0], side[1], z,
+                           (uint32_t)plan.q_groups, dq_gain, dk_gain, sums ? (float*)workspace : nullptr);
+        if (sums)
+            hipLaunchKernelGGL(bf1::gain_sum_kernel, sum_groups, dim3(bf1::SUM_THREADS), 0, stm, (const float*)workspace,
+                               plan.q_groups, plan.groups, head_dim, dq_gain, dk_gain);
         return bf1::status_of(hipGetLastError());
     };
     auto pick = [&](auto x_c, auto d_c, auto out_c) {
         using T = decltype(x_c);
         using TD = decltype(d_c);
         using TO = decltype(out_c);
-        constexpr int HB = bf1::BWD_HEADS;
         if (interleaved)
-            return wide ? go(bf1::norm_rope_bwd_kernel<T, TD, TO, true, true, HB>)
-                        : go(bf1::norm_rope_bwd_kernel<T, TD, TO, true, false, HB>);
-        return wide ? go(bf1::norm_rope_bwd_kernel<T, TD, TO, false, true, HB>)
-                    : go(bf1::norm_rope_bwd_kernel<T, TD, TO, false, false, HB>);
+            return wide ? go(bf1::norm_rope_bwd_kernel<T, TD, TO, true, true>)
+                        : go(bf1::norm_rope_bwd_kernel<T, TD, TO, true, false>);
+        return wide ? go(bf1::norm_rope_bwd_kernel<T, TD, TO, false, true>)
+                    : go(bf1::norm_rope_bwd_kernel<T, TD, TO, false, false>);
     };
     auto outs = [&](auto x_c, auto d_c) {
         return out_type == BF1_TYPE_BF16 ? pick(x_c, d_c, (__bf16)0) : pick(x_c, d_c, 0.f);
