@@ -22,8 +22,7 @@
 namespace bf1 {
 namespace {
 
-constexpr int WAVES = 4;
-constexpr int THREADS = WAVES * 64;
+constexpr int THREADS = 256;
 constexpr int MOST_NODES = 64;
 
 int status_of(hipError_t e) { return e == hipSuccess ? BF1_OK : BF1_ERR_HIP; }
@@ -42,10 +41,10 @@ __global__ __launch_bounds__(THREADS) void tree_step_kernel(const int32_t* __res
                                                             const int32_t* __restrict__ after, int32_t batch, int32_t rows,
                                                             uint64_t* __restrict__ masks, int32_t* __restrict__ positions) {
     const int lane = threadIdx.x & 63;
-    const int64_t b = (int64_t)blockIdx.x * WAVES + (threadIdx.x >> 6);
+    const int64_t b = (int64_t)blockIdx.x * (THREADS / 64) + (threadIdx.x >> 6);
     if (b >= batch) {  // the rows behind the last tree
         const int64_t first = batch > 0 ? max(token_start[batch], 0) : 0;
-        for (int64_t r = first + (b - batch) * 64 + lane; r < rows; r += ((int64_t)gridDim.x * WAVES - batch) * 64) {
+        for (int64_t r = first + (b - batch) * 64 + lane; r < rows; r += ((int64_t)gridDim.x * (THREADS / 64) - batch) * 64) {
             masks[r] = 0;
             positions[r] = -1;
         }
@@ -77,7 +76,7 @@ __global__ __launch_bounds__(THREADS) void tree_step_kernel(const int32_t* __res
 // Attention
 // ---------------------------------------------------------------------------
 constexpr int UNIT = 32;       // keys of a wave's step
-constexpr int MAX_LIST = 160;  // bound on the earlier blocks that nodes of two neighbouring blocks read, L <= 64
+constexpr int MAX_LIST = 96;   // 28 + 28 + 1 + 32: earlier blocks that nodes of two neighbouring blocks read, L <= 32
 
 struct Tree {
     const __bf16 *Q, *K, *V;
@@ -104,165 +103,182 @@ __device__ __forceinline__ bool finite(float x) { return fabsf(x) < INFINITY; }
 __device__ __forceinline__ float weighed(float x, float w) { return finite(x) ? x * w : x; }
 
 // Whether block i, o blocks before a query's block, is on its route.
-__device__ __forceinline__ bool on_route(int64_t o, int64_t i, int32_t L) {
+__device__ __forceinline__ bool on_route(int32_t o, int32_t i, int32_t L) {
     return o <= L || i == 0 || (o >= 4 && (o & (o - 1)) == 0);
 }
 
-// A wave's view of a sequence's tree.  Bit i of the masks is node i.
-struct Nodes {
-    int32_t start, count;    // first row, rows
-    int64_t len;             // committed tokens
-    int64_t j;               // the block of position len; nodes are in it or in the next
-    uint64_t valid, far;     // nodes with a place; of them those in block j + 1
-    uint64_t mask;           // this lane's node: the drafted keys it reads
-    int32_t drafted;         // keys behind the committed ones that may be read
-    bool near;               // whether nodes of block j + 1 read block j
-};
-template <int PW>
-__device__ __forceinline__ Nodes nodes_of(const Tree& a, int b) {
-    const int lane = threadIdx.x & 63;
-    Nodes t;
-    t.start = min(max(a.token_start[b], 0), a.rows);
-    t.count = min(max(a.token_start[b + 1], t.start), a.rows) - t.start;
-    t.len = max(a.before[b], 0);
-    t.j = t.len / PW;
-    const int32_t most = min(min(t.count, a.max_nodes), MOST_NODES);
-    const int64_t pos = lane < most ? a.positions[t.start + lane] : -1;
-    const bool valid = pos >= t.len && pos < t.len + MOST_NODES;
-    t.valid = __ballot(valid);
-    t.far = __ballot(valid && pos >= (t.j + 1) * PW);
-    t.near = a.dense || on_route(1, t.j, a.L);
-    t.mask = valid ? a.masks[t.start + lane] & t.valid & (t.near ? ~0ull : pos >= (t.j + 1) * PW ? t.far : ~t.far) : 0;
-    t.drafted = t.valid ? 64 - __builtin_clzll(t.valid) : 0;
-    return t;
+// What is the same in all lanes, in a scalar register.
+__device__ __forceinline__ int32_t scalar(int32_t x) { return __builtin_amdgcn_readfirstlane(x); }
+// What no kernel of the call writes: one entry for all lanes comes by a scalar load.
+__device__ __forceinline__ const __attribute__((address_space(4))) int32_t* fixed(const int32_t* p) {
+    return (const __attribute__((address_space(4))) int32_t*)p;
 }
 
-// 16 NT columns (q-heads of neighbouring nodes) of one (sequence, kv-head); the waves
-// take units of 32 keys, WAVES * nsplit apart.
+// A workgroup takes 16 NT CW columns (q-heads of neighbouring nodes) of one (sequence,
+// kv-head) and a split of its keys.  Its four waves are CW column waves, 16 NT columns
+// each, in KW = 4 / CW key groups, which take tiles of 16 CW (CW = 1: 32) keys in turns.
 //
-// Scores S = K Q^T on 16x16x32 tiles: A = K rows straight from memory (lane l: key l % 16,
-// 16-byte chunk 4 s + l / 16), B = Q rows, so lane l holds keys 4 (l / 16) + 0..3 of each
-// of the unit's two tiles and column l % 16: the eight of them are the B operand of
-// O^T += V^T P^T as they stand.  V comes through the wave's own LDS by transpose reads.
-// A weight goes in as two bf16 parts (16 of its bits: what is left out is below 2^-17 of
-// it, the output is rounded to 2^-9), its sum in fp32.
+// Scores S = K Q^T on 16x16x32 tiles: A = K rows (lane l: key l % 16, 16-byte chunk 4 s +
+// l / 16), B = Q rows, so lane l holds keys 4 (l / 16) + 0..3 of each of a unit's two tiles
+// and column l % 16: the eight of them are the B operand of O^T += V^T P^T as they stand.  A
+// weight goes in as two bf16 parts (16 of its bits: what is left out is below 2^-17 of it,
+// the output is rounded to 2^-9), its sum in fp32.
+//
+// CW = 1: K rows go straight to registers, V rows through the wave's own LDS by transpose
+// reads, both asked for a unit ahead.  CW > 1: the waves of a key group share its tiles in
+// LDS, two of them, filled by direct loads while the other one is read; 16-byte chunk c of
+// a K row r lies at c ^ (r & 7), 32-byte slots of V rows at s ^ vslot(r), so that no read has
+// a bank conflict.
+//
+// Bound by the matrix cores where trees are large (weights in two parts make 3/2 of the
+// products; the chip's power limit holds them to some 1 PFLOP/s) and by latency where there
+// is little to read.  Replays of a graph: eight dense lists of 16-32K, up to 64 nodes in groups
+// of 8, pages of 128 291 us (155 GFLOP, 0.4 GB), 32 sequences of 16-32K on the route, up to 32
+// nodes in groups of 2 32 us (93 MB), one sequence of 32K, 16 nodes, 11.1 us with its merge.
 //
 // A key that a row does not read has weight 0 and does nothing, as long as its value is
-// finite.  Where an accumulator is not finite at the end, the wave goes over its units
+// finite.  Where an accumulator is not finite at the end, the wave goes over its keys
 // once more and adds value by value, leaving out what a row does not read.
-template <int D, int G, int PW, int NT>
-__global__ __launch_bounds__(THREADS, 2) void attn_tree_kernel(Tree a) {
+template <int D, int G, int PW, int NT, int CW, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, 2) void attn_tree_kernel(Tree a) {
+    constexpr int THREADS = 64 * WAVES;
+    constexpr int KW = WAVES / CW;
+    constexpr int TILE = CW == 4 ? 64 : 32;       // keys of a key group's turn
     constexpr int KS = D / 32, DT = D / 16, RB = 2 * D;
-    constexpr int UPP = PW / UNIT;                // units of a page
-    constexpr int SEGS = UNIT * RB / 1024;        // direct V loads of a unit
-    constexpr int COLS = 16 * NT, OST = D + 4;
+    constexpr int UPP = PW / TILE;                // tiles of a page
+    constexpr int COLS = 16 * NT * CW, OST = D + 4;
     constexpr int NPG = COLS / G;                 // nodes of a workgroup
-    constexpr int V_BYTES = WAVES * 2 * UNIT * RB, R_BYTES = WAVES * COLS * (OST + 2) * 4;
+    constexpr int K_LDS = CW == 1 ? 0 : TILE * RB, BUF_LDS = K_LDS + TILE * RB;
+    constexpr int SEGS = BUF_LDS / 1024 / CW;     // direct loads of a wave and tile
+    constexpr int V_BYTES = KW * 2 * BUF_LDS, R_BYTES = KW * COLS * (OST + 2) * 4;
     __shared__ __align__(256) u32x4 lds[(V_BYTES > R_BYTES ? V_BYTES : R_BYTES) / 16];
     __shared__ int32_t list[MAX_LIST], sees[MAX_LIST];
 
     const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, quad = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int b = blockIdx.x, h = blockIdx.y;
-    const int s = blockIdx.z % a.nsplit, rg = blockIdx.z / a.nsplit;
-    const int64_t bh = (int64_t)b * a.Hkv + h;
+    const int kg = wave / CW, cw = wave % CW;
+    // Workgroups go to the XCDs in turns, x first: those of the same keys (y) to one, next to
+    // each other.
+    const int rg = blockIdx.y;
+    uint32_t bh = blockIdx.z * 8 + blockIdx.x, s = 0;
+    if (a.nsplit > 1) {
+        const uint32_t work = bh;
+        bh = work / (uint32_t)a.nsplit;
+        s = work - bh * (uint32_t)a.nsplit;
+    }
+    if (bh >= (uint32_t)(a.batch * a.Hkv)) return;
+    const int b = (int)(bh / (uint32_t)a.Hkv), h = (int)bh - b * a.Hkv;
     const int Hq = a.Hkv * G;
-    const Nodes t = nodes_of<PW>(a, b);
-    const int n0 = rg * NPG;
-    if (rg == 0 && s == 0)  // rows past what a tree can have
-        for (int64_t x = tid + (int64_t)min(a.max_nodes, MOST_NODES) * G * D; x < (int64_t)t.count * G * D; x += THREADS) {
-            const int64_t r = (t.start + x / (G * D)) * Hq + h * G + x % (G * D) / D;
+    // The sequence: its rows and how many, its committed tokens, and the block of the first
+    // drafted position; nodes are in that block or in the next.
+    const int32_t start = min(max(fixed(a.token_start)[b], 0), a.rows);
+    const int32_t rows = min(max(fixed(a.token_start)[b + 1], start), a.rows) - start;
+    const int32_t len = max(fixed(a.before)[b], 0), j = len / PW;
+    const int n0 = rg * NPG, most = min(a.max_nodes, MOST_NODES), nodes = min(rows, most);
+    if (rows > most && rg == 0 && s == 0)  // rows past what a tree can have
+        for (int64_t x = tid + (int64_t)most * G * D; x < (int64_t)rows * G * D; x += THREADS) {
+            const int64_t r = (start + x / (G * D)) * Hq + h * G + x % (G * D) / D;
             a.O[r * D + x % D] = (__bf16)__builtin_nanf("");
             if (a.LSE != nullptr && x % D == 0) a.LSE[r] = __builtin_nanf("");
         }
-    if (n0 >= min(min(t.count, a.max_nodes), MOST_NODES)) return;
+    if (n0 >= nodes) return;
 
-    // ---- the earlier blocks that some node reads, their pages and readers ------------
-    // bit 0: nodes of block j read it, bit 1: those of block j + 1
+    // ---- everything that waits for nothing else is asked for at once ------------------
+    const int64_t pos = a.positions[min(start + lane, a.rows - 1)];
+    const uint64_t bits = a.masks[min(start + lane, a.rows - 1)];
     const int32_t* pages = a.table + (int64_t)b * a.max_pages;
-    const bool any_far = t.far != 0;
-    int count = 0;
-    bool bad = t.j >= a.max_pages || t.valid == 0;
-    if (a.dense) {
-        count = bad ? 0 : (int)t.j;
-        for (int e = tid; e < count; e += THREADS) bad |= (uint32_t)pages[e] >= (uint32_t)a.num_pages;
-    } else {
-        const int64_t j = t.j;
-        // lanes 0..27: j - 4, j - 8, ..; 28..55: j + 1 - 4, ..; 56: block 0; then the local ones
-        for (int r0 = 0; r0 < 64 + a.L; r0 += 64) {
-            const int e = r0 + lane;
-            int64_t o;
-            if (e < 56) {
-                o = (int64_t(1) << (2 + e % 28)) - (e >= 28);
-            } else {
-                o = e == 56 ? j : e >= 64 ? e - 63 : 0;
-            }
-            const int64_t i = j - o;
-            bool ok = o > 0 && i >= 0 && !bad;
-            if (e < 64) ok = ok && o > a.L;                           // the local ones come by themselves
-            if (e < 56) ok = ok && i > 0 && (e < 28 || any_far);      // block 0 too
-            if (e >= 64) ok = ok && e - 63 <= a.L;
-            const int see = (on_route(o, i, a.L) ? 1 : 0) | (any_far && on_route(o + 1, i, a.L) ? 2 : 0);
-            ok = ok && see != 0;
-            const uint64_t some = __ballot(ok);
-            const int at = count + __popcll(some & ((1ull << lane) - 1));
-            if (ok && wave == 0 && at < MAX_LIST) {
-                const int32_t p = pages[i];
-                list[at] = p;
-                sees[at] = see;
-            }
-            count += __popcll(some);
-        }
-        count = min(count, MAX_LIST);
-    }
-    const int64_t top = t.len + t.drafted;  // end of the cache's rows that may be read
-    const int rows0 = (int)min(top - t.j * PW, (int64_t)PW);
-    const int rows1 = (int)max(top - (t.j + 1) * PW, (int64_t)0);
-    int32_t page0 = -1, page1 = -1;
-    if (!bad && rows0 > 0) page0 = pages[t.j];
-    if (!bad && rows1 > 0 && t.j + 1 < a.max_pages) page1 = pages[t.j + 1];
-    if (rows0 > 0) bad |= (uint32_t)page0 >= (uint32_t)a.num_pages;
-    if (rows1 > 0) bad |= (uint32_t)page1 >= (uint32_t)a.num_pages;
-    __syncthreads();
-    if (!a.dense)
-        for (int e = lane; e < count; e += 64) bad |= (uint32_t)list[e] >= (uint32_t)a.num_pages;
-    bad = __syncthreads_or(bad);
-
-    // this lane's columns
-    uint64_t mask[NT];
-    bool isfar[NT], valid[NT];
+    const bool inside = j < a.max_pages;  // the table
+    const int32_t page0 = inside ? fixed(pages)[j] : -1, page1 = j + 1 < a.max_pages ? fixed(pages)[j + 1] : -1;
+    // Earlier blocks that nodes of block j or j + 1 may read, o before j: lanes 0..27 4, 8, .., 28..55
+    // 4 - 1, 8 - 1, .., 56 block 0, 57.. the first local ones.
+    int32_t o = lane < 56 ? (1 << (2 + (lane < 28 ? lane : lane - 28))) - (lane >= 28) : lane == 56 ? j : lane - 56;
+    bool ok = inside && o > 0 && o <= j && (lane > 56 ? o <= a.L : o > a.L && (lane == 56 || o < j));
+    int32_t page = a.dense ? (inside && tid < j ? pages[tid] : 0) : ok ? pages[j - o] : -1;
     bf16x8 qf[NT][KS];
 #pragma unroll
     for (int c = 0; c < NT; ++c) {
-        const int node = n0 + (16 * c + col) / G;
-        const int nc = min(node, 63);
-        mask[c] = (uint64_t)__shfl((unsigned long long)t.mask, nc);
-        valid[c] = node < 64 && (t.valid >> nc & 1);
-        isfar[c] = t.far >> nc & 1;
-        const u32x4* src = reinterpret_cast<const u32x4*>(
-            a.Q + ((int64_t)(t.start + min(node, t.count - 1)) * Hq + h * G + col % G) * D);
+        const int node = min(n0 + (16 * (cw * NT + c) + col) / G, rows - 1);
+        const u32x4* src = reinterpret_cast<const u32x4*>(a.Q + ((int64_t)(start + node) * Hq + h * G + col % G) * D);
 #pragma unroll
         for (int k = 0; k < KS; ++k) qf[c][k] = __builtin_bit_cast(bf16x8, src[4 * k + quad]);
     }
 
-    const int early = bad ? 0 : count * UPP;
-    const int units0 = bad ? 0 : (rows0 + UNIT - 1) / UNIT, units1 = bad ? 0 : (rows1 + UNIT - 1) / UNIT;
-    const int units = early + units0 + units1;
-    const int nsb = min(a.nsplit, max(1, (units + WAVES - 1) / WAVES));
-    if (a.nsplit > 1 && s == 0 && rg == 0 && tid == 0) a.used[bh] = nsb;
-    if (s >= nsb) return;
-
-    char* vbuf = reinterpret_cast<char*>(&lds[0]) + wave * (2 * UNIT * RB);
     auto vslot = [](int r) { return D == 128 ? (r & 7) : ((r >> 1) & 3); };
+    char* const buf0 = reinterpret_cast<char*>(&lds[0]) + kg * (2 * BUF_LDS);  // this key group's
     const uint32_t koff = (uint32_t)(col * RB + quad * 16);
+    // Direct loads: 1 KB segment i of a tile is rows 1024 / RB * i ..; K's come before V's.
     uint32_t voff[SEGS];
 #pragma unroll
     for (int i = 0; i < SEGS; ++i) {
-        const int r = i * (1024 / RB) + lane / (RB / 16), pc = lane % (RB / 16);
-        voff[i] = (uint32_t)(r * RB + 16 * (2 * ((pc >> 1) ^ vslot(r)) + (pc & 1)));
+        constexpr int RPS = 1024 / RB;
+        const int seg = (i * CW + cw) % (TILE / RPS);  // i < SEGS / 2: K (CW > 1)
+        const int r = seg * RPS + lane / (RB / 16), pc = lane % (RB / 16);
+        const bool isk = CW > 1 && i < SEGS / 2;
+        voff[i] = (uint32_t)(r * RB + 16 * (isk ? pc ^ (r & 7) : 2 * ((pc >> 1) ^ vslot(r)) + (pc & 1)));
     }
     const int tr = 4 * quad + (col >> 2);
-    const uint32_t vtr = lds_addr(vbuf) + tr * RB + 8 * (col & 3) + 32 * vslot(tr);
+    const uint32_t vtr = lds_addr(buf0) + K_LDS + tr * RB + 8 * (col & 3) + 32 * vslot(tr);
+    uint32_t klds[KS];  // this lane's chunk of k-step k in K rows of LDS
+#pragma unroll
+    for (int k = 0; k < KS; ++k) klds[k] = (uint32_t)(col * RB + 16 * ((4 * k + quad) ^ (col & 7)));
+
+    // ---- the nodes: bit i of a mask is node i -------------------------------------------
+    const bool placed = lane < nodes && pos >= len && pos < (int64_t)len + MOST_NODES;
+    const bool next = placed && pos >= (j + 1) * (int64_t)PW;  // in block j + 1
+    const uint64_t all_valid = __ballot(placed), all_far = __ballot(next);
+    const bool near = a.dense || on_route(1, j, a.L);  // whether nodes of block j + 1 read block j
+    const uint64_t reads = placed ? bits & all_valid & (near ? ~0ull : next ? all_far : ~all_far) : 0;
+    const bool any_far = all_far != 0;
+    uint64_t mask[NT];
+    bool isfar[NT], valid[NT];  // of this lane's columns
+#pragma unroll
+    for (int c = 0; c < NT; ++c) {
+        const int node = n0 + (16 * (cw * NT + c) + col) / G, nc = min(node, 63);
+        mask[c] = (uint64_t)__shfl((unsigned long long)reads, nc);
+        valid[c] = node < 64 && (all_valid >> nc & 1);
+        isfar[c] = all_far >> nc & 1;
+    }
+
+    // ---- the earlier blocks that some node reads, their pages and readers ---------------
+    // bit 0: nodes of block j read it, bit 1: those of block j + 1
+    int count = 0;
+    bool bad = !inside || all_valid == 0;
+    if (a.dense) {
+        count = bad ? 0 : j;
+        bad |= (uint32_t)page >= (uint32_t)a.num_pages;
+        for (int e = tid + THREADS; e < count; e += THREADS) bad |= (uint32_t)pages[e] >= (uint32_t)a.num_pages;
+    } else {
+        for (int l = 0;;) {
+            const int see = (on_route(o, j - o, a.L) ? 1 : 0) | (any_far && on_route(o + 1, j - o, a.L) ? 2 : 0);
+            ok = ok && see != 0;
+            bad |= ok && (uint32_t)page >= (uint32_t)a.num_pages;
+            const uint64_t some = __ballot(ok);
+            const int at = count + __popcll(some & ((1ull << lane) - 1));
+            if (ok && wave == 0) {
+                list[at] = page;
+                sees[at] = see;
+            }
+            count += __popcll(some);
+            l += l == 0 ? 7 : 64;
+            if (l >= a.L) break;
+            o = l + 1 + lane;  // more local ones
+            ok = inside && o <= j && o <= a.L;
+            page = ok ? pages[j - o] : -1;
+        }
+    }
+    const int drafted = all_valid ? 64 - __builtin_clzll(all_valid) : 0;  // keys behind the committed ones that may be read
+    const int top = len % PW + drafted;  // rows from the start of block j on that may be read
+    const int rows0 = min(top, PW), rows1 = max(top - PW, 0);
+    if (rows0 > 0) bad |= (uint32_t)page0 >= (uint32_t)a.num_pages;
+    if (rows1 > 0) bad |= (uint32_t)page1 >= (uint32_t)a.num_pages;
+    bad = scalar(__syncthreads_or(bad));  // and the list is there
+
+    const int early = bad ? 0 : count * UPP;
+    const int units0 = bad ? 0 : (rows0 + TILE - 1) / TILE, units1 = bad ? 0 : (rows1 + TILE - 1) / TILE;
+    const int units = early + units0 + units1;  // tiles
+    const int nsb = min(a.nsplit, max(1, (units + KW - 1) / KW));
+    if (a.nsplit > 1 && s == 0 && rg == 0 && tid == 0) a.used[bh] = nsb;
+    if (s >= nsb) return;
 
     f32x4 acc[NT][DT];
     float m_run[NT], l_run[NT];
@@ -275,100 +291,115 @@ __global__ __launch_bounds__(THREADS, 2) void attn_tree_kernel(Tree a) {
             for (int x = 0; x < DT; ++x) acc[c][x] = f32x4{0.f, 0.f, 0.f, 0.f};
         }
     };
+    const int hop = KW * nsb, u0 = s * KW + kg;
+    // The page of tile u and who reads it; 4: block j, 5: block j + 1.
+    auto page_of = [&](int u) {
+        const int e = min(u, early - 1) / UPP;
+        return u < early ? (a.dense ? fixed(pages)[e] : list[e]) : u < early + units0 ? page0 : page1;
+    };
     struct Where {
         int64_t base;    // element offset of the page's slice
         uint32_t bytes;  // its rows that may be read
-        uint32_t soff;   // the unit in it
-        int kind;        // readers of an earlier page; 4: block j, 5: block j + 1
-        int row;         // first row of the unit in its page
+        uint32_t soff;   // the tile in it
+        int kind, row;   // its readers; the tile's first row
     };
-    auto where = [&](int u) {
+    auto where = [&](int u, int32_t page) {
         Where w;
-        int page;
-        int n = PW;
+        int n = PW, first = 0;
         if (u < early) {
-            const int e = u / UPP;
-            page = a.dense ? pages[e] : list[e];
-            w.kind = a.dense ? 3 : sees[e];
-            w.row = (u - e * UPP) * UNIT;
+            w.kind = a.dense ? 3 : sees[u / UPP];
+            first = u / UPP * UPP;
         } else if (u < early + units0) {
-            page = page0;
             n = rows0;
             w.kind = 4;
-            w.row = (u - early) * UNIT;
+            first = early;
         } else {
-            page = page1;
             n = rows1;
             w.kind = 5;
-            w.row = (u - early - units0) * UNIT;
+            first = early + units0;
         }
-        page = __builtin_amdgcn_readfirstlane(page);
+        w.row = (u - first) * TILE;
         w.kind = __builtin_amdgcn_readfirstlane(w.kind);
-        w.base = ((int64_t)page * a.Hkv + h) * PW * D;
-        w.bytes = (uint32_t)n * RB;
+        w.base = ((int64_t)__builtin_amdgcn_readfirstlane(page) * a.Hkv + h) * PW * D;
+        w.bytes = (uint32_t)__builtin_amdgcn_readfirstlane(n) * RB;
         w.soff = (uint32_t)w.row * RB;
         return w;
     };
     u32x4 kr[2][KS];
-    auto load_k = [&](const Where& w) {
+    auto load_k = [&](const Where& w, int sub) {  // 32 keys from memory
         const __amdgpu_buffer_rsrc_t r = head_rsrc(a.K + w.base, w.bytes);
 #pragma unroll
         for (int x = 0; x < 2; ++x)
 #pragma unroll
             for (int k = 0; k < KS; ++k)
-                kr[x][k] = __builtin_amdgcn_raw_buffer_load_b128(r, koff + 16 * x * RB + 64 * k, w.soff, 0);
+                kr[x][k] = __builtin_amdgcn_raw_buffer_load_b128(r, koff + 16 * x * RB + 64 * k, w.soff + sub * UNIT * RB, 0);
     };
-    auto load_v = [&](const Where& w, int buf) {
-        const __amdgpu_buffer_rsrc_t r = head_rsrc(a.V + w.base, w.bytes);
-#pragma unroll
-        for (int i = 0; i < SEGS; ++i) load_lds16(r, vbuf + buf * (UNIT * RB) + i * 1024, voff[i], w.soff);
+    auto load_piece = [&](const Where& w, int buf, int i) {  // direct load i of this wave
+        const bool isk = CW > 1 && i < SEGS / 2;
+        char* dst = buf0 + buf * BUF_LDS + (i * CW + cw) * 1024;
+        const __amdgpu_buffer_rsrc_t r = head_rsrc((isk ? a.K : a.V) + w.base, w.bytes);
+        if constexpr (CW == 1)
+            load_lds16(r, dst, voff[i], w.soff);
+        else
+            load_lds_async<16>(r, dst, voff[i], w.soff);
     };
-    // Scores of the unit in kr, masked, in log2 units.
-    auto scores = [&](const Where& w, f32x4 (&sc)[NT][2]) {
+    auto load_tile = [&](const Where& w, int buf) {
 #pragma unroll
-        for (int c = 0; c < NT; ++c)
-#pragma unroll
-            for (int x = 0; x < 2; ++x) {
-                f32x4 y = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int k = 0; k < KS; ++k)
-                    y = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kr[x][k]), qf[c][k], y, 0, 0, 0);
-                sc[c][x] = y;
-            }
+        for (int i = 0; i < SEGS; ++i) load_piece(w, buf, i);
+    };
+    // Raw scores of keys from `from` on, -infinity where a row does not read a key.
+    auto mask_scores = [&](const Where& w, int from, auto& sc) {
+        constexpr int N = sizeof(sc[0]) / sizeof(f32x4);  // 16-key tiles
         if (w.kind < 4) {
+            if (w.kind == 3 || (w.kind == 1 && !any_far)) return;
 #pragma unroll
             for (int c = 0; c < NT; ++c) {
                 const bool see = isfar[c] ? w.kind & 2 : w.kind & 1;
 #pragma unroll
-                for (int x = 0; x < 2; ++x)
+                for (int x = 0; x < N; ++x)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) sc[c][x][r] = see ? sc[c][x][r] * a.c_log2 : -INFINITY;
+                    for (int r = 0; r < 4; ++r) sc[c][x][r] = see ? sc[c][x][r] : -INFINITY;
             }
             return;
         }
-        // the unit's first key, counted from the first drafted one
-        const int first = (int)((t.j + (w.kind - 4)) * PW + w.row - t.len) + 4 * quad;
+        // the first key, counted from the first drafted one
+        const int first = (w.kind - 4) * PW + w.row + from - len % PW + 4 * quad;
 #pragma unroll
         for (int c = 0; c < NT; ++c) {
-            const bool held = !isfar[c] || t.near;
+            const bool held = !isfar[c] || near;
 #pragma unroll
-            for (int x = 0; x < 2; ++x)
+            for (int x = 0; x < N; ++x)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const int n = first + 16 * x + r;
                     const bool see = n < 0 ? held : n < 64 && (mask[c] >> (n & 63) & 1);
-                    sc[c][x][r] = see ? sc[c][x][r] * a.c_log2 : -INFINITY;
+                    sc[c][x][r] = see ? sc[c][x][r] : -INFINITY;
                 }
         }
     };
-    // Scores -> weights in place; what came before is rescaled.
-    auto soften = [&](int c, f32x4 (&sc)[2], auto safe) {
+    auto multiply = [&](auto& sc, auto sub_c) {  // by the K rows in kr: 16-key tiles 2 sub and 2 sub + 1
+        constexpr int X = 2 * decltype(sub_c)::value;
+#pragma unroll
+        for (int c = 0; c < NT; ++c) sc[c][X] = sc[c][X + 1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < KS; ++k)
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+#pragma unroll
+                for (int c = 0; c < NT; ++c)
+                    sc[c][X + x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kr[x][k]), qf[c][k],
+                                                                           sc[c][X + x], 0, 0, 0);
+    };
+    // Scores -> weights in place (log2 units, less the largest so far); what came before is
+    // rescaled.
+    auto soften = [&](int c, auto& sc, auto safe) {
+        constexpr int N = sizeof(sc) / sizeof(f32x4);
         float mx = -INFINITY;
 #pragma unroll
-        for (int x = 0; x < 2; ++x)
+        for (int x = 0; x < N; ++x)
 #pragma unroll
             for (int r = 0; r < 4; ++r) mx = fmaxf(mx, sc[x][r]);
-        const float m_new = fmaxf(m_run[c], col_max(mx));
+        const float m_new = fmaxf(m_run[c], col_max(mx) * a.c_log2);
         const float m_use = m_new == -INFINITY ? 0.f : m_new;
         if (__any(m_new > m_run[c])) {
             const float alpha = __builtin_amdgcn_exp2f(m_run[c] - m_use);
@@ -381,92 +412,197 @@ __global__ __launch_bounds__(THREADS, 2) void attn_tree_kernel(Tree a) {
             m_run[c] = m_new;
         }
 #pragma unroll
-        for (int x = 0; x < 2; ++x)
+        for (int x = 0; x < N; ++x)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                sc[x][r] = __builtin_amdgcn_exp2f(sc[x][r] - m_use);
+                sc[x][r] = __builtin_amdgcn_exp2f(fmaf(sc[x][r], a.c_log2, -m_use));
                 l_run[c] += sc[x][r];
             }
     };
-    const int hop = WAVES * nsb, u0 = s * WAVES + wave;
-    // One unit: its K rows are in flight to kr and its V rows to buffer BUF.  The next
-    // unit's V rows are asked for before the wait for them, its K rows as soon as the
-    // scores have taken kr.
-    auto step = [&](int u, const Where& w, Where& nx, auto buf_c) {
-        constexpr int BUF = decltype(buf_c)::value;
-        const bool more = u + hop < units;
-        if (more) {
-            nx = where(u + hop);
-            load_v(nx, BUF ^ 1);
-            __builtin_amdgcn_sched_barrier(0);
-            __builtin_amdgcn_s_waitcnt(0x0F70 | SEGS);
-        } else {
-            __builtin_amdgcn_s_waitcnt(VMCNT0);
+    // Weights of 32 keys as two bf16 parts.
+    auto split = [&](const f32x4* sc, bf16x8& hi, bf16x8& lo) {
+        u32x4 h, l;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+            typedef float f32x2 __attribute__((ext_vector_type(2)));
+            const f32x2 w = {sc[x / 2][x % 2 * 2], sc[x / 2][x % 2 * 2 + 1]};
+            h[x] = __builtin_bit_cast(uint32_t, __builtin_convertvector(w, bf16x2));
+            const f32x2 rest = {w[0] - __uint_as_float(h[x] << 16), w[1] - __uint_as_float(h[x] & 0xffff0000u)};
+            l[x] = __builtin_bit_cast(uint32_t, __builtin_convertvector(rest, bf16x2));
         }
-        __builtin_amdgcn_sched_barrier(0);
-        f32x4 sc[NT][2];
-        scores(w, sc);
-        if (more) load_k(nx);
-        __builtin_amdgcn_sched_barrier(0);
-        bf16x8 hi[NT], lo[NT];
+        hi = __builtin_bit_cast(bf16x8, h);
+        lo = __builtin_bit_cast(bf16x8, l);
+    };
+    // Their products with 16-wide tiles d and d + 1 of 32 V rows: two transpose reads each.
+    auto both = [&](int d, const bf16x8 (&hi)[NT], const bf16x8 (&lo)[NT], u32x2 v0, u32x2 v1, u32x2 v2, u32x2 v3) {
+        const bf16x8 vt[2] = {__builtin_bit_cast(bf16x8, u32x4{v0[0], v0[1], v1[0], v1[1]}),
+                              __builtin_bit_cast(bf16x8, u32x4{v2[0], v2[1], v3[0], v3[1]})};
 #pragma unroll
-        for (int c = 0; c < NT; ++c) {
-            soften(c, sc[c], std::false_type{});
+        for (int part = 0; part < 2; ++part)
 #pragma unroll
-            for (int x = 0; x < 2; ++x)
+            for (int y = 0; y < 2; ++y)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    hi[c][4 * x + r] = (__bf16)sc[c][x][r];
-                    lo[c][4 * x + r] = (__bf16)(sc[c][x][r] - (float)hi[c][4 * x + r]);
-                }
-        }
-#pragma unroll
-        for (int d0 = 0; d0 < DT; d0 += 2) {
-            u32x2 v0[2], v1[2];
-            asm volatile(
-                "ds_read_b64_tr_b16 %0, %4 offset:%6\n\tds_read_b64_tr_b16 %1, %4 offset:%7\n\t"
-                "ds_read_b64_tr_b16 %2, %5 offset:%6\n\tds_read_b64_tr_b16 %3, %5 offset:%7\n\t"
-                "s_waitcnt lgkmcnt(0)"
-                : "=&v"(v0[0]), "=&v"(v1[0]), "=&v"(v0[1]), "=&v"(v1[1])
-                : "v"(vtr ^ (32 * d0)), "v"(vtr ^ (32 * d0 + 32)), "i"(BUF * UNIT * RB), "i"(BUF * UNIT * RB + 16 * RB)
-                : "memory");
-#pragma unroll
-            for (int y = 0; y < 2; ++y) {
-                const bf16x8 vt = __builtin_bit_cast(bf16x8, u32x4{v0[y][0], v0[y][1], v1[y][0], v1[y][1]});
-#pragma unroll
-                for (int c = 0; c < NT; ++c) {
-                    acc[c][d0 + y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, hi[c], acc[c][d0 + y], 0, 0, 0);
-                    acc[c][d0 + y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, lo[c], acc[c][d0 + y], 0, 0, 0);
-                }
-            }
-        }
+                for (int c = 0; c < NT; ++c)
+                    acc[c][d + y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt[y], part ? lo[c] : hi[c], acc[c][d + y], 0, 0,
+                                                                           0);
     };
     clear();
-    if (u0 < units) {
-        Where w = where(u0), nx = w;
-        load_v(w, 0);
-        load_k(w);
-        for (int u = u0; u < units; u += 2 * hop) {
-            step(u, w, nx, std::integral_constant<int, 0>{});
-            if (u + hop < units) step(u + hop, nx, w, std::integral_constant<int, 1>{});
+    if constexpr (CW == 1) {
+        // One unit: its K rows are in flight to kr and its V rows to buffer BUF.  The next
+        // unit's V rows are asked for before the wait for them, its K rows as soon as the
+        // scores have taken kr, and the page after that.
+        int32_t coming = 0;
+        auto step = [&](int u, const Where& w, Where& nx, auto buf_c) {
+            constexpr int BUF = decltype(buf_c)::value;
+            const bool more = u + hop < units;
+            if (more) {
+                nx = where(u + hop, coming);
+                load_tile(nx, BUF ^ 1);
+                __builtin_amdgcn_sched_barrier(0);
+                __builtin_amdgcn_s_waitcnt(0x0F70 | SEGS);
+            } else {
+                __builtin_amdgcn_s_waitcnt(VMCNT0);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            f32x4 sc[NT][2];
+            multiply(sc, std::integral_constant<int, 0>{});
+            if (more) {
+                if (u + 2 * hop < units) coming = page_of(u + 2 * hop);
+                __builtin_amdgcn_sched_barrier(0);
+                load_k(nx, 0);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            mask_scores(w, 0, sc);
+            bf16x8 hi[NT], lo[NT];
+#pragma unroll
+            for (int c = 0; c < NT; ++c) {
+                soften(c, sc[c], std::false_type{});
+                split(sc[c], hi[c], lo[c]);
+            }
+#pragma unroll
+            for (int d = 0; d < DT; d += 2) {
+                u32x2 v0, v1, v2, v3;
+                asm volatile(
+                    "ds_read_b64_tr_b16 %0, %4 offset:%6\n\tds_read_b64_tr_b16 %1, %4 offset:%7\n\t"
+                    "ds_read_b64_tr_b16 %2, %5 offset:%6\n\tds_read_b64_tr_b16 %3, %5 offset:%7\n\t"
+                    "s_waitcnt lgkmcnt(0)"
+                    : "=&v"(v0), "=&v"(v1), "=&v"(v2), "=&v"(v3)
+                    : "v"(vtr ^ (32 * d)), "v"(vtr ^ (32 * d + 32)), "i"(BUF * BUF_LDS), "i"(BUF * BUF_LDS + 16 * RB)
+                    : "memory");
+                both(d, hi, lo, v0, v1, v2, v3);
+            }
+        };
+        if (u0 < units) {
+            Where w = where(u0, page_of(u0)), nx = w;
+            if (u0 + hop < units) coming = page_of(u0 + hop);
+            load_tile(w, 0);
+            load_k(w, 0);
+            for (int u = u0; u < units; u += 2 * hop) {
+                step(u, w, nx, std::integral_constant<int, 0>{});
+                if (u + hop < units) step(u + hop, nx, w, std::integral_constant<int, 1>{});
+            }
         }
-        bool fine = true;
+    } else {
+        // A tile is asked for a turn ahead, a load here and there among the products of the one
+        // before it: all at once, behind the barrier, they kept the waves from their LDS reads
+        // (eight lists of 32K, 64 nodes in groups of 8, one workgroup a compute unit 1260 us,
+        // now 940; two 440, 430).  Where there is none any more the loads read nothing.
+        const int turns = max(0, (units - s * KW + hop - 1) / hop);  // of every key group, the last one maybe without keys
+        auto ahead = [&](int u) {
+            Where w = where(min(u, units - 1), page_of(min(u, units - 1)));
+            w.bytes = (uint32_t)scalar(u < units ? (int32_t)w.bytes : 0);
+            return w;
+        };
+        auto step = [&](int i, auto buf_c) {
+            constexpr int BUF = decltype(buf_c)::value;
+            const int u = u0 + i * hop;
+            // this tile has come, for all waves, and nobody reads the other one any more
+            __builtin_amdgcn_s_waitcnt(VMCNT0);
+            asm volatile("" ::: "memory");
+            __syncthreads();
+            if (u >= units) return;
+            const Where w = where(u, 0), nx = ahead(u + hop);
+            auto ask = [&](int from, int to) {
+#pragma unroll
+                for (int i = from; i < to; ++i) load_piece(nx, BUF ^ 1, i);
+            };
+            const char* kb = buf0 + BUF * BUF_LDS;
+            constexpr int SUBS = TILE / UNIT;
+            f32x4 sc[NT][2 * SUBS];
+            auto score = [&](auto sub_c) {
+                constexpr int SUB = decltype(sub_c)::value;
+#pragma unroll
+                for (int x = 0; x < 2; ++x)
+#pragma unroll
+                    for (int k = 0; k < KS; ++k)
+                        kr[x][k] = *reinterpret_cast<const u32x4*>(kb + klds[k] + (SUB * UNIT + 16 * x) * RB);
+                multiply(sc, sub_c);
+            };
+            score(std::integral_constant<int, 0>{});
+            ask(0, SEGS / 4);
+            if constexpr (SUBS > 1) score(std::integral_constant<int, 1>{});
+            ask(SEGS / 4, SEGS / 2);
+            mask_scores(w, 0, sc);
+            // V operands of a half come while the weights are made, or the other half's products run
+            constexpr int HALF = DT / 2;
+            u32x2 v[2][HALF][2];
+            auto fetch = [&](int to, int sub, int half) {
+#pragma unroll
+                for (int d = 0; d < HALF; ++d)
+#pragma unroll
+                    for (int y = 0; y < 2; ++y)
+                        v[to][d][y] = lds_read_tr16((vtr ^ (32 * (half * HALF + d))) + BUF * BUF_LDS + (sub * UNIT + 16 * y) * RB);
+            };
+            fetch(0, 0, 0);
+#pragma unroll
+            for (int c = 0; c < NT; ++c) soften(c, sc[c], std::false_type{});
+            ask(SEGS / 2, SEGS / 4 * 3);
+#pragma unroll
+            for (int sub = 0; sub < SUBS; ++sub) {
+                bf16x8 hi[NT], lo[NT];
+#pragma unroll
+                for (int c = 0; c < NT; ++c) split(sc[c] + 2 * sub, hi[c], lo[c]);
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    if (half == 0 || sub + 1 < SUBS) fetch(half ^ 1, sub + half, half ^ 1);
+#pragma unroll
+                    for (int d = 0; d < HALF; d += 2)
+                        both(half * HALF + d, hi, lo, v[half][d][0], v[half][d][1], v[half][d + 1][0], v[half][d + 1][1]);
+                    if (sub == 0 && half == 0) ask(SEGS / 4 * 3, SEGS);
+                }
+            }
+        };
+        if (turns > 0) load_tile(ahead(u0), 0);
+        for (int i = 0; i < turns; i += 2) {
+            step(i, std::integral_constant<int, 0>{});
+            if (i + 1 < turns) step(i + 1, std::integral_constant<int, 1>{});
+        }
+        __builtin_amdgcn_s_waitcnt(VMCNT0);  // before the tiles' place in LDS is used again
+        asm volatile("" ::: "memory");
+    }
+    if (u0 < units) {
+        // 0 times anything finite is 0
+        f32x4 odd[2] = {};
 #pragma unroll
         for (int c = 0; c < NT; ++c)
 #pragma unroll
             for (int x = 0; x < DT; ++x)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) fine = fine && finite(acc[c][x][r]);
-        if (!__all(fine)) {
+                for (int r = 0; r < 4; ++r) odd[x & 1][r] = fmaf(acc[c][x][r], 0.f, odd[x & 1][r]);
+        const float any = ((odd[0][0] + odd[1][0]) + (odd[0][1] + odd[1][1])) + ((odd[0][2] + odd[1][2]) + (odd[0][3] + odd[1][3]));
+        if (__any(any != 0.f)) {
             clear();
-            for (int u = u0; u < units; u += hop) {
-                const Where z = where(u);
-                load_k(z);
+            for (int u = u0 * (TILE / UNIT); u < units * (TILE / UNIT); ++u) {
+                const int sub = u % (TILE / UNIT);
+                if ((u / (TILE / UNIT) - u0) % hop != 0) continue;
+                const Where z = where(u / (TILE / UNIT), page_of(u / (TILE / UNIT)));
+                load_k(z, sub);
                 __builtin_amdgcn_sched_barrier(0);
                 __builtin_amdgcn_s_waitcnt(VMCNT0);
                 __builtin_amdgcn_sched_barrier(0);
                 f32x4 sc[NT][2];
-                scores(z, sc);
+                multiply(sc, std::integral_constant<int, 0>{});
+                mask_scores(z, sub * UNIT, sc);
                 const __amdgpu_buffer_rsrc_t vr = head_rsrc(a.V + z.base, z.bytes);
 #pragma unroll
                 for (int c = 0; c < NT; ++c) {
@@ -487,7 +623,8 @@ __global__ __launch_bounds__(THREADS, 2) void attn_tree_kernel(Tree a) {
                         const bool reads = __shfl(sr, from) != -INFINITY;
 #pragma unroll
                         for (int y = 0; y < DT; ++y) {
-                            const u32x2 v = __builtin_amdgcn_raw_buffer_load_b64(vr, key * RB + 32 * y + 8 * quad, z.soff, 0);
+                            const u32x2 v = __builtin_amdgcn_raw_buffer_load_b64(
+                                vr, (sub * UNIT + key) * RB + 32 * y + 8 * quad, z.soff, 0);
 #pragma unroll
                             for (int q = 0; q < 4; ++q) {
                                 const float f = __uint_as_float(q & 1 ? v[q / 2] & 0xffff0000u : v[q / 2] << 16);
@@ -501,43 +638,46 @@ __global__ __launch_bounds__(THREADS, 2) void attn_tree_kernel(Tree a) {
         }
     }
 
-    // ---- the waves' results through LDS (over the V units) -----------------------------
-    float* r_o = reinterpret_cast<float*>(&lds[0]);  // [wave][column][OST]
-    float* r_m = r_o + WAVES * COLS * OST;           // [wave][column][max, sum]
+    // ---- the key groups' results through LDS (over the tiles) ---------------------------
+    float* r_o = reinterpret_cast<float*>(&lds[0]);  // [key group][column][OST]
+    float* r_m = r_o + KW * COLS * OST;              // [key group][column][max, sum]
     __syncthreads();
 #pragma unroll
     for (int c = 0; c < NT; ++c) {
         const float l = col_sum(l_run[c]);
-        float* dst = r_o + (wave * COLS + 16 * c + col) * OST + 4 * quad;
+        const int at = kg * COLS + 16 * (cw * NT + c) + col;
+        float* dst = r_o + at * OST + 4 * quad;
 #pragma unroll
         for (int x = 0; x < DT; ++x) *reinterpret_cast<f32x4*>(dst + 16 * x) = acc[c][x];
         if (quad == 0) {
-            r_m[(wave * COLS + 16 * c + col) * 2] = m_run[c];
+            r_m[at * 2] = m_run[c];
             // a row without a place, or without a page that it needs, shows
-            r_m[(wave * COLS + 16 * c + col) * 2 + 1] = bad || !valid[c] ? __builtin_nanf("") : l;
+            r_m[at * 2 + 1] = bad || !valid[c] ? __builtin_nanf("") : l;
         }
     }
     __syncthreads();
-    const int64_t rec = (bh * a.groups + rg) * a.nsplit + s;
-    for (int x = tid; x < COLS * D / 4; x += THREADS) {
-        const int e = x / (D / 4), d = x % (D / 4) * 4;
-        float M = -INFINITY, l = 0.f;
+    const int64_t rec = ((int64_t)bh * a.groups + rg) * a.nsplit + s;
+    constexpr int PER = THREADS / (D / 4);  // columns at a time, four dims a thread
+    const int d = tid % (D / 4) * 4;
 #pragma unroll
-        for (int w = 0; w < WAVES; ++w) M = fmaxf(M, r_m[(w * COLS + e) * 2]);
+    for (int e0 = 0; e0 < COLS; e0 += PER) {
+        const int e = e0 + tid / (D / 4);
+        float m[KW], M = -INFINITY, l = 0.f;
+#pragma unroll
+        for (int w = 0; w < KW; ++w) M = fmaxf(M, m[w] = r_m[(w * COLS + e) * 2]);
         const float M_use = M == -INFINITY ? 0.f : M;
         f32x4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int w = 0; w < WAVES; ++w) {
-            const float scale = __builtin_amdgcn_exp2f(r_m[(w * COLS + e) * 2] - M_use);
+        for (int w = 0; w < KW; ++w) {
+            const float scale = KW == 1 ? 1.f : __builtin_amdgcn_exp2f(m[w] - M_use);
             const f32x4 y = *reinterpret_cast<const f32x4*>(r_o + (w * COLS + e) * OST + d);
             l = fmaf(r_m[(w * COLS + e) * 2 + 1], scale, l);
 #pragma unroll
             for (int r = 0; r < 4; ++r) o[r] += weighed(y[r], scale);
         }
+        if (n0 + e / G >= nodes) continue;
         if (nsb == 1) {
-            const int node = n0 + e / G;
-            if (node >= min(t.count, min(a.max_nodes, MOST_NODES))) continue;
-            const int64_t row = (int64_t)(t.start + node) * Hq + h * G + e % G;
+            const int64_t row = (int64_t)(start + n0 + e / G) * Hq + h * G + e % G;
             const float inv = l == 0.f ? 0.f : 1.f / l;
             *reinterpret_cast<bf16x4*>(a.O + row * D + d) =
                 bf16x4{(__bf16)(o[0] * inv), (__bf16)(o[1] * inv), (__bf16)(o[2] * inv), (__bf16)(o[3] * inv)};
@@ -555,9 +695,9 @@ __global__ __launch_bounds__(THREADS, 2) void attn_tree_kernel(Tree a) {
 
 // Sum of the splits' records, in split order: 256 threads, four dims each, of as many
 // columns.
-template <int D, int G, int NT>
+template <int D, int G, int COLS>
 __global__ __launch_bounds__(THREADS) void merge_tree_kernel(Tree a) {
-    constexpr int COLS = 16 * NT, TPC = D / 4, PER = THREADS / TPC;  // columns of a workgroup
+    constexpr int TPC = D / 4, PER = THREADS / TPC;  // columns of a workgroup
     constexpr int PARTS = COLS / PER;
     const int part = blockIdx.x % PARTS;
     const int64_t x = blockIdx.x / PARTS;  // (sequence, kv-head, group)
@@ -613,37 +753,57 @@ __global__ __launch_bounds__(THREADS) void merge_tree_kernel(Tree a) {
 }
 
 // What a call's launches go by, from its sizes alone.
+//
+// Columns of a workgroup: 16 for little work, where a short path counts (the code of a
+// wave that runs once comes to it no faster than it is fetched), 64 or 128 for more, where
+// a key row should serve many columns.  Work: 16-column tiles times 32-key tiles.  us in
+// replays of a graph, 16 / 32 / 64 / 128 columns with their best splits, heads of 128: one
+// sequence of 32K on the route, 64 nodes in groups of 2 14.7 / 17.1 / 18.0 / 20.9 (work 2100),
+// two 18.1 / 18.3 / 19.6 / 22.5 (4200), four 23.5 / 23.4 / 21.7 / 25.5 (8400), 32 of them 112 / 71 /
+// 49 / 53 (68000); dense lists of 8100, one 32.6 / 31.4 / 28.6 / 34.3 (16000), eight 162 / 105 / 84 /
+// 75 (130000).
+//
+// Splits fill 256 workgroups, one a compute unit; 128 columns over long lists 512 (eight
+// lists of 32K, 64 nodes in groups of 8: 475 / 290).  64 columns run as workgroups of eight
+// waves, four key groups, where there are no more than 256 of them (32 sequences of 32K, 32 nodes
+// in groups of 2 34.0, with four waves 40.8; 64 sequences 72.7 and 62.0).
 struct Plan {
-    int32_t nt, groups, nsplit;
+    int32_t cols, groups, waves, nsplit;
     int64_t bytes;
 };
-constexpr int64_t PLACES = 512;  // workgroups that run at once
-constexpr int MOST_SPLITS = 64;
+constexpr int64_t PLACES = 256, MOST_SPLITS = 32;
 Plan plan_of(int32_t batch, int32_t max_nodes, int32_t Hkv, int32_t G, int32_t d, int32_t B, int64_t max_pages, int32_t L,
              int32_t dense) {
     Plan p;
     const int32_t cols = std::min(max_nodes, MOST_NODES) * G;
-    p.nt = cols <= 16 ? 1 : 2;
-    p.groups = (cols + 16 * p.nt - 1) / (16 * p.nt);
-    const int64_t pages = dense ? max_pages : route_pred_count(max_pages - 1, L) + 2;
-    const int64_t rounds = (pages * (B / UNIT) + WAVES - 1) / WAVES;
-    const int64_t rows = std::max<int64_t>(1, (int64_t)batch * Hkv * p.groups);
-    int64_t n = std::min<int64_t>(std::min<int64_t>(PLACES / rows, rounds / 2), MOST_SPLITS);
+    const int64_t tiles = (dense ? max_pages : route_pred_count(max_pages - 1, L) + 2) * (B / UNIT);
+    const int64_t bh = (int64_t)batch * Hkv;
+    const double work = (double)bh * ((cols + 15) / 16) * tiles;
+    p.cols = cols <= 16 || work <= 8000 ? 16 : cols <= 32 ? 32 : cols <= 64 || work <= 100000 ? 64 : 128;
+    p.groups = (cols + p.cols - 1) / p.cols;
+    const int64_t rows = std::max<int64_t>(1, bh * p.groups);
+    p.waves = p.cols == 64 && rows <= PLACES ? 8 : 4;
+    // turns of a key group with one split
+    const int64_t turns = p.cols == 128 ? (tiles + 1) / 2 : (tiles + p.waves - 1) / (p.cols == 64 ? p.waves / 2 : p.waves);
+    int64_t n = PLACES / rows;
+    if (p.cols == 128 && turns * rows >= 8 * 2 * PLACES) n = 2 * PLACES / rows;
+    n = std::min(std::min(n, turns), MOST_SPLITS);
     p.nsplit = n < 2 ? 1 : (int32_t)n;
     p.bytes = p.nsplit <= 1 ? 0
-                            : (rows * p.nsplit * 16 * p.nt * (d + 2) * 4 + 15) / 16 * 16 +
-                                  ((int64_t)batch * Hkv * 4 + 15) / 16 * 16;
+                            : (rows * p.nsplit * p.cols * (d + 2) * 4 + 15) / 16 * 16 + (bh * 4 + 15) / 16 * 16;
     return p;
 }
 
-template <int D, int G, int PW, int NT>
+template <int D, int G, int PW, int NT, int CW, int WAVES>
 hipError_t launch(const Tree& a, hipStream_t s) {
-    hipLaunchKernelGGL((attn_tree_kernel<D, G, PW, NT>),
-                       dim3((unsigned)a.batch, (unsigned)a.Hkv, (unsigned)(a.nsplit * a.groups)), dim3(THREADS), 0, s, a);
+    constexpr int COLS = 16 * NT * CW;
+    const int64_t work = ((int64_t)a.batch * a.Hkv * a.nsplit + 7) / 8;
+    hipLaunchKernelGGL((attn_tree_kernel<D, G, PW, NT, CW, WAVES>), dim3(8, (unsigned)a.groups, (unsigned)work),
+                       dim3(64 * WAVES), 0, s, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.nsplit <= 1) return e;
-    constexpr int PARTS = 16 * NT / (THREADS / (D / 4));
-    hipLaunchKernelGGL((merge_tree_kernel<D, G, NT>), dim3((unsigned)((int64_t)a.batch * a.Hkv * a.groups * PARTS)),
+    constexpr int PARTS = COLS / (THREADS / (D / 4));
+    hipLaunchKernelGGL((merge_tree_kernel<D, G, COLS>), dim3((unsigned)((int64_t)a.batch * a.Hkv * a.groups * PARTS)),
                        dim3(THREADS), 0, s, a);
     return hipGetLastError();
 }
@@ -657,7 +817,7 @@ int check_sizes(int32_t batch, int32_t max_nodes, int32_t Hq, int32_t Hkv, int32
     if ((d != 64 && d != 128) || (B != 64 && B != 128) || (G != 1 && G != 2 && G != 4 && G != 8))
         return BF1_ERR_UNSUPPORTED;
     if ((!dense && L > 32) || Hkv > 65535 || max_nodes > MOST_NODES) return BF1_ERR_UNSUPPORTED;
-    if ((int64_t)batch * Hkv > (int64_t(1) << 20)) return BF1_ERR_UNSUPPORTED;
+    if ((int64_t)batch * Hkv > (int64_t(1) << 18)) return BF1_ERR_UNSUPPORTED;
     return BF1_OK;
 }
 
@@ -677,7 +837,7 @@ int bf1_tree_step(const int32_t* parents, const int32_t* token_start, const int3
         for (const int32_t* p : {token_start, seq_lens_before, seq_lens})
             if (!bf1::aligned(p, 4)) return BF1_ERR_INVALID_ARG;
     // a wave per tree, and at least one for the rows behind them
-    hipLaunchKernelGGL(bf1::tree_step_kernel, dim3((unsigned)(batch / bf1::WAVES + 1)), dim3(bf1::THREADS), 0,
+    hipLaunchKernelGGL(bf1::tree_step_kernel, dim3((unsigned)(batch / (bf1::THREADS / 64) + 1)), dim3(bf1::THREADS), 0,
                        (hipStream_t)stream, parents, token_start, seq_lens_before, seq_lens, batch, (int32_t)rows,
                        (uint64_t*)masks, positions);
     return bf1::status_of(hipGetLastError());
@@ -741,7 +901,13 @@ int bf1_attn_tree(const void* Q, const void* K_pages, const void* V_pages, const
     hipStream_t s = (hipStream_t)stream;
     auto nt = [&](auto d_c, auto g_c, auto pw_c) {
         constexpr int D = decltype(d_c)::value, GG = decltype(g_c)::value, PW = decltype(pw_c)::value;
-        return p.nt == 1 ? bf1::launch<D, GG, PW, 1>(a, s) : bf1::launch<D, GG, PW, 2>(a, s);
+        switch (p.cols) {
+            case 16: return bf1::launch<D, GG, PW, 1, 1, 4>(a, s);
+            case 32: return bf1::launch<D, GG, PW, 2, 1, 4>(a, s);
+            case 64:
+                return p.waves == 8 ? bf1::launch<D, GG, PW, 2, 2, 8>(a, s) : bf1::launch<D, GG, PW, 2, 2, 4>(a, s);
+            default: return bf1::launch<D, GG, PW, 2, 4, 4>(a, s);
+        }
     };
     auto pw = [&](auto d_c, auto g_c) {
         return B == 64 ? nt(d_c, g_c, std::integral_constant<int, 64>{}) : nt(d_c, g_c, std::integral_constant<int, 128>{});

@@ -185,6 +185,29 @@ def test_attn_tree_sizes(nodes, G):
         c.check(c.run(max_nodes=nodes - 2), most=nodes - 2)
 
 
+@pytest.mark.parametrize("L", [0, 2])
+@pytest.mark.parametrize("copies,Hq,Hkv,nodes,d,B", [(5, 16, 2, 64, 64, 64), (5, 8, 4, 64, 64, 64), (2, 8, 4, 64, 128, 64),
+                                                     (5, 8, 4, 16, 64, 128), (4, 8, 1, 64, 128, 128)])
+def test_attn_tree_columns(copies, Hq, Hkv, nodes, d, B, L):
+    """Batches whose rows run 128, 64 (in workgroups of four and of eight waves) and 32 columns
+    at a time: trees that reach into the next block, sequences at blocks' ends."""
+    rng = np.random.default_rng(copies + nodes)
+    held = [j * B + o for j in (0, 1, 2, 3, 5, 9, 16) for o in (3, B - 1)] * copies
+    counts = [int(rng.integers(nodes * 3 // 4, nodes + 1)) if rng.random() < 0.5 else int(rng.integers(0, 4)) for _ in held]
+    counts[0] = nodes
+    c = Case(held, counts, Hq, Hkv, d, B, seed=nodes, deep=True, width=20000 if Hq // Hkv == 8 else 0)
+    c.check(c.run(L, max_nodes=nodes), L)
+
+
+@pytest.mark.parametrize("width", [20, 200, 2000, 20000])
+@pytest.mark.parametrize("G,nodes", [(1, 40), (4, 16), (8, 33)])
+def test_attn_tree_wide_tables(width, G, nodes):
+    """The same lists under ever wider tables, that is with every number of columns and splits."""
+    c = Case([700, 64, 200, 0], [nodes, 3, nodes // 2, 5], 2 * G, 2, 64, 64, seed=width, width=width)
+    for dense in (True, False):
+        c.check(c.run(dense=dense, max_nodes=nodes), dense=dense)
+
+
 def test_attn_tree_long_lists_split():
     c = Case([9000, 4097, 64], [5, 16, 2], 8, 4, 128, 64, seed=4)
     for kw in (dict(dense=True, L=0), dict(L=2)):
@@ -224,25 +247,26 @@ def test_attn_tree_rows_without_a_place():
     assert c.run()[0].isnan().all()
 
 
+@pytest.mark.parametrize("Hq,nodes,width", [(4, 16, 0), (2, 20, 20000), (4, 20, 20000), (8, 40, 20000)])  # 16 to 128 columns
 @pytest.mark.parametrize("where", ["k", "v"])
-def test_attn_tree_values_that_are_not_finite(where):
+def test_attn_tree_values_that_are_not_finite(where, Hq, nodes, width):
     """A key or value that is not finite reaches the rows that read it, as the formula has
     it, and no other."""
-    B, d = 64, 64
-    c = Case([300, 127], [16, 16], 4, 2, d, B, seed=7, deep=False)
+    B, d, G = 64, 64, Hq // 2
+    make = lambda: Case([300, 127], [nodes, 16], Hq, 2, d, B, seed=7, width=width)  # noqa: E731
+    c, clean = make(), make()
     x = c.k if where == "k" else c.v
-    # in drafted node 5 of sequence 0, and in a committed key that rows of block 1 of sequence 1
-    # read but rows of block 2 do not: none of the route is, so a key of the tree's again
+    # drafted node 5 of sequence 0 and node 3 of sequence 1
     x[c.table[0, 305 // B], 1, 305 % B, 3] = float("inf")
     x[c.table[1, 130 // B], 0, 130 % B, 9] = float("nan") if where == "v" else float("inf")
-    clean = Case([300, 127], [16, 16], 4, 2, d, B, seed=7, deep=False)
-    got, want = c.run(), clean.run()
+    dense = width > 0
+    got, want = c.run(dense=dense), clean.run(dense=dense)
     o, lse, w = f64(got[0]), f64(got[1]), f64(want[0])
     for b, node, head, dim in ((0, 5, 1, 3), (1, 3, 0, 9)):
         for r in range(c.start[b], c.start[b + 1]):
             reads = c.masks[r] >> node & 1
-            for h in range(4):
-                hit = reads and h // 2 == head
+            for h in range(Hq):
+                hit = reads and h // G == head
                 if not hit:
                     assert np.isfinite(o[r, h]).all() and np.abs(o[r, h] - w[r, h]).max() < 2.0 ** -6, (b, r, h)
                 elif where == "v":
@@ -252,9 +276,10 @@ def test_attn_tree_values_that_are_not_finite(where):
                     assert np.isnan(o[r, h]).all() or np.abs(o[r, h]).max() < 10
 
 
-def test_attn_tree_infinity_under_a_small_weight():
+@pytest.mark.parametrize("Hq,nodes,width", [(2, 4, 0), (2, 16, 30000), (2, 32, 30000), (4, 64, 30000)])
+def test_attn_tree_infinity_under_a_small_weight(Hq, nodes, width):
     """An infinite value is there at any weight, also across units, waves and splits."""
-    c = Case([5000], [4], 2, 1, 128, 64, seed=9, scale=4.0)
+    c = Case([5000], [nodes], Hq, 1, 128, 64, seed=9, scale=4.0, width=width)
     page = c.table[0, 7]
     c.v[page, 0, 20, 5] = float("-inf")
     got = c.run(dense=True)

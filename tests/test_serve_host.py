@@ -182,7 +182,7 @@ def test_attn_tree_refusals(lib):
                      ({8: 0}, INVALID), ({9: 0}, INVALID), ({13: 1 << 31}, UNSUPPORTED), ({0: FAKE + 8}, INVALID),
                      ({1: None}, INVALID), ({3: FAKE + 4}, INVALID), ({4: None}, INVALID), ({5: FAKE + 2}, INVALID),
                      ({6: None}, INVALID), ({7: None}, INVALID), ({10: FAKE}, INVALID), ({11: FAKE + 1}, INVALID),
-                     ({22: 0}, SMALL), ({21: FAKE + 4}, INVALID), ({12: 1 << 20}, UNSUPPORTED),
+                     ({22: 0}, SMALL), ({21: FAKE + 4}, INVALID), ({12: (1 << 15) + 1}, UNSUPPORTED),
                      ({12: 1, 15: 65536, 16: 65536}, UNSUPPORTED)]:
         assert lib.bf1_attn_tree(*_with(ok, at)) == want, at
     for at in ({12: 0}, {13: 0}, {14: 0}):
@@ -192,7 +192,7 @@ def test_attn_tree_refusals(lib):
     assert lib.bf1_attn_tree_workspace_size(3, 16, 16, 8, 128, 64, 9, 2, 0, None) == INVALID
     assert lib.bf1_attn_tree_workspace_size(3, 16, 16, 8, 128, 96, 9, 2, 0, ctypes.byref(size)) == UNSUPPORTED
     assert bf1.attn_tree_workspace_size(0, 16, 16, 8, 128, 64, 9) == 0
-    assert bf1.attn_tree_workspace_size(1 << 17, 64, 8, 8, 128, 64, 9) == 0  # rows enough without splits
+    assert bf1.attn_tree_workspace_size(1 << 15, 64, 8, 8, 128, 64, 9) == 0  # rows enough without splits
 
 
 def test_page_refusals(lib):
