@@ -31,8 +31,12 @@ bool launchable(int64_t blocks) { return blocks < (int64_t(1) << 32) / THREADS; 
 // order, below its head.
 //
 // Two kernels: counts and table rows, one workgroup per place (integer atomics, whose
-// order does not change a sum); then one workgroup that gives growing blocks their
-// owners, takes pages for copies and collects what is free.
+// order does not change a sum), which also leaves each place's length and growing page;
+// then one workgroup that gives growing blocks their owners, takes pages for copies and
+// collects what is free.  Bound by latency: some 8 bytes per table entry and page, in
+// loads that wait for each other.  Replays of a graph with the copies: 32 places of 2-4K
+// tokens 10.9 us, 512 of 1-2K 12.7 (18.6 and 25.8 with owners found through the counts in
+// memory and a scan of the pages that began after that).
 struct Fork {
     int32_t batch;
     const int32_t *seq_lens, *sources, *keep_lens, *table;
@@ -76,6 +80,11 @@ __global__ __launch_bounds__(THREADS) void fork_rows_kernel(Fork f) {
         }
         if (i < full && p >= 0 && p < f.num_pages) atomicAdd(f.shares + p, 1);
     }
+    if (threadIdx.x == 0) {
+        f.lens_out[b] = (int32_t)n;
+        const int32_t p = n & (B - 1) ? from[full] : -1;
+        f.copy_from[b] = p < f.num_pages ? max(p, -1) : -1;  // the page of a block that is still written
+    }
 }
 
 constexpr int OWN_THREADS = 1024;
@@ -104,96 +113,148 @@ __device__ __forceinline__ int32_t group_scan(int32_t x, int32_t* part, int32_t*
     return before + inc - x;
 }
 
+constexpr int PER = 16;                         // pages of a thread and round
+constexpr int32_t ROUND = OWN_THREADS * PER;
+constexpr int SLOT_BITS = 12;
+
+// shares of pages p0 + PER tid .., 0 behind the last one.
+__device__ __forceinline__ void load_shares(const Fork& f, int32_t p0, int32_t (&x)[PER]) {
+    const int32_t p = p0 + (int32_t)threadIdx.x * PER;
+    if (f.num_pages - p >= PER) {
+        typedef int32_t i32x4 __attribute__((ext_vector_type(4), aligned(4)));
+#pragma unroll
+        for (int i = 0; i < PER; i += 4) {
+            const i32x4 v = *reinterpret_cast<const i32x4*>(f.shares + p + i);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) x[i + k] = v[k];
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) x[i] = p + i < f.num_pages ? f.shares[p + i] : 0;
+    }
+}
+
 __global__ __launch_bounds__(OWN_THREADS) void fork_own_kernel(Fork f) {
     __shared__ int32_t part[OWN_WAVES];
+    __shared__ int32_t asked[OWN_THREADS], slots[1 << SLOT_BITS];
+    __shared__ uint32_t kept[ROUND / 32];  // a bit per page of the first round
     const int32_t tid = threadIdx.x;
     const int32_t head = min(max(*f.free_head, 0), f.num_free);
-    // Growing blocks whose page has no other holder: the first place that asks for one
-    // leaves its number, INT32_MIN + place, in the count.
-    for (int32_t b = tid; b < f.batch; b += OWN_THREADS) {
-        int32_t src;
-        const int64_t n = goes_on(f, b, &src);
-        int32_t page = -1;
-        if (n & ((1 << f.shift) - 1)) {
-            page = f.table[(int64_t)src * f.width + (n >> f.shift)];
-            if (page < 0 || page >= f.num_pages) page = -1;
-        }
-        f.copy_from[b] = page;
-        if (page >= 0 && __hip_atomic_load(f.shares + page, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) < 0)
-            atomicMin(f.shares + page, INT32_MIN + b);
-    }
-    __threadfence();
-    __syncthreads();
+    int32_t share[PER];
+    load_shares(f, 0, share);
     int32_t taken = 0;
-    for (int32_t b0 = 0; b0 < f.batch; b0 += OWN_THREADS) {
-        const int32_t b = b0 + tid;
-        int32_t page = -1, src = -1;
-        int64_t n = 0;
-        bool copies = false;
-        if (b < f.batch) {
-            n = goes_on(f, b, &src);
-            page = f.copy_from[b];
-            copies = page >= 0 && __hip_atomic_load(f.shares + page, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) !=
-                                      INT32_MIN + b;
-        }
+    // Place b, which asks for page `page` (-1: none) and keeps it or takes a new one.
+    auto settle = [&](int32_t b, int32_t page, bool copies) {
         int32_t all;
         const int32_t rank = taken + group_scan(copies, part, &all);
         if (b < f.batch) {
-            const int32_t at = (int32_t)(n >> f.shift), rows = (int32_t)(n & ((1 << f.shift) - 1));
-            int32_t from = -1, to = -1;
+            int32_t from = -1, to = -1, rows = 0;
             if (copies) {
+                int32_t n = f.lens_out[b];
+                rows = n & ((1 << f.shift) - 1);
                 if (rank < f.num_free - head) to = max(f.free_pages[head + rank], -1);
-                if (to >= 0)
-                    from = page;
-                else
-                    n -= rows;  // no page for its partial block
-                f.table_out[(int64_t)b * f.width + at] = to;
+                f.table_out[(int64_t)b * f.width + (n >> f.shift)] = to;
+                from = to >= 0 ? page : -1;
+                if (to < 0) f.lens_out[b] = n - rows;  // no page for its partial block
             }
-            f.lens_out[b] = (int32_t)n;
+            f.copy_from[b] = from;
             f.copy_to[b] = to;
             f.copy_rows[b] = to >= 0 ? rows : 0;
-            if (copies) f.copy_from[b] = from;
         }
         taken += all;
+    };
+    if (f.batch <= OWN_THREADS) {  // a place per thread: what they ask for meets in LDS
+        const int32_t page = tid < f.batch ? f.copy_from[tid] : -1;
+        const bool wants = page >= 0 && f.shares[page] < 0;
+        asked[tid] = page;
+        if (tid < ROUND / 32) kept[tid] = 0;
+        // The first place that asks for a page: the least one of a slot wins it, and knows its
+        // page's other places by their page; who lost to another page goes on to another slot.
+        bool open = wants, first = false;
+        for (uint32_t mix = 0x9E3779B1u; __syncthreads_or(open); mix += 0x3C6EF372u) {
+            const uint32_t slot = (uint32_t)page * mix >> (32 - SLOT_BITS);
+            if (open) slots[slot] = OWN_THREADS;
+            __syncthreads();
+            if (open) atomicMin(slots + slot, tid);
+            __syncthreads();
+            if (open) {
+                const int32_t winner = slots[slot];
+                first = winner == tid;
+                open = asked[winner] != page;
+            }
+        }
+        if (first) {  // the page has its one holder again
+            f.shares[page] = 0;
+            if (page < ROUND) atomicOr(kept + page / 32, 1u << page % 32);
+        }
+        settle(tid, page, page >= 0 && !first);
+    } else {
+        // The first place that asks for a page leaves its number, INT32_MIN + place, in the count.
+        for (int32_t b = tid; b < f.batch; b += OWN_THREADS) {
+            const int32_t page = f.copy_from[b];
+            if (page >= 0 && __hip_atomic_load(f.shares + page, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) < 0)
+                atomicMin(f.shares + page, INT32_MIN + b);
+        }
+        __threadfence();
+        __syncthreads();
+        for (int32_t b0 = 0; b0 < f.batch; b0 += OWN_THREADS) {
+            const int32_t b = b0 + tid, page = b < f.batch ? f.copy_from[b] : -1;
+            const bool first = page >= 0 && __hip_atomic_load(f.shares + page, __ATOMIC_RELAXED,
+                                                              __HIP_MEMORY_SCOPE_AGENT) == INT32_MIN + b;
+            settle(b, page, page >= 0 && !first);
+            if (first) f.copy_rows[b] = INT32_MIN + page;  // kept, for the next loop
+        }
+        __syncthreads();
+        for (int32_t b = tid; b < f.batch; b += OWN_THREADS) {
+            const int32_t x = f.copy_rows[b];
+            if (x >= 0) continue;
+            __hip_atomic_store(f.shares + (x - INT32_MIN), 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            f.copy_rows[b] = 0;
+        }
+        __threadfence();
+        __syncthreads();
+        load_shares(f, 0, share);
+        if (tid < ROUND / 32) kept[tid] = 0;
+        __syncthreads();
     }
     taken = min(taken, f.num_free - head);
-    __syncthreads();
-    // A kept block's page has its one holder again.
-    for (int32_t b = tid; b < f.batch; b += OWN_THREADS) {
-        const int32_t page = f.copy_from[b];
-        if (page >= 0 && f.copy_to[b] < 0) {
-            __hip_atomic_store(f.shares + page, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            f.copy_from[b] = -1;
+    // Free pages, counted, and put below the head in ascending order.  What this workgroup wrote
+    // to the counts of later rounds is there: behind the barriers of its own scans.
+    auto free_bits = [&](int32_t p0) {
+        const uint32_t k = p0 == 0 ? kept[tid / 2] >> tid % 2 * PER : 0u;
+        uint32_t bits = 0;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) bits |= (uint32_t)(share[i] < 0 && !(k >> i & 1)) << i;
+        return bits;
+    };
+    uint32_t bits = free_bits(0);
+    int32_t freed = __popc(bits), all;
+    if (f.num_pages > ROUND) {
+        __threadfence();
+        __syncthreads();
+        for (int32_t p0 = ROUND; p0 < f.num_pages; p0 += ROUND) {
+            load_shares(f, p0, share);
+            freed += __popc(free_bits(p0));
         }
     }
-    __threadfence();
-    __syncthreads();
-    // Free pages: counted, then put below the head in ascending order.
-    constexpr int PER = 16;  // pages of a thread and round
-    int32_t freed = 0;
-    for (int32_t p0 = 0; p0 < f.num_pages; p0 += OWN_THREADS * PER)
-#pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            const int64_t p = (int64_t)p0 + i * OWN_THREADS + tid;
-            freed += p < f.num_pages && __hip_atomic_load(f.shares + p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) < 0;
-        }
-    int32_t all;
-    group_scan(freed, part, &all);
+    const int32_t rank = group_scan(freed, part, &all);
     const int32_t start = max(head + taken - all, 0);
-    int32_t at = start;
-    if (all > 0)
-        for (int32_t p0 = 0; p0 < f.num_pages && at < start + all; p0 += OWN_THREADS) {
-            const int64_t p = (int64_t)p0 + tid;
-            const bool is = p < f.num_pages &&
-                            __hip_atomic_load(f.shares + p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) < 0;
-            int32_t here;
-            const int32_t rank = group_scan(is, part, &here);
-            if (is) {
-                __hip_atomic_store(f.shares + p, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                if (at + rank < head + taken) f.free_pages[at + rank] = (int32_t)p;
-            }
-            at += here;
+    int32_t base = start;
+    for (int32_t p0 = 0; p0 < f.num_pages; p0 += ROUND) {
+        if (p0 > 0) {
+            load_shares(f, p0, share);
+            bits = free_bits(p0);
         }
+        int32_t before = rank, here = all;
+        if (f.num_pages > ROUND) before = group_scan(__popc(bits), part, &here);
+        int32_t at = base + before;
+        for (uint32_t x = bits; x; x &= x - 1, ++at) {
+            const int32_t p = p0 + tid * PER + __builtin_ctz(x);
+            f.shares[p] = 0;
+            if (at < head + taken) f.free_pages[at] = p;
+        }
+        base += here;
+    }
     if (tid == 0) *f.head_out = start;
 }
 

@@ -694,42 +694,42 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_tree_kernel(Tree a) {
 }
 
 // Sum of the splits' records, in split order: 256 threads, four dims each, of as many
-// columns.
+// columns.  Up to eight records are asked for before what says how many there are.
 template <int D, int G, int COLS>
 __global__ __launch_bounds__(THREADS) void merge_tree_kernel(Tree a) {
     constexpr int TPC = D / 4, PER = THREADS / TPC;  // columns of a workgroup
-    constexpr int PARTS = COLS / PER;
-    const int part = blockIdx.x % PARTS;
-    const int64_t x = blockIdx.x / PARTS;  // (sequence, kv-head, group)
-    const int rg = (int)(x % a.groups);
-    const int64_t bh = x / a.groups;
-    const int b = (int)(bh / a.Hkv), h = (int)(bh - (int64_t)b * a.Hkv);
-    const int e = part * PER + threadIdx.x / TPC, d = threadIdx.x % TPC * 4;
-    const int node = rg * (COLS / G) + e / G;
-    const int start = min(max(a.token_start[b], 0), a.rows);
-    const int count = min(max(a.token_start[b + 1], start), a.rows) - start;
-    if (node >= min(count, min(a.max_nodes, MOST_NODES))) return;
-    const int nsb = a.used[bh];
-    if (nsb <= 1) return;  // the result stands there already
-    const int64_t rec0 = x * a.nsplit;
+    const int rg = blockIdx.y;
+    const int64_t bh = blockIdx.z;
+    const int b = (int)(blockIdx.z / (uint32_t)a.Hkv), h = (int)bh - b * a.Hkv;
+    const int e = blockIdx.x * PER + threadIdx.x / TPC, d = threadIdx.x % TPC * 4;
+    const int64_t rec0 = (bh * a.groups + rg) * a.nsplit;
     const float* ml = a.ws + (int64_t)a.batch * a.Hkv * a.groups * a.nsplit * COLS * D + (rec0 * COLS + e) * 2;
     const float* src = a.ws + (rec0 * COLS + e) * D + d;
-    float M = -INFINITY, l = 0.f;
-    f32x4 o = {0.f, 0.f, 0.f, 0.f};
     constexpr int U = 8;
-    for (int q0 = 0; q0 < nsb; q0 += U) {
-        float mq[U], lq[U];
-        f32x4 oq[U];
+    float mq[U], lq[U];
+    f32x4 oq[U];
+    auto load = [&](int q0) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int64_t q = min(q0 + u, nsb - 1);
+            const int64_t q = min(q0 + u, a.nsplit - 1);
             mq[u] = ml[q * COLS * 2];
             lq[u] = ml[q * COLS * 2 + 1];
             oq[u] = *reinterpret_cast<const f32x4*>(src + q * COLS * D);
         }
+    };
+    load(0);
+    const int nsb = fixed(a.used)[bh];
+    const int start = min(max(fixed(a.token_start)[b], 0), a.rows);
+    const int count = min(max(fixed(a.token_start)[b + 1], start), a.rows) - start;
+    const int node = rg * (COLS / G) + e / G;
+    if (node >= min(count, min(a.max_nodes, MOST_NODES))) return;  // used was not written where there is none
+    if (nsb <= 1) return;                                          // the result stands there already
+    float M = -INFINITY, l = 0.f;
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    for (int q0 = 0;;) {
         float mm = M;
 #pragma unroll
-        for (int u = 0; u < U; ++u) mm = fmaxf(mm, mq[u]);
+        for (int u = 0; u < U; ++u) mm = q0 + u < nsb ? fmaxf(mm, mq[u]) : mm;
         const float use = mm == -INFINITY ? 0.f : mm;
         const float alpha = __builtin_amdgcn_exp2f(M - use);
         l *= alpha;
@@ -744,6 +744,9 @@ __global__ __launch_bounds__(THREADS) void merge_tree_kernel(Tree a) {
             for (int r = 0; r < 4; ++r) o[r] += weighed(oq[u][r], w);
         }
         M = mm;
+        q0 += U;
+        if (q0 >= nsb) break;
+        load(q0);
     }
     const int64_t row = (int64_t)(start + node) * (a.Hkv * G) + h * G + e % G;
     const float inv = l == 0.f ? 0.f : 1.f / l;
@@ -803,7 +806,7 @@ hipError_t launch(const Tree& a, hipStream_t s) {
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.nsplit <= 1) return e;
     constexpr int PARTS = COLS / (THREADS / (D / 4));
-    hipLaunchKernelGGL((merge_tree_kernel<D, G, COLS>), dim3((unsigned)((int64_t)a.batch * a.Hkv * a.groups * PARTS)),
+    hipLaunchKernelGGL((merge_tree_kernel<D, G, COLS>), dim3(PARTS, (unsigned)a.groups, (unsigned)(a.batch * a.Hkv)),
                        dim3(THREADS), 0, s, a);
     return hipGetLastError();
 }

@@ -109,7 +109,8 @@ def test_sequences_fork_grow_and_end(batch, pages, B, seed):
     assert pool.head == 0 and sorted(pool.free) == list(range(pages))
 
 
-@pytest.mark.parametrize("batch,width", [(1, 1), (1, 300), (255, 3), (1023, 2), (1025, 2), (2100, 3)])
+@pytest.mark.parametrize("batch,width", [(1, 1), (1, 300), (255, 3), (1023, 2), (1024, 3), (1025, 2), (2100, 3),
+                                         (180, 100), (1100, 20)])
 def test_page_fork_matches_the_oracle(batch, width):
     rng = np.random.default_rng(batch)
     B = 64
