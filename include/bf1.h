@@ -525,7 +525,7 @@ int bf1_qk_norm_rope_bwd(const void* dQ, const void* dK, int32_t grad_type, cons
  *   Q, O      : [rows, Hq, head_dim] bf16, packed; LSE [rows, Hq] fp32, may be NULL
  *   masks     : any; bits of nodes without a place do nothing
  *   K_pages, V_pages, page_table : bf1_decode_attn's and bf1_decode_plan's
- *   max_nodes : largest tree of the call, at most 64
+ *   max_nodes : largest tree of the call, 1 to 64
  * A row whose position is not within 64 from its sequence's length on (also -1), whose
  * number is max_nodes or more, or whose sequence lacks a page that some node of it reads,
  * gets NaN; a row that reads nothing 0 and LSE -infinity.  Rows behind the last tree are

@@ -813,7 +813,7 @@ hipError_t launch(const Tree& a, hipStream_t s) {
 
 int check_sizes(int32_t batch, int32_t max_nodes, int32_t Hq, int32_t Hkv, int32_t d, int32_t B, int32_t max_pages,
                 int32_t L, int32_t dense) {
-    if (batch < 0 || max_nodes < 0 || Hkv < 1 || Hq < 1 || Hq % Hkv != 0 || max_pages < 1 || (dense & ~1) ||
+    if (batch < 0 || max_nodes < 1 || Hkv < 1 || Hq < 1 || Hq % Hkv != 0 || max_pages < 1 || (dense & ~1) ||
         (!dense && L < 0))
         return BF1_ERR_INVALID_ARG;
     const int32_t G = Hq / Hkv;
@@ -851,7 +851,7 @@ int bf1_attn_tree_workspace_size(int32_t batch, int32_t max_nodes, int32_t Hq, i
     if (!bytes) return BF1_ERR_INVALID_ARG;
     const int bad = bf1::check_sizes(batch, max_nodes, Hq, Hkv, head_dim, B, max_pages_per_seq, L, dense);
     if (bad != BF1_OK) return bad;
-    *bytes = batch == 0 || max_nodes == 0
+    *bytes = batch == 0
                  ? 0
                  : bf1::plan_of(batch, max_nodes, Hkv, Hq / Hkv, head_dim, B, max_pages_per_seq, L, dense).bytes;
     return BF1_OK;
@@ -866,7 +866,7 @@ int bf1_attn_tree(const void* Q, const void* K_pages, const void* V_pages, const
     if (bad != BF1_OK) return bad;
     if (rows < 0 || num_pages < 1) return BF1_ERR_INVALID_ARG;
     if (rows >= (int64_t(1) << 31)) return BF1_ERR_UNSUPPORTED;
-    if (batch == 0 || rows == 0 || max_nodes == 0) return BF1_OK;
+    if (batch == 0 || rows == 0) return BF1_OK;
     for (const void* p : {Q, K_pages, V_pages, (const void*)O})
         if (!bf1::aligned(p, 16)) return BF1_ERR_INVALID_ARG;
     if (O == Q || !bf1::aligned(masks, 8)) return BF1_ERR_INVALID_ARG;

@@ -217,6 +217,19 @@ def test_norm_rope_strided_rows(d, shift):
     assert all(torch.equal(a, b) for a, b in zip(got, want))
 
 
+def test_norm_rope_strides_past_32_bits():
+    flat = torch.zeros(3 * 2 ** 30 + 4096, dtype=torch.bfloat16, device="cuda")
+    q = flat.as_strided((4, 2, 128), (2 ** 30, 128, 1))
+    k = flat[1024:].as_strided((4, 1, 128), (2 ** 30, 128, 1))
+    q.copy_(normal(1, 4, 2, 128))
+    k.copy_(normal(2, 4, 1, 128))
+    gain, (f, _) = 1 + 0.3 * normal(3, 128, dtype=torch.float32), bf1.rope_freqs(128)
+    pos = i32([5, 6, 7, 8])
+    want = bf1.qk_norm_rope(q.contiguous(), k.contiguous(), gain, gain, pos, f)
+    got = bf1.qk_norm_rope(q, k, gain, gain, pos, f, q_out=flat[2048:].as_strided(q.shape, q.stride()), k_out=k)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
 def test_norm_rope_in_place():
     q, k, qg, kg, pos, freqs, f = case(2, 51, 5, 2, 128, 64, torch.float32)
     a = bf1.qk_norm_rope(q, k, qg, kg, i32(pos), f)

@@ -350,7 +350,7 @@ def test_attn_tree_refusals():
                      (dict(out=torch.empty(3, 4, 64, device="cuda")), "out")]:
         with pytest.raises(ValueError, match=why):
             bf1.attn_tree(**{**ok, **bad})
-    for bad in (dict(max_nodes=65), dict(max_nodes=-1), dict(L=33), dict(L=-1), dict(q=ok["q"][:, :3].contiguous())):
+    for bad in (dict(max_nodes=65), dict(max_nodes=0), dict(L=33), dict(L=-1), dict(q=ok["q"][:, :3].contiguous())):
         with pytest.raises(bf1.BF1Error):
             bf1.attn_tree(**{**ok, **bad})
 
@@ -408,3 +408,23 @@ def test_kv_compact_missing_pages_buffers_and_refusals():
         bf1.kv_compact(**{**ok, "accepted": torch.zeros((1, 65), dtype=torch.int32, device="cuda")})
     with pytest.raises(bf1.BF1Error):
         bf1.kv_compact(**ok, out=ok["lens_before"])
+
+
+def test_caches_past_32_bits():
+    """Pages behind 2^32 elements: attention, moved rows and copies there as at the front."""
+    Hkv, d, B, P = 8, 128, 64, 66000  # 4.3e9 elements each
+    k, v = (torch.empty((P, Hkv, B, d), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    c = Case([500, 70], [9, 6], 16, Hkv, d, B, seed=21, spare=0)
+    n = c.k.shape[0]
+    k[P - n:], v[P - n:] = torch.nan_to_num(c.k, nan=9.0, posinf=9.0).cuda(), torch.nan_to_num(c.v, nan=9.0, posinf=9.0).cuda()
+    far = np.where(c.table < 0, c.table, c.table + P - n)
+    args = signed(c.masks), i32(c.pos), i32(c.held), i32(c.start)
+    got = bf1.attn_tree(c.q.cuda(), k, v, *args, i32(far))
+    c.check(got)
+    front = k[P - n:].clone(), v[P - n:].clone()
+    acc, lens, after = i32([[0, 3, 8], [1, 2, -1]]), i32(c.held), i32([509, 76])
+    a = bf1.kv_compact(k, v, acc, lens, after, i32(far))
+    b = bf1.kv_compact(*front, acc, lens, after, i32(c.table))
+    assert torch.equal(a, b) and torch.equal(k[P - n:], front[0]) and torch.equal(v[P - n:], front[1])
+    bf1.kv_copy(k, v, i32([P - 1, P - 2]), i32([P - n - 1, 0]), i32([64, 33]))
+    assert torch.equal(k[P - n - 1], k[P - 1]) and torch.equal(v[0, :, :33], v[P - 2, :, :33])

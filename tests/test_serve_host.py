@@ -176,7 +176,7 @@ def test_tree_step_refusals(lib):
 def test_attn_tree_refusals(lib):
     ok = [FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, 900, 7, FAKE + 4096, FAKE + 8192, 3, 20, 16, 16, 8, 128, 64, 2, 0, FAKE,
           1 << 40, None]
-    for at, want in [({12: -1}, INVALID), ({13: -1}, INVALID), ({14: -1}, INVALID), ({14: 65}, UNSUPPORTED), ({15: 0}, INVALID),
+    for at, want in [({12: -1}, INVALID), ({13: -1}, INVALID), ({14: 0}, INVALID), ({14: 65}, UNSUPPORTED), ({15: 0}, INVALID),
                      ({15: 17}, INVALID), ({15: 24}, UNSUPPORTED), ({15: 128}, UNSUPPORTED), ({17: 96}, UNSUPPORTED),
                      ({18: 32}, UNSUPPORTED), ({19: -1}, INVALID), ({19: 33}, UNSUPPORTED), ({20: 2}, INVALID),
                      ({8: 0}, INVALID), ({9: 0}, INVALID), ({13: 1 << 31}, UNSUPPORTED), ({0: FAKE + 8}, INVALID),
@@ -185,7 +185,7 @@ def test_attn_tree_refusals(lib):
                      ({22: 0}, SMALL), ({21: FAKE + 4}, INVALID), ({12: (1 << 15) + 1}, UNSUPPORTED),
                      ({12: 1, 15: 65536, 16: 65536}, UNSUPPORTED)]:
         assert lib.bf1_attn_tree(*_with(ok, at)) == want, at
-    for at in ({12: 0}, {13: 0}, {14: 0}):
+    for at in ({12: 0}, {13: 0}):
         assert lib.bf1_attn_tree(*_with(ok, at)) == bf1.BF1_OK
     assert lib.bf1_attn_tree(*_with(ok, {20: 1, 19: 1000, 22: 0})) == SMALL  # L is not used
     size = ctypes.c_int64()
