@@ -13,7 +13,7 @@
 // memory: a row is read once and written once, 16 bytes a lane and load.  Replays of a
 // graph: 32768 tokens of 16 + 8 heads of 128 from joined rows 91 us for 403 MB (4.4 TB/s; a
 // large copy reaches 5.0), 32 tokens 4.2; the gradient of 16382 such tokens from fp32
-// gradients 90 us for 403 MB, with the sums over workgroups, of 128 tokens 12.
+// gradients 88 us for 403 MB, with the sums over workgroups, of 128 tokens 8.4.
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -270,7 +270,7 @@ __global__ __launch_bounds__(THREADS) void norm_rope_kernel(Side q, Side k, Shap
 // The gradient.  A workgroup belongs to one side, the first `q_groups` to Q, and goes over
 // that side's tiles (THREADS / team tokens, `chunk` heads), as many apart as the side has
 // workgroups.  It keeps its sums of the gain's gradient in registers; at the end its teams
-// meet (lane moves, then LDS) and write one record [d], which the next kernel sums over
+// meet in LDS and write one record [d], which the next kernel sums over
 // the workgroups, in their order.  The records go by the call's sizes alone, so the
 // result is the same each time.
 template <typename T, typename TD, typename TO, bool INTER, bool WIDE>
@@ -278,7 +278,7 @@ __global__ __launch_bounds__(THREADS) void norm_rope_bwd_kernel(Side q, Side k, 
                                                                 float* __restrict__ q_dgain, float* __restrict__ k_dgain,
                                                                 float* __restrict__ records) {
     constexpr int P = PAIRS<T>;
-    extern __shared__ float part[];  // [wave][lane of a team, element]
+    __shared__ __align__(16) float part[THREADS * 2 * P];
     const Lane x = lane_of<INTER, P>((int32_t)(threadIdx.x & ((1u << z.lshift) - 1)), z.d, z.half);
     const bool isk = blockIdx.x >= q_groups;
     const Side& w = isk ? k : q;
@@ -326,24 +326,19 @@ __global__ __launch_bounds__(THREADS) void norm_rope_bwd_kernel(Side q, Side k, 
     }
     float* dgain = isk ? k_dgain : q_dgain;
     if (dgain == nullptr) return;
-    const int32_t team = 1 << z.lshift, l = threadIdx.x & (team - 1), wave = threadIdx.x >> 6;
+    // Column c is element c % 2 P of a team's lane c / 2 P; a thread sums a column over the teams.
 #pragma unroll
-    for (int e = 0; e < 2 * P; ++e) {
-        float a = acc[e];
-        for (int32_t m = team; m < 64; m <<= 1) a += __shfl_xor(a, m);
-        if ((threadIdx.x & 63) < team) part[(wave * team + l) * 2 * P + e] = a;
-    }
+    for (int e = 0; e < 2 * P; e += 4)
+        *reinterpret_cast<f32x4*>(part + threadIdx.x * 2 * P + e) = f32x4{acc[e], acc[e + 1], acc[e + 2], acc[e + 3]};
     __syncthreads();
-    if ((int32_t)threadIdx.x >= team) return;
-    // the first team's lanes write what the waves' teams of the same lane have
-#pragma unroll
-    for (int e = 0; e < 2 * P; ++e) {
+    const int32_t cols = 2 * P << z.lshift;
+    for (int32_t c = threadIdx.x; c < cols; c += THREADS) {
         float a = 0.f;
-#pragma unroll
-        for (int w = 0; w < THREADS / 64; ++w) a += part[(w * team + l) * 2 * P + e];
-        const int32_t at = e < P ? x.a + e : x.b + e - P;
-        if (e < P ? e >= x.na : e - P >= x.nb) continue;
-        (records != nullptr ? records + (int64_t)blockIdx.x * z.d : dgain)[at] = a;
+#pragma unroll 8
+        for (int32_t at = c; at < THREADS * 2 * P; at += cols) a += part[at];
+        const Lane y = lane_of<INTER, P>(c / (2 * P), z.d, z.half);
+        const int32_t e = c % (2 * P), at = e < P ? y.a + e : y.b + e - P;
+        if (e < P ? e < y.na : e - P < y.nb) (records != nullptr ? records + (int64_t)blockIdx.x * z.d : dgain)[at] = a;
     }
 }
 
@@ -617,9 +612,8 @@ int bf1_qk_norm_rope_bwd(const void* dQ, const void* dK, int32_t grad_type, cons
     }
     const bf1::Shape z{positions, positions_batch_stride, freqs, (uint32_t)(rows << lshift), (uint32_t)n, 0,
                        head_dim, half, lshift, gain_type == BF1_TYPE_F32, eps, amplitude, 1.f / (float)head_dim};
-    const size_t lds = (size_t)bf1::THREADS / 64 * (1 << lshift) * 2 * P * 4;
     auto go = [&](auto kern) {
-        hipLaunchKernelGGL(kern, dim3((unsigned)plan.groups), dim3(bf1::THREADS), lds, stm, side[0], side[1], z,
+        hipLaunchKernelGGL(kern, dim3((unsigned)plan.groups), dim3(bf1::THREADS), 0, stm, side[0], side[1], z,
                            (uint32_t)plan.q_groups, dq_gain, dk_gain, sums ? (float*)workspace : nullptr);
         if (sums)
             hipLaunchKernelGGL(bf1::gain_sum_kernel, sum_groups, dim3(bf1::SUM_THREADS), 0, stm, (const float*)workspace,

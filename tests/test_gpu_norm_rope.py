@@ -147,10 +147,11 @@ def test_norm_rope_gradient_matches_the_oracle(batch, n, Hq, Hkv, d, r, dtype, i
             if g is None:
                 assert dg is None
                 continue
-            # a lane sums the rows of its tiles (2 heads each, at most 1024 workgroups), then six
-            # lane moves, four waves, 32 records and 32 threads, one after the other
-            rows = 2 * -(-batch * n * (Hq + Hkv + 1) * 64 // (256 * 2) // 1024 + 1)
-            bar = off + (rows + 6 + 4 + 32 + 32) * U * mag + U * np.abs(want)
+            # a lane sums the rows of its tiles (up to 16 heads of a token each, for these sizes
+            # one tile a workgroup), then the teams of a workgroup (256 lanes, d / 16 or d / 8 a
+            # team, a power of two), 32 records and 32 threads follow one after the other
+            teams = 256 // 2 ** max(0, int(np.ceil(np.log2(d / (16 if dtype is torch.bfloat16 else 8) + 1))) - 1)
+            bar = off + (16 + teams + 32 + 32) * U * mag + U * np.abs(want)
             assert (np.abs(f64(dg) - want) <= bar).all(), np.abs(f64(dg) - want).max()
 
 
