@@ -994,6 +994,8 @@ def _norm_rope_sides(q, k, q_gain, k_gain, positions, freqs):
 
 def _type(dtype):
     import torch
+    if dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError(f"dtype must be bfloat16 or float32, got {dtype}")
     return 0 if dtype is torch.bfloat16 else 1
 
 

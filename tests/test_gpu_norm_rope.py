@@ -274,7 +274,8 @@ def test_norm_rope_empty_and_refusals():
                      (dict(k=k.float()), "k must"), (dict(q=q.half()), "bf16"), (dict(q_gain=qg[:64]), "q_gain"),
                      (dict(k_gain=kg.float()), "dtype"), (dict(q_gain=qg.half()), "gains"), (dict(q_gain=qg.cpu()), "device"),
                      (dict(q=q.transpose(2, 3).contiguous().transpose(2, 3)), "side by side"),
-                     (dict(q_out=torch.empty(1, 4, 50, 64, device="cuda")), "q_out")]:
+                     (dict(q_out=torch.empty(1, 4, 50, 64, device="cuda")), "q_out"),
+                     (dict(q=q.float(), k=k.float(), dtype=torch.float16), "dtype")]:
         with pytest.raises(ValueError, match=why):
             bf1.qk_norm_rope(**{**ok, **bad})
     for bad in (dict(eps=0.0), dict(dtype=torch.float32), dict(q_out=torch.empty(1, 4, 1, 128, device="cuda",

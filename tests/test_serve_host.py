@@ -162,6 +162,9 @@ def test_qk_norm_rope_bwd_refusals(lib):
     assert lib.bf1_qk_norm_rope_bwd_workspace_size(2, 10, 4, 2, 130, 132, 0, ctypes.byref(size)) == UNSUPPORTED
     assert bf1.qk_norm_rope_bwd_workspace_size(1, 1, 1, 1, 64, 64, torch.bfloat16) == 0  # one workgroup
     assert 0 < bf1.qk_norm_rope_bwd_workspace_size(4, 100000, 16, 8, 128, 128, torch.bfloat16) <= 1 << 22
+    for other in (torch.float16, torch.float64, None):
+        with pytest.raises(ValueError, match="dtype"):
+            bf1.qk_norm_rope_bwd_workspace_size(1, 1, 1, 1, 64, 64, other)
 
 
 def test_tree_step_refusals(lib):
