@@ -469,7 +469,7 @@ int bf1_decode_attn_q8(const void* Q, const void* K_pages, const void* V_pages, 
  *     forward   y = turn(x r gain)                 turn as bf1_rope's, with `amplitude`
  *     gradient  dn = the transposed turn of dy, u = dn gain,
  *               dx = r (u - x r mean(u x r)),  dgain = sum over rows of dn x r
- * Sums, the norm and the turn are fp32 (squares too: a row's elements lie below 2^60),
+ * Sums, the norm and the turn are fp32 (squares too: a row's elements lie below 2^59),
  * results are rounded once.
  *   Q, K, positions, freqs, Q_out, K_out, interleaved, amplitude: as bf1_rope's; outputs
  *               may have any strides that write no element twice
@@ -516,6 +516,7 @@ int bf1_qk_norm_rope_bwd(const void* dQ, const void* dK, int32_t grad_type, cons
  *   masks     : [rows] int64, bit k of a row: node k is the node or one before it
  *   positions : [rows] int32, for bf1_rope or bf1_qk_norm_rope, too
  * Rows behind the last tree, of nodes without a place and past the 64th: mask 0, position -1.
+ * Up to 2^30 rows.
  *
  * bf1_attn_tree: attention of all nodes, one kernel, or two with workspace.  The node at
  * position p, block j = p / B, reads the committed keys of the blocks of P(j) (Eq. 1; with
@@ -549,7 +550,7 @@ int bf1_attn_tree(const void* Q, const void* K_pages, const void* V_pages, const
  *   accepted     : [batch, accepted_width <= 64] int32: numbers of a path, ascending; the
  *                  first one that is not above the one before it, or is no node's, ends it
  *   seq_lens     : the lengths with the drafted tokens
- *   seq_lens_out : [batch] int32, seq_lens_before plus the nodes accepted; neither input
+ *   seq_lens_out : [batch] int32, seq_lens_before plus the nodes accepted; none of the inputs
  * Rows may lie where others go.  A row from or to a page that is none is left out.  The
  * same call again moves other rows: seq_lens_out is for the step's next.
  */
@@ -571,9 +572,9 @@ int bf1_kv_compact(void* K_pages, void* V_pages, const int32_t* accepted, int32_
  *                    itself, as a cache of prefixes does, adds 1 to theirs
  *   free_pages     : [num_free] int32, updated: bf1_page_step's list, with room for every page.
  *                    Pages that nobody holds any more are put back below the head, ascending
- *   free_head, free_head_out : [1] int32; may be the same
- *   seq_lens_out   : [batch] int32; neither of the three inputs
- *   copy_from, copy_to, copy_rows : [batch] int32, distinct buffers: see below
+ *   seq_lens_out, copy_from, copy_to, copy_rows : [batch] int32, see below
+ *   free_head, free_head_out : [1] int32; may be the same.  All else that is written is a
+ *                    buffer of its own
  * Full blocks are shared.  A block that goes on being written has one holder: the first
  * place that continues it keeps its page, if no other sequence and no caller holds that;
  * for the others it is to be copied, the first copy_rows[b] tokens of page copy_from[b] to
@@ -587,7 +588,8 @@ int bf1_kv_compact(void* K_pages, void* V_pages, const int32_t* accepted, int32_
  * bf1_kv_copy: rows 0 .. copy_rows[i] - 1 (B at most) of K and V page copy_from[i] to page
  * copy_to[i], all heads, for i < count; entries outside the cache are left out.  No page is
  * copied to twice, or both to and from.  The tails of the 8-bit cache are such pages, too
- * (num_pages = batch).
+ * (num_pages = batch): a place goes on inside the block that its source is writing, or from the
+ * end of a full one; of a block that is complete no tail is left.
  */
 int bf1_page_fork(int32_t batch, const int32_t* seq_lens, const int32_t* sources, const int32_t* keep_lens,
                   const int32_t* page_table, int32_t max_pages_per_seq, int32_t* shares, int32_t num_pages,

@@ -1240,8 +1240,9 @@ def page_fork(seq_lens, sources, keep_lens, page_table, shares, free_pages, free
     free_pages, page_step's list with room for every page: pages that nobody holds any more
     go back below the head.  Full blocks are shared; a block that goes on being written
     stays with the first place that continues it, if nobody else holds its page, and is
-    copied for the others: kv_copy with the result's lists, for each layer's cache (for a
-    CacheQ8 move the tails instead).  Without a free page a sequence goes on without that
+    copied for the others: kv_copy with the result's lists, for each layer's cache.  Of a
+    CacheQ8 the tails are copied instead, places as pages; there a sequence goes on inside
+    the block that its source is writing, or from the end of a full one.  Without a free page a sequence goes on without that
     block's tokens.  To run the same call again (a warm-up before a capture, a retry), put
     shares and free_pages back as they were first."""
     if out is None and stream is None:

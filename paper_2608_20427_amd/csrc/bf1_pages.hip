@@ -379,9 +379,16 @@ int bf1_page_fork(int32_t batch, const int32_t* seq_lens, const int32_t* sources
                               (const void*)copy_to, (const void*)copy_rows})
             if (!bf1::aligned(p, 4)) return BF1_ERR_INVALID_ARG;
     // old rows and lengths are read while new ones are written
-    if (batch > 0 && (page_table_out == page_table || seq_lens_out == seq_lens || seq_lens_out == keep_lens ||
-                      seq_lens_out == sources))
-        return BF1_ERR_INVALID_ARG;
+    if (batch > 0) {
+        const int32_t *in[] = {seq_lens, sources, keep_lens, page_table, free_head},
+                      *out[] = {shares, free_pages, page_table_out, seq_lens_out, copy_from, copy_to, copy_rows, free_head_out};
+        for (int i = 0; i < 8; ++i) {
+            for (const int32_t* p : in)
+                if (out[i] == p && !(p == free_head && out[i] == free_head_out)) return BF1_ERR_INVALID_ARG;
+            for (int j = 0; j < i; ++j)
+                if (out[i] == out[j]) return BF1_ERR_INVALID_ARG;
+        }
+    }
     const bf1::Fork f{batch, seq_lens, sources, keep_lens, page_table, max_pages_per_seq, shares, num_pages, free_pages,
                       num_free, free_head, B == 64 ? 6 : 7, page_table_out, seq_lens_out, free_head_out, copy_from, copy_to,
                       copy_rows};
@@ -422,7 +429,9 @@ int bf1_kv_compact(void* K_pages, void* V_pages, const int32_t* accepted, int32_
                           (const void*)seq_lens_out})
         if (!bf1::aligned(p, 4)) return BF1_ERR_INVALID_ARG;
     // a sequence's lengths are read by all its heads' workgroups while one writes the new one
-    if (seq_lens_out == seq_lens_before || seq_lens_out == seq_lens) return BF1_ERR_INVALID_ARG;
+    if (seq_lens_out == seq_lens_before || seq_lens_out == seq_lens || seq_lens_out == page_table ||
+        (accepted_width > 0 && seq_lens_out == accepted))
+        return BF1_ERR_INVALID_ARG;
     if (!bf1::launchable((int64_t)batch * Hkv)) return BF1_ERR_UNSUPPORTED;
     auto go = [&](auto kern) {
         hipLaunchKernelGGL(kern, dim3((unsigned)((int64_t)batch * Hkv)), dim3(bf1::THREADS), 0, (hipStream_t)stream,

@@ -824,6 +824,8 @@ int check_sizes(int32_t batch, int32_t max_nodes, int32_t Hq, int32_t Hkv, int32
     return BF1_OK;
 }
 
+constexpr int64_t MOST_ROWS = int64_t(1) << 30;  // row numbers are 32 bits, a step of 64 past the last one too
+
 }  // namespace
 }  // namespace bf1
 
@@ -832,13 +834,13 @@ extern "C" {
 int bf1_tree_step(const int32_t* parents, const int32_t* token_start, const int32_t* seq_lens_before,
                   const int32_t* seq_lens, int32_t batch, int64_t rows, int64_t* masks, int32_t* positions, void* stream) {
     if (batch < 0 || rows < 0) return BF1_ERR_INVALID_ARG;
-    if (rows >= (int64_t(1) << 31) || batch > (1 << 24)) return BF1_ERR_UNSUPPORTED;
+    if (rows > bf1::MOST_ROWS || batch > (1 << 24)) return BF1_ERR_UNSUPPORTED;
     if (rows == 0) return BF1_OK;
     if (!bf1::aligned(parents, 4) || !bf1::aligned(masks, 8) || !bf1::aligned(positions, 4)) return BF1_ERR_INVALID_ARG;
     if (positions == parents) return BF1_ERR_INVALID_ARG;
     if (batch > 0)
         for (const int32_t* p : {token_start, seq_lens_before, seq_lens})
-            if (!bf1::aligned(p, 4)) return BF1_ERR_INVALID_ARG;
+            if (!bf1::aligned(p, 4) || p == positions) return BF1_ERR_INVALID_ARG;
     // a wave per tree, and at least one for the rows behind them
     hipLaunchKernelGGL(bf1::tree_step_kernel, dim3((unsigned)(batch / (bf1::THREADS / 64) + 1)), dim3(bf1::THREADS), 0,
                        (hipStream_t)stream, parents, token_start, seq_lens_before, seq_lens, batch, (int32_t)rows,
@@ -865,7 +867,7 @@ int bf1_attn_tree(const void* Q, const void* K_pages, const void* V_pages, const
     const int bad = bf1::check_sizes(batch, max_nodes, Hq, Hkv, head_dim, B, max_pages_per_seq, L, dense);
     if (bad != BF1_OK) return bad;
     if (rows < 0 || num_pages < 1) return BF1_ERR_INVALID_ARG;
-    if (rows >= (int64_t(1) << 31)) return BF1_ERR_UNSUPPORTED;
+    if (rows > bf1::MOST_ROWS) return BF1_ERR_UNSUPPORTED;
     if (batch == 0 || rows == 0) return BF1_OK;
     for (const void* p : {Q, K_pages, V_pages, (const void*)O})
         if (!bf1::aligned(p, 16)) return BF1_ERR_INVALID_ARG;

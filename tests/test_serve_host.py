@@ -170,6 +170,7 @@ def test_qk_norm_rope_bwd_refusals(lib):
 def test_tree_step_refusals(lib):
     ok = [FAKE, FAKE, FAKE, FAKE, 3, 20, FAKE + 4096, FAKE + 8192, None]
     for at, want in [({4: -1}, INVALID), ({5: -1}, INVALID), ({5: 1 << 31}, UNSUPPORTED), ({4: (1 << 24) + 1}, UNSUPPORTED),
+                     ({5: (1 << 30) + 1}, UNSUPPORTED), ({1: FAKE + 8192}, INVALID), ({3: FAKE + 8192}, INVALID),
                      ({0: None}, INVALID), ({1: FAKE + 2}, INVALID), ({2: None}, INVALID), ({3: None}, INVALID),
                      ({6: FAKE + 4}, INVALID), ({7: None}, INVALID), ({7: FAKE}, INVALID)]:
         assert lib.bf1_tree_step(*_with(ok, at)) == want, at
@@ -183,6 +184,7 @@ def test_attn_tree_refusals(lib):
                      ({15: 17}, INVALID), ({15: 24}, UNSUPPORTED), ({15: 128}, UNSUPPORTED), ({17: 96}, UNSUPPORTED),
                      ({18: 32}, UNSUPPORTED), ({19: -1}, INVALID), ({19: 33}, UNSUPPORTED), ({20: 2}, INVALID),
                      ({8: 0}, INVALID), ({9: 0}, INVALID), ({13: 1 << 31}, UNSUPPORTED), ({0: FAKE + 8}, INVALID),
+                     ({13: (1 << 30) + 1}, UNSUPPORTED),
                      ({1: None}, INVALID), ({3: FAKE + 4}, INVALID), ({4: None}, INVALID), ({5: FAKE + 2}, INVALID),
                      ({6: None}, INVALID), ({7: None}, INVALID), ({10: FAKE}, INVALID), ({11: FAKE + 1}, INVALID),
                      ({22: 0}, SMALL), ({21: FAKE + 4}, INVALID), ({12: (1 << 15) + 1}, UNSUPPORTED),
@@ -207,7 +209,9 @@ def test_page_refusals(lib):
                      ({2: FAKE + 2}, INVALID), ({3: None}, INVALID), ({4: None}, INVALID), ({6: None}, INVALID),
                      ({8: None}, INVALID), ({10: None}, INVALID), ({12: None}, INVALID), ({13: None}, INVALID),
                      ({14: None}, INVALID), ({15: None}, INVALID), ({16: None}, INVALID), ({17: FAKE + 1}, INVALID),
-                     ({12: far[3]}, INVALID), ({13: far[0]}, INVALID), ({13: far[1]}, INVALID), ({13: far[2]}, INVALID)]:
+                     ({12: far[3]}, INVALID), ({13: far[0]}, INVALID), ({13: far[1]}, INVALID), ({13: far[2]}, INVALID),
+                     ({15: far[0]}, INVALID), ({15: FAKE + 128}, INVALID), ({17: far[8]}, INVALID), ({8: far[4]}, INVALID),
+                     ({14: FAKE + 64}, INVALID), ({16: far[6]}, INVALID)]:
         assert lib.bf1_page_fork(*_with(ok, at)) == want, at
     ok = [FAKE, FAKE * 2, FAKE, FAKE, FAKE, 5, 7, 8, 128, 64, None]
     for at, want in [({5: -1}, INVALID), ({6: 0}, INVALID), ({7: 0}, INVALID), ({8: 96}, UNSUPPORTED), ({9: 32}, UNSUPPORTED),
@@ -220,6 +224,7 @@ def test_page_refusals(lib):
                      ({10: 0}, INVALID), ({11: 32}, UNSUPPORTED), ({12: 16}, UNSUPPORTED), ({0: None}, INVALID),
                      ({1: FAKE}, INVALID), ({2: None}, INVALID), ({4: None}, INVALID), ({5: FAKE + 1}, INVALID),
                      ({6: None}, INVALID), ({13: None}, INVALID), ({13: FAKE}, INVALID), ({13: FAKE + 64}, INVALID),
+                     ({2: FAKE + 128}, INVALID),
                      ({7: 1 << 24, 10: 1 << 10}, UNSUPPORTED)]:
         assert lib.bf1_kv_compact(*_with(ok, at)) == want, at
     assert lib.bf1_kv_compact(*_with(ok, {7: 0, 0: None})) == bf1.BF1_OK
