@@ -115,8 +115,8 @@ __device__ __forceinline__ const __attribute__((address_space(4))) int32_t* fixe
 }
 
 // A workgroup takes 16 NT CW columns (q-heads of neighbouring nodes) of one (sequence,
-// kv-head) and a split of its keys.  Its four waves are CW column waves, 16 NT columns
-// each, in KW = 4 / CW key groups, which take tiles of 16 CW (CW = 1: 32) keys in turns.
+// kv-head) and a split of its keys.  Its four or eight waves are CW column waves, 16 NT columns
+// each, in KW = WAVES / CW key groups, which take tiles of 16 CW (CW = 1: 32) keys in turns.
 //
 // Scores S = K Q^T on 16x16x32 tiles: A = K rows (lane l: key l % 16, 16-byte chunk 4 s +
 // l / 16), B = Q rows, so lane l holds keys 4 (l / 16) + 0..3 of each of a unit's two tiles
@@ -662,6 +662,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_tree_kernel(Tree a) {
 #pragma unroll
     for (int e0 = 0; e0 < COLS; e0 += PER) {
         const int e = e0 + tid / (D / 4);
+        if (PER > COLS && e >= COLS) break;
         float m[KW], M = -INFINITY, l = 0.f;
 #pragma unroll
         for (int w = 0; w < KW; ++w) M = fmaxf(M, m[w] = r_m[(w * COLS + e) * 2]);
@@ -769,7 +770,11 @@ __global__ __launch_bounds__(THREADS) void merge_tree_kernel(Tree a) {
 // Splits fill 256 workgroups, one a compute unit; 128 columns over long lists 512 (eight
 // lists of 32K, 64 nodes in groups of 8: 475 / 290).  64 columns run as workgroups of eight
 // waves, four key groups, where there are no more than 256 of them (32 sequences of 32K, 32 nodes
-// in groups of 2 34.0, with four waves 40.8; 64 sequences 72.7 and 62.0).
+// in groups of 2 34.0, with four waves 40.8; 64 sequences 72.7 and 62.0).  So do 16 where at most
+// two splits would fit, which they replace: a merge costs more than the longer walk of one workgroup,
+// up to 32 tiles.  Heads of 128 in groups of 2, 16 nodes, four waves / eight: eight sequences of 8K on
+// the route 14.3 (two splits) / 12.7, of 2K dense 22.9 / 26.5, sixteen 15.2 (one) / 13.9 and 31.2 /
+// 28.5, 24 (more than 256 workgroups) 19.1 / 24.3.
 struct Plan {
     int32_t cols, groups, waves, nsplit;
     int64_t bytes;
@@ -785,13 +790,14 @@ Plan plan_of(int32_t batch, int32_t max_nodes, int32_t Hkv, int32_t G, int32_t d
     p.cols = cols <= 16 || work <= 8000 ? 16 : cols <= 32 ? 32 : cols <= 64 || work <= 100000 ? 64 : 128;
     p.groups = (cols + p.cols - 1) / p.cols;
     const int64_t rows = std::max<int64_t>(1, bh * p.groups);
-    p.waves = p.cols == 64 && rows <= PLACES ? 8 : 4;
+    const bool one = p.cols == 16 && 3 * rows > PLACES && (tiles <= 32 || 2 * rows > PLACES);  // no split of eight waves
+    p.waves = rows <= PLACES && (p.cols == 64 || one) ? 8 : 4;
     // turns of a key group with one split
     const int64_t turns = p.cols == 128 ? (tiles + 1) / 2 : (tiles + p.waves - 1) / (p.cols == 64 ? p.waves / 2 : p.waves);
     int64_t n = PLACES / rows;
     if (p.cols == 128 && turns * rows >= 8 * 2 * PLACES) n = 2 * PLACES / rows;
     n = std::min(std::min(n, turns), MOST_SPLITS);
-    p.nsplit = n < 2 ? 1 : (int32_t)n;
+    p.nsplit = n < 2 || one ? 1 : (int32_t)n;
     p.bytes = p.nsplit <= 1 ? 0
                             : (rows * p.nsplit * p.cols * (d + 2) * 4 + 15) / 16 * 16 + (bh * 4 + 15) / 16 * 16;
     return p;
@@ -907,7 +913,8 @@ int bf1_attn_tree(const void* Q, const void* K_pages, const void* V_pages, const
     auto nt = [&](auto d_c, auto g_c, auto pw_c) {
         constexpr int D = decltype(d_c)::value, GG = decltype(g_c)::value, PW = decltype(pw_c)::value;
         switch (p.cols) {
-            case 16: return bf1::launch<D, GG, PW, 1, 1, 4>(a, s);
+            case 16:
+                return p.waves == 8 ? bf1::launch<D, GG, PW, 1, 1, 8>(a, s) : bf1::launch<D, GG, PW, 1, 1, 4>(a, s);
             case 32: return bf1::launch<D, GG, PW, 2, 1, 4>(a, s);
             case 64:
                 return p.waves == 8 ? bf1::launch<D, GG, PW, 2, 2, 8>(a, s) : bf1::launch<D, GG, PW, 2, 2, 4>(a, s);

@@ -199,6 +199,30 @@ def test_attn_tree_columns(copies, Hq, Hkv, nodes, d, B, L):
     c.check(c.run(L, max_nodes=nodes), L)
 
 
+@pytest.mark.parametrize("batch,Hq,Hkv,nodes,d,B", [(14, 8, 8, 3, 128, 64), (28, 8, 8, 16, 64, 64), (14, 16, 8, 8, 64, 64),
+                                                    (16, 8, 2, 12, 64, 128), (14, 16, 4, 9, 128, 128), (10, 8, 1, 20, 128, 64)])
+def test_attn_tree_eight_waves(batch, Hq, Hkv, nodes, d, B):
+    """16 columns at a time in workgroups of eight waves: as many sequences, heads and nodes as
+    leave room for two splits or none; also with a value that is not finite, which sends its
+    columns over their keys once more."""
+    assert bf1.attn_tree_workspace_size(batch, nodes, Hq, Hkv, d, B, 12) == 0
+    rng = np.random.default_rng(batch + nodes)
+    held = [int(j * B + o) for j, o in zip(rng.integers(0, 10, batch), rng.choice([0, 1, 40, B - 2, B - 1], batch))]
+    held[:2] = [9 * B + B - 1, 8 * B + 5]
+    c = Case(held, [nodes, nodes, 0] + [int(x) for x in rng.integers(1, nodes + 1, batch - 3)], Hq, Hkv, d, B, seed=nodes,
+             deep=True)
+    for L, dense in ((2, False), (0, False), (2, True)):
+        c.check(c.run(L, dense, max_nodes=nodes), L, dense)
+    x, page = c.v, c.table[1, 8]
+    clean = c.run(max_nodes=nodes)
+    x[page, 0, 2, 5] = float("inf")  # position 8 B + 2: committed, every node of sequence 1 reads it
+    o = c.run(max_nodes=nodes)[0]
+    hit = torch.zeros(o.shape, dtype=torch.bool, device="cuda")
+    hit[c.start[1]:c.start[2], :Hq // Hkv, 5] = True
+    # the others of its rows are sums over 500 keys, below 2: both within a step, 2^-7, at most
+    assert (o[hit] == float("inf")).all() and (o[~hit].float() - clean[0][~hit].float()).abs().max() < 2.0 ** -6
+
+
 @pytest.mark.parametrize("width", [20, 200, 2000, 20000])
 @pytest.mark.parametrize("G,nodes", [(1, 40), (4, 16), (8, 33)])
 def test_attn_tree_wide_tables(width, G, nodes):
