@@ -273,8 +273,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_tree_kernel(Tree a) {
     if (rows1 > 0) bad |= (uint32_t)page1 >= (uint32_t)a.num_pages;
     bad = scalar(__syncthreads_or(bad));  // and the list is there
 
-    const int early = bad ? 0 : count * UPP;
-    const int units0 = bad ? 0 : (rows0 + TILE - 1) / TILE, units1 = bad ? 0 : (rows1 + TILE - 1) / TILE;
+    const int early = scalar(bad ? 0 : count * UPP);
+    const int units0 = scalar(bad ? 0 : (rows0 + TILE - 1) / TILE), units1 = scalar(bad ? 0 : (rows1 + TILE - 1) / TILE);
     const int units = early + units0 + units1;  // tiles
     const int nsb = min(a.nsplit, max(1, (units + KW - 1) / KW));
     if (a.nsplit > 1 && s == 0 && rg == 0 && tid == 0) a.used[bh] = nsb;
@@ -318,10 +318,10 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_tree_kernel(Tree a) {
             w.kind = 5;
             first = early + units0;
         }
-        w.row = (u - first) * TILE;
-        w.kind = __builtin_amdgcn_readfirstlane(w.kind);
-        w.base = ((int64_t)__builtin_amdgcn_readfirstlane(page) * a.Hkv + h) * PW * D;
-        w.bytes = (uint32_t)__builtin_amdgcn_readfirstlane(n) * RB;
+        w.row = scalar((u - first) * TILE);
+        w.kind = scalar(w.kind);
+        w.base = ((int64_t)scalar(page) * a.Hkv + h) * PW * D;
+        w.bytes = (uint32_t)scalar(n) * RB;
         w.soff = (uint32_t)w.row * RB;
         return w;
     };
