@@ -448,16 +448,16 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_tree_kernel(Tree a) {
     };
     clear();
     if constexpr (CW == 1) {
-        // One unit: its K rows are in flight to kr and its V rows to buffer BUF.  The next
+        // One unit: its K rows are in flight to kr and its V rows to buffer `buf`.  The next
         // unit's V rows are asked for before the wait for them, its K rows as soon as the
         // scores have taken kr, and the page after that.
         int32_t coming = 0;
-        auto step = [&](int u, const Where& w, Where& nx, auto buf_c) {
-            constexpr int BUF = decltype(buf_c)::value;
+        Where w{}, nx{};
+        auto step = [&](int u, int buf) {
             const bool more = u + hop < units;
             if (more) {
                 nx = where(u + hop, coming);
-                load_tile(nx, BUF ^ 1);
+                load_tile(nx, buf ^ 1);
                 __builtin_amdgcn_sched_barrier(0);
                 __builtin_amdgcn_s_waitcnt(0x0F70 | SEGS);
             } else {
@@ -483,23 +483,24 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_tree_kernel(Tree a) {
             for (int d = 0; d < DT; d += 2) {
                 u32x2 v0, v1, v2, v3;
                 asm volatile(
-                    "ds_read_b64_tr_b16 %0, %4 offset:%6\n\tds_read_b64_tr_b16 %1, %4 offset:%7\n\t"
-                    "ds_read_b64_tr_b16 %2, %5 offset:%6\n\tds_read_b64_tr_b16 %3, %5 offset:%7\n\t"
+                    "ds_read_b64_tr_b16 %0, %4\n\tds_read_b64_tr_b16 %1, %4 offset:%6\n\t"
+                    "ds_read_b64_tr_b16 %2, %5\n\tds_read_b64_tr_b16 %3, %5 offset:%6\n\t"
                     "s_waitcnt lgkmcnt(0)"
                     : "=&v"(v0), "=&v"(v1), "=&v"(v2), "=&v"(v3)
-                    : "v"(vtr ^ (32 * d)), "v"(vtr ^ (32 * d + 32)), "i"(BUF * BUF_LDS), "i"(BUF * BUF_LDS + 16 * RB)
+                    : "v"((vtr ^ (32 * d)) + buf * BUF_LDS), "v"((vtr ^ (32 * d + 32)) + buf * BUF_LDS), "i"(16 * RB)
                     : "memory");
                 both(d, hi, lo, v0, v1, v2, v3);
             }
         };
         if (u0 < units) {
-            Where w = where(u0, page_of(u0)), nx = w;
+            w = where(u0, page_of(u0));
             if (u0 + hop < units) coming = page_of(u0 + hop);
             load_tile(w, 0);
             load_k(w, 0);
-            for (int u = u0; u < units; u += 2 * hop) {
-                step(u, w, nx, std::integral_constant<int, 0>{});
-                if (u + hop < units) step(u + hop, nx, w, std::integral_constant<int, 1>{});
+#pragma unroll 1
+            for (int u = u0, buf = 0; u < units; u += hop, buf ^= 1) {
+                step(u, buf);
+                w = nx;
             }
         }
     } else {
@@ -659,7 +660,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_tree_kernel(Tree a) {
     const int64_t rec = ((int64_t)bh * a.groups + rg) * a.nsplit + s;
     constexpr int PER = THREADS / (D / 4);  // columns at a time, four dims a thread
     const int d = tid % (D / 4) * 4;
-#pragma unroll
+#pragma unroll 1
     for (int e0 = 0; e0 < COLS; e0 += PER) {
         const int e = e0 + tid / (D / 4);
         if (PER > COLS && e >= COLS) break;
