@@ -552,7 +552,9 @@ int bf1_attn_tree(const void* Q, const void* K_pages, const void* V_pages, const
  *   seq_lens     : the lengths with the drafted tokens
  *   seq_lens_out : [batch] int32, seq_lens_before plus the nodes accepted; none of the inputs
  * Rows may lie where others go.  A row from or to a page that is none is left out.  The
- * same call again moves other rows: seq_lens_out is for the step's next.
+ * same call again moves other rows: seq_lens_out is for the step's next.  Pages behind it stay
+ * in the table; bf1_page_fork from seq_lens, with seq_lens_out as keep_lens, frees them, where
+ * bf1_page_step would take new ones for the same blocks.
  */
 int bf1_kv_compact(void* K_pages, void* V_pages, const int32_t* accepted, int32_t accepted_width,
                    const int32_t* seq_lens_before, const int32_t* seq_lens, const int32_t* page_table, int32_t batch,

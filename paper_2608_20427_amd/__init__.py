@@ -1195,7 +1195,9 @@ def kv_compact(k_pages, v_pages, accepted, lens_before, seq_lens, page_table, ou
 
     accepted: int32 [batch, up to 64], a path's nodes, ascending; the first entry that is
     not above the one before it, or is no node (-1), ends it.  seq_lens: with the drafted
-    tokens, as page_step returned it."""
+    tokens, as page_step returned it.  The pages behind the new lengths stay in the table:
+    give seq_lens and, as keep_lens, the result to page_fork before the next page_step, which
+    frees them."""
     if out is None and stream is None:
         r = (_MARSHAL or _native()).kv_compact(k_pages, v_pages, accepted, lens_before, seq_lens, page_table)
         if r is not None:

@@ -663,7 +663,6 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_tree_kernel(Tree a) {
 #pragma unroll 1
     for (int e0 = 0; e0 < COLS; e0 += PER) {
         const int e = e0 + tid / (D / 4);
-        if (PER > COLS && e >= COLS) break;
         float m[KW], M = -INFINITY, l = 0.f;
 #pragma unroll
         for (int w = 0; w < KW; ++w) M = fmaxf(M, m[w] = r_m[(w * COLS + e) * 2]);
@@ -759,23 +758,23 @@ __global__ __launch_bounds__(THREADS) void merge_tree_kernel(Tree a) {
 
 // What a call's launches go by, from its sizes alone.
 //
-// Columns of a workgroup: 16 for little work, where a short path counts (the code of a
-// wave that runs once comes to it no faster than it is fetched), 64 or 128 for more, where
-// a key row should serve many columns.  Work: 16-column tiles times 32-key tiles.  us in
-// replays of a graph, 16 / 32 / 64 / 128 columns with their best splits, heads of 128: one
-// sequence of 32K on the route, 64 nodes in groups of 2 14.7 / 17.1 / 18.0 / 20.9 (work 2100),
-// two 18.1 / 18.3 / 19.6 / 22.5 (4200), four 23.5 / 23.4 / 21.7 / 25.5 (8400), 32 of them 112 / 71 /
-// 49 / 53 (68000); dense lists of 8100, one 32.6 / 31.4 / 28.6 / 34.3 (16000), eight 162 / 105 / 84 /
-// 75 (130000).
+// Columns of a workgroup: 16 for little work, where a short path counts, 32 to 128 for more,
+// where a key row should serve many columns.  Work: 16-column tiles times 32-key tiles.  us in
+// replays of a graph, 16 / 32 / 64 / 128 columns with their best splits, 64 nodes, heads of 128 in
+// groups of 2: sequences of 32K on the route, trees that cross a block, one (work 1500) 14.0 / 16.3
+// / 17.7 / 20.8, four (6100) 18.9 / 20.5 / 21.4 / 24.8, eight (12300) 30.1 / 24.8 / 25.8 / 28.0,
+// sixteen (25000) 55.5 / 35.0 / 30.7 / 38.8; dense lists of 8100, one (16400) 31.3 / 26.5 / 27.4 /
+// 34.1, four (66000) 83.8 / 53.8 / 47.1 / 47.2, eight (131000) 160 / 98 / 79.3 / 76.0.
 //
 // Splits fill 256 workgroups, one a compute unit; 128 columns over long lists 512 (eight
 // lists of 32K, 64 nodes in groups of 8: 475 / 290).  64 columns run as workgroups of eight
 // waves, four key groups, where there are no more than 256 of them (32 sequences of 32K, 32 nodes
-// in groups of 2 34.0, with four waves 40.8; 64 sequences 72.7 and 62.0).  So do 16 where at most
-// two splits would fit, which they replace: a merge costs more than the longer walk of one workgroup,
-// up to 32 tiles.  Heads of 128 in groups of 2, 16 nodes, four waves / eight: eight sequences of 8K on
-// the route 14.3 (two splits) / 12.7, of 2K dense 22.9 / 26.5, sixteen 15.2 (one) / 13.9 and 31.2 /
-// 28.5, 24 (more than 256 workgroups) 19.1 / 24.3.
+// in groups of 2 34.0, with four waves 40.8; 64 sequences 72.7 and 62.0).  Up to 32 columns are not
+// split where that would take fewer than twelve tiles off a workgroup's list, for the merge is a
+// launch.  16 nodes, unsplit / in splits: one sequence of 100 tokens 6.7 / 8.3, of 32K 12.3 / 11.1
+// and, crossing a block, 16.9 / 12.7; four of 700 11.4 / 11.7, of 8K 11.3 / 11.8 and 14.9 / 12.5;
+// eight of 8K 11.4 / 13.2 and 16.2 / 15.2, of 32K 13.0 / 13.4 and 19.1 / 17.2.  Eight waves in an
+// unsplit workgroup of 16 columns are no faster (eight of 8K 11.5, of 32K 13.7).
 struct Plan {
     int32_t cols, groups, waves, nsplit;
     int64_t bytes;
@@ -788,17 +787,16 @@ Plan plan_of(int32_t batch, int32_t max_nodes, int32_t Hkv, int32_t G, int32_t d
     const int64_t tiles = (dense ? max_pages : route_pred_count(max_pages - 1, L) + 2) * (B / UNIT);
     const int64_t bh = (int64_t)batch * Hkv;
     const double work = (double)bh * ((cols + 15) / 16) * tiles;
-    p.cols = cols <= 16 || work <= 8000 ? 16 : cols <= 32 ? 32 : cols <= 64 || work <= 100000 ? 64 : 128;
+    p.cols = cols <= 16 || work <= 12000 ? 16 : cols <= 32 || work <= 20000 ? 32 : cols <= 64 || work <= 100000 ? 64 : 128;
     p.groups = (cols + p.cols - 1) / p.cols;
     const int64_t rows = std::max<int64_t>(1, bh * p.groups);
-    const bool one = p.cols == 16 && 3 * rows > PLACES && (tiles <= 32 || 2 * rows > PLACES);  // no split of eight waves
-    p.waves = rows <= PLACES && (p.cols == 64 || one) ? 8 : 4;
+    p.waves = p.cols == 64 && rows <= PLACES ? 8 : 4;
     // turns of a key group with one split
     const int64_t turns = p.cols == 128 ? (tiles + 1) / 2 : (tiles + p.waves - 1) / (p.cols == 64 ? p.waves / 2 : p.waves);
     int64_t n = PLACES / rows;
     if (p.cols == 128 && turns * rows >= 8 * 2 * PLACES) n = 2 * PLACES / rows;
     n = std::min(std::min(n, turns), MOST_SPLITS);
-    p.nsplit = n < 2 || one ? 1 : (int32_t)n;
+    p.nsplit = n < 2 || (p.cols <= 32 && tiles * (n - 1) < 12 * n) ? 1 : (int32_t)n;
     p.bytes = p.nsplit <= 1 ? 0
                             : (rows * p.nsplit * p.cols * (d + 2) * 4 + 15) / 16 * 16 + (bh * 4 + 15) / 16 * 16;
     return p;
@@ -914,8 +912,7 @@ int bf1_attn_tree(const void* Q, const void* K_pages, const void* V_pages, const
     auto nt = [&](auto d_c, auto g_c, auto pw_c) {
         constexpr int D = decltype(d_c)::value, GG = decltype(g_c)::value, PW = decltype(pw_c)::value;
         switch (p.cols) {
-            case 16:
-                return p.waves == 8 ? bf1::launch<D, GG, PW, 1, 1, 8>(a, s) : bf1::launch<D, GG, PW, 1, 1, 4>(a, s);
+            case 16: return bf1::launch<D, GG, PW, 1, 1, 4>(a, s);
             case 32: return bf1::launch<D, GG, PW, 2, 1, 4>(a, s);
             case 64:
                 return p.waves == 8 ? bf1::launch<D, GG, PW, 2, 2, 8>(a, s) : bf1::launch<D, GG, PW, 2, 2, 4>(a, s);

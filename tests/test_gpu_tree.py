@@ -187,7 +187,8 @@ def test_attn_tree_sizes(nodes, G):
 
 @pytest.mark.parametrize("L", [0, 2])
 @pytest.mark.parametrize("copies,Hq,Hkv,nodes,d,B", [(5, 16, 2, 64, 64, 64), (5, 8, 4, 64, 64, 64), (2, 8, 4, 64, 128, 64),
-                                                     (5, 8, 4, 16, 64, 128), (4, 8, 1, 64, 128, 128)])
+                                                     (5, 8, 4, 16, 64, 128), (4, 8, 1, 64, 128, 128),
+                                                     (4, 4, 1, 64, 128, 128)])
 def test_attn_tree_columns(copies, Hq, Hkv, nodes, d, B, L):
     """Batches whose rows run 128, 64 (in workgroups of four and of eight waves) and 32 columns
     at a time: trees that reach into the next block, sequences at blocks' ends."""
@@ -201,11 +202,9 @@ def test_attn_tree_columns(copies, Hq, Hkv, nodes, d, B, L):
 
 @pytest.mark.parametrize("batch,Hq,Hkv,nodes,d,B", [(14, 8, 8, 3, 128, 64), (28, 8, 8, 16, 64, 64), (14, 16, 8, 8, 64, 64),
                                                     (16, 8, 2, 12, 64, 128), (14, 16, 4, 9, 128, 128), (10, 8, 1, 20, 128, 64)])
-def test_attn_tree_eight_waves(batch, Hq, Hkv, nodes, d, B):
-    """16 columns at a time in workgroups of eight waves: as many sequences, heads and nodes as
-    leave room for two splits or none; also with a value that is not finite, which sends its
-    columns over their keys once more."""
-    assert bf1.attn_tree_workspace_size(batch, nodes, Hq, Hkv, d, B, 12) == 0
+def test_attn_tree_short_lists(batch, Hq, Hkv, nodes, d, B):
+    """16 columns at a time, as many sequences, heads and nodes as leave room for two splits or
+    none; also with a value that is not finite, which sends its columns over their keys once more."""
     rng = np.random.default_rng(batch + nodes)
     held = [int(j * B + o) for j, o in zip(rng.integers(0, 10, batch), rng.choice([0, 1, 40, B - 2, B - 1], batch))]
     held[:2] = [9 * B + B - 1, 8 * B + 5]
@@ -271,7 +270,7 @@ def test_attn_tree_rows_without_a_place():
     assert c.run()[0].isnan().all()
 
 
-@pytest.mark.parametrize("Hq,nodes,width", [(4, 16, 0), (2, 20, 20000), (4, 20, 20000), (8, 40, 20000)])  # 16 to 128 columns
+@pytest.mark.parametrize("Hq,nodes,width", [(4, 16, 0), (2, 20, 440), (2, 20, 20000), (4, 20, 20000), (8, 40, 20000)])  # 16 to 128
 @pytest.mark.parametrize("where", ["k", "v"])
 def test_attn_tree_values_that_are_not_finite(where, Hq, nodes, width):
     """A key or value that is not finite reaches the rows that read it, as the formula has
