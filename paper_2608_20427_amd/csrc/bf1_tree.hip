@@ -85,8 +85,8 @@ struct Tree {
     __bf16* O;
     float* LSE;
     float* ws;      // records
-    int32_t* used;  // splits that wrote one, of each (sequence, kv-head)
-    int32_t batch, rows, max_nodes, max_pages, num_pages, Hkv, L, dense, nsplit, groups;
+    int32_t* used;  // splits that wrote one and, with slots, its first slot, of each (sequence, kv-head)
+    int32_t batch, rows, max_nodes, max_pages, num_pages, Hkv, L, dense, nsplit, groups, slots;
     float c_log2;
 };
 
@@ -107,11 +107,55 @@ __device__ __forceinline__ bool on_route(int32_t o, int32_t i, int32_t L) {
     return o <= L || i == 0 || (o >= 4 && (o & (o - 1)) == 0);
 }
 
+// Records of a call's workspace, in front of their columns' maxima and sums.
+__device__ __forceinline__ int64_t records(const Tree& a) {
+    return a.slots > 0 ? (int64_t)a.Hkv * a.slots : (int64_t)a.batch * a.Hkv * a.groups * a.nsplit;
+}
 // What is the same in all lanes, in a scalar register.
 __device__ __forceinline__ int32_t scalar(int32_t x) { return __builtin_amdgcn_readfirstlane(x); }
 // What no kernel of the call writes: one entry for all lanes comes by a scalar load.
 __device__ __forceinline__ const __attribute__((address_space(4))) int32_t* fixed(const int32_t* p) {
     return (const __attribute__((address_space(4))) int32_t*)p;
+}
+
+// Dense lists of unequal length: a kv-head's `slots` workgroups are dealt to the sequences by
+// their tiles, so that the longest share is about the least there is.  A sequence of t tiles
+// gets 1 + floor(t / q) splits, each of as many slots as its nodes have groups; of 64 q, from the
+// mean on, the first whose sum fits.  At 2.2 times the mean it does: fewer than slots / 2.2, and one
+// split of every group, of which there are slots / 2 at most.  Every wave of the call finds the same.
+struct Share {
+    int32_t b, rg, s, n, first;  // the slot's sequence (-1: none), group, which of n splits; b's first slot
+};
+template <int TILE, int NPG>
+__device__ __forceinline__ Share share_of(const Tree& a, int32_t slot, int lane) {
+    int32_t tiles = 0, g = 0;  // of sequence `lane`
+    if (lane < a.batch) {
+        const int32_t start = min(max(a.token_start[lane], 0), a.rows);
+        const int32_t rows = min(max(a.token_start[lane + 1], start), a.rows) - start;
+        g = (min(rows, min(a.max_nodes, MOST_NODES)) + NPG - 1) / NPG;
+        tiles = max(a.before[lane], 0) / TILE + 1;
+    }
+    float total = (float)tiles * (float)g;
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) total += __shfl_xor(total, m);
+    const float per = 1.f / (total * (1.f + (float)lane * (1.25f / 64)) / (float)a.slots + 1.f);
+    int32_t sum = 0;
+    for (int b = 0; b < a.batch; ++b)
+        sum += (1 + (int32_t)((float)__builtin_amdgcn_readlane(tiles, b) * per)) * __builtin_amdgcn_readlane(g, b);
+    const uint64_t fits = __ballot(sum <= a.slots);
+    const float best = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(per), fits ? __builtin_ctzll(fits) : 63));
+    const int32_t n = 1 + (int32_t)((float)tiles * best);
+    int32_t end = n * g;
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) {
+        const int32_t y = __shfl_up(end, m);
+        if (lane >= m) end += y;
+    }
+    const uint64_t here = __ballot(slot >= end - n * g && slot < end);
+    if (here == 0) return {-1, 0, 0, 0, 0};
+    const int b = __builtin_ctzll(here);
+    const int32_t first = __builtin_amdgcn_readlane(end - n * g, b), each = __builtin_amdgcn_readlane(g, b);
+    return {b, (slot - first) % each, (slot - first) / each, __builtin_amdgcn_readlane(n, b), first};
 }
 
 // A workgroup takes 16 NT CW columns (q-heads of neighbouring nodes) of one (sequence,
@@ -159,9 +203,21 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_tree_kernel(Tree a) {
     const int kg = wave / CW, cw = wave % CW;
     // Workgroups go to the XCDs in turns, x first: those of the same keys (y) to one, next to
     // each other.
-    const int rg = blockIdx.y;
+    int rg = blockIdx.y;
     uint32_t bh = blockIdx.z * 8 + blockIdx.x, s = 0;
-    if (a.nsplit > 1) {
+    int32_t splits = a.nsplit, slot = 0, slot0 = 0;
+    if (CW > 1 && a.slots > 0) {
+        const uint32_t id = blockIdx.x * gridDim.z + blockIdx.z, head = id / (uint32_t)a.slots;
+        if (head >= (uint32_t)a.Hkv) return;
+        slot = (int32_t)(id - head * (uint32_t)a.slots);
+        const Share x = share_of<TILE, NPG>(a, slot, lane);
+        if (x.b < 0) return;
+        bh = (uint32_t)(x.b * a.Hkv) + head;
+        rg = x.rg;
+        s = (uint32_t)x.s;
+        splits = x.n;
+        slot0 = x.first;
+    } else if (a.nsplit > 1) {
         const uint32_t work = bh;
         bh = work / (uint32_t)a.nsplit;
         s = work - bh * (uint32_t)a.nsplit;
@@ -276,8 +332,11 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_tree_kernel(Tree a) {
     const int early = scalar(bad ? 0 : count * UPP);
     const int units0 = scalar(bad ? 0 : (rows0 + TILE - 1) / TILE), units1 = scalar(bad ? 0 : (rows1 + TILE - 1) / TILE);
     const int units = early + units0 + units1;  // tiles
-    const int nsb = min(a.nsplit, max(1, (units + KW - 1) / KW));
-    if (a.nsplit > 1 && s == 0 && rg == 0 && tid == 0) a.used[bh] = nsb;
+    const int nsb = min(splits, max(1, (units + KW - 1) / KW));
+    if (a.nsplit > 1 && s == 0 && rg == 0 && tid == 0) {
+        a.used[2 * bh] = nsb;
+        a.used[2 * bh + 1] = slot0;
+    }
     if (s >= nsb) return;
 
     f32x4 acc[NT][DT];
@@ -657,7 +716,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_tree_kernel(Tree a) {
         }
     }
     __syncthreads();
-    const int64_t rec = ((int64_t)bh * a.groups + rg) * a.nsplit + s;
+    const int64_t rec = CW > 1 && a.slots > 0 ? (int64_t)h * a.slots + slot
+                                              : ((int64_t)bh * a.groups + rg) * a.nsplit + s;
     constexpr int PER = THREADS / (D / 4);  // columns at a time, four dims a thread
     const int d = tid % (D / 4) * 4;
 #pragma unroll 1
@@ -686,7 +746,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_tree_kernel(Tree a) {
         } else {
             *reinterpret_cast<f32x4*>(a.ws + (rec * COLS + e) * D + d) = o;
             if (d == 0) {
-                float* ml = a.ws + (int64_t)a.batch * a.Hkv * a.groups * a.nsplit * COLS * D + (rec * COLS + e) * 2;
+                float* ml = a.ws + records(a) * COLS * D + (rec * COLS + e) * 2;
                 ml[0] = M;
                 ml[1] = l;
             }
@@ -695,16 +755,28 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_tree_kernel(Tree a) {
 }
 
 // Sum of the splits' records, in split order: 256 threads, four dims each, of as many
-// columns.  Up to eight records are asked for before what says how many there are.
-template <int D, int G, int COLS>
+// columns.  Up to eight records are asked for before what says how many there are; where a
+// sequence's first slot has to be known (SLOTS), behind it.
+template <int D, int G, int COLS, bool SLOTS>
 __global__ __launch_bounds__(THREADS) void merge_tree_kernel(Tree a) {
     constexpr int TPC = D / 4, PER = THREADS / TPC;  // columns of a workgroup
     const int rg = blockIdx.y;
     const int64_t bh = blockIdx.z;
     const int b = (int)(blockIdx.z / (uint32_t)a.Hkv), h = (int)bh - b * a.Hkv;
     const int e = blockIdx.x * PER + threadIdx.x / TPC, d = threadIdx.x % TPC * 4;
-    const int64_t rec0 = (bh * a.groups + rg) * a.nsplit;
-    const float* ml = a.ws + (int64_t)a.batch * a.Hkv * a.groups * a.nsplit * COLS * D + (rec0 * COLS + e) * 2;
+    int64_t rec0 = (bh * a.groups + rg) * a.nsplit;
+    int32_t last = a.nsplit - 1, step = 1;  // the last record, and how far they are apart
+    const int node = rg * (COLS / G) + e / G;
+    const int start = min(max(fixed(a.token_start)[b], 0), a.rows);
+    const int count = min(max(fixed(a.token_start)[b + 1], start), a.rows) - start;
+    if constexpr (SLOTS) {
+        const int nodes = min(count, min(a.max_nodes, MOST_NODES));
+        if (node >= nodes) return;
+        last = fixed(a.used)[2 * bh] - 1;
+        step = (nodes + COLS / G - 1) / (COLS / G);
+        rec0 = (int64_t)h * a.slots + fixed(a.used)[2 * bh + 1] + rg;
+    }
+    const float* ml = a.ws + records(a) * COLS * D + (rec0 * COLS + e) * 2;
     const float* src = a.ws + (rec0 * COLS + e) * D + d;
     constexpr int U = 8;
     float mq[U], lq[U];
@@ -712,17 +784,14 @@ __global__ __launch_bounds__(THREADS) void merge_tree_kernel(Tree a) {
     auto load = [&](int q0) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int64_t q = min(q0 + u, a.nsplit - 1);
+            const int64_t q = (int64_t)min(q0 + u, last) * step;
             mq[u] = ml[q * COLS * 2];
             lq[u] = ml[q * COLS * 2 + 1];
             oq[u] = *reinterpret_cast<const f32x4*>(src + q * COLS * D);
         }
     };
     load(0);
-    const int nsb = fixed(a.used)[bh];
-    const int start = min(max(fixed(a.token_start)[b], 0), a.rows);
-    const int count = min(max(fixed(a.token_start)[b + 1], start), a.rows) - start;
-    const int node = rg * (COLS / G) + e / G;
+    const int nsb = fixed(a.used)[2 * bh];
     if (node >= min(count, min(a.max_nodes, MOST_NODES))) return;  // used was not written where there is none
     if (nsb <= 1) return;                                          // the result stands there already
     float M = -INFINITY, l = 0.f;
@@ -775,8 +844,13 @@ __global__ __launch_bounds__(THREADS) void merge_tree_kernel(Tree a) {
 // and, crossing a block, 16.9 / 12.7; four of 700 11.4 / 11.7, of 8K 11.3 / 11.8 and 14.9 / 12.5;
 // eight of 8K 11.4 / 13.2 and 16.2 / 15.2, of 32K 13.0 / 13.4 and 19.1 / 17.2.  Eight waves in an
 // unsplit workgroup of 16 columns are no faster (eight of 8K 11.5, of 32K 13.7).
+//
+// Dense lists of up to 64 sequences that run 64 or 128 columns and are split have as many splits in
+// all, but each sequence its share (share_of).  Heads of 128, 64 nodes in groups of 8, equal splits /
+// shares: one list of 32K among seven of 1K 247 / 93, lists of 32K, 16K, .. 250 248 / 129, eight of 18
+// to 32K with 32 to 64 nodes 275 / 267, eight of 32K 406 / 409; in groups of 2, eight of 8K 76.4 / 79.0.
 struct Plan {
-    int32_t cols, groups, waves, nsplit;
+    int32_t cols, groups, waves, nsplit, slots;
     int64_t bytes;
 };
 constexpr int64_t PLACES = 256, MOST_SPLITS = 32;
@@ -797,22 +871,27 @@ Plan plan_of(int32_t batch, int32_t max_nodes, int32_t Hkv, int32_t G, int32_t d
     if (p.cols == 128 && turns * rows >= 8 * 2 * PLACES) n = 2 * PLACES / rows;
     n = std::min(std::min(n, turns), MOST_SPLITS);
     p.nsplit = n < 2 || (p.cols <= 32 && tiles * (n - 1) < 12 * n) ? 1 : (int32_t)n;
+    p.slots = dense && p.cols >= 64 && p.nsplit > 1 && batch > 1 && batch <= 64 ? p.nsplit * (int32_t)rows / Hkv : 0;
     p.bytes = p.nsplit <= 1 ? 0
-                            : (rows * p.nsplit * p.cols * (d + 2) * 4 + 15) / 16 * 16 + (bh * 4 + 15) / 16 * 16;
+                            : (rows * p.nsplit * p.cols * (d + 2) * 4 + 15) / 16 * 16 + (bh * 8 + 15) / 16 * 16;
     return p;
 }
 
 template <int D, int G, int PW, int NT, int CW, int WAVES>
 hipError_t launch(const Tree& a, hipStream_t s) {
     constexpr int COLS = 16 * NT * CW;
-    const int64_t work = ((int64_t)a.batch * a.Hkv * a.nsplit + 7) / 8;
-    hipLaunchKernelGGL((attn_tree_kernel<D, G, PW, NT, CW, WAVES>), dim3(8, (unsigned)a.groups, (unsigned)work),
+    const int64_t work = ((int64_t)a.Hkv * (a.slots > 0 ? a.slots : (int64_t)a.batch * a.nsplit) + 7) / 8;
+    hipLaunchKernelGGL((attn_tree_kernel<D, G, PW, NT, CW, WAVES>),
+                       dim3(8, (unsigned)(a.slots > 0 ? 1 : a.groups), (unsigned)work),
                        dim3(64 * WAVES), 0, s, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.nsplit <= 1) return e;
     constexpr int PARTS = COLS / (THREADS / (D / 4));
-    hipLaunchKernelGGL((merge_tree_kernel<D, G, COLS>), dim3(PARTS, (unsigned)a.groups, (unsigned)(a.batch * a.Hkv)),
-                       dim3(THREADS), 0, s, a);
+    const dim3 grid(PARTS, (unsigned)a.groups, (unsigned)(a.batch * a.Hkv));
+    if (a.slots > 0)
+        hipLaunchKernelGGL((merge_tree_kernel<D, G, COLS, true>), grid, dim3(THREADS), 0, s, a);
+    else
+        hipLaunchKernelGGL((merge_tree_kernel<D, G, COLS, false>), grid, dim3(THREADS), 0, s, a);
     return hipGetLastError();
 }
 
@@ -884,7 +963,7 @@ int bf1_attn_tree(const void* Q, const void* K_pages, const void* V_pages, const
     const bf1::Plan p = bf1::plan_of(batch, max_nodes, Hkv, G, head_dim, B, max_pages_per_seq, L, dense);
     if (p.bytes > 0 && !bf1::aligned(workspace, 16)) return BF1_ERR_INVALID_ARG;
     if (workspace_bytes < p.bytes) return BF1_ERR_BUFFER_TOO_SMALL;
-    const int64_t used = ((int64_t)batch * Hkv * 4 + 15) / 16 * 16;
+    const int64_t used = ((int64_t)batch * Hkv * 8 + 15) / 16 * 16;
     bf1::Tree a{(const __bf16*)Q,
                 (const __bf16*)K_pages,
                 (const __bf16*)V_pages,
@@ -907,6 +986,7 @@ int bf1_attn_tree(const void* Q, const void* K_pages, const void* V_pages, const
                 dense,
                 p.nsplit,
                 p.groups,
+                p.slots,
                 bf1::LOG2E / sqrtf((float)head_dim)};
     hipStream_t s = (hipStream_t)stream;
     auto nt = [&](auto d_c, auto g_c, auto pw_c) {

@@ -241,6 +241,28 @@ def test_attn_tree_long_lists_split():
     c.check(c.run())
 
 
+@pytest.mark.parametrize("batch,G,Hkv,nodes,d,B", [(5, 8, 1, 64, 64, 64), (5, 4, 2, 16, 128, 128), (2, 8, 1, 33, 128, 64),
+                                                   (64, 8, 1, 8, 64, 64), (65, 8, 1, 8, 64, 64), (19, 2, 3, 40, 64, 128)])
+def test_attn_tree_unequal_dense_lists(batch, G, Hkv, nodes, d, B):
+    """Dense lists under a wide table, whose splits go by each sequence's length: one long one
+    among short and empty ones, sequences that draft nothing or lack a page."""
+    rng = np.random.default_rng(batch + nodes)
+    held = [2500] + [int(x) for x in rng.choice([0, 1, B - 1, B, 300, 900], batch - 1)]
+    counts = [nodes] + [int(x) for x in rng.integers(0, nodes + 1, batch - 1)]
+    counts[-1] = 0 if batch > 2 else 1
+    for h in (held, held[::-1]):
+        n = counts if h is held else counts[::-1]
+        c = Case(h, n, G * Hkv, Hkv, d, B, seed=batch, width=2000)
+        assert bf1.attn_tree_workspace_size(batch, nodes, G * Hkv, Hkv, d, B, c.width, dense=True) > 0
+        got = c.run(dense=True, max_nodes=nodes)
+        c.check(got, dense=True)
+        assert all(torch.equal(x, y) for x, y in zip(got, c.run(dense=True, max_nodes=nodes)))
+    c.table[-1, 3] = -1  # of the long one
+    o, lse = c.run(dense=True, max_nodes=nodes)
+    assert o[c.start[-2]:].isnan().all() and lse[c.start[-2]:].isnan().all()
+    assert torch.equal(o[:c.start[-2]], got[0][:c.start[-2]]) and o[:c.start[-2]].isfinite().all()
+
+
 def test_attn_tree_wide_batch():
     rng = np.random.default_rng(8)
     c = Case(rng.integers(0, 400, 150), list(rng.integers(0, 20, 150)), 4, 2, 64, 64, seed=8)
