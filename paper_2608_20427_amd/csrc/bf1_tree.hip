@@ -176,9 +176,9 @@ __device__ __forceinline__ Share share_of(const Tree& a, int32_t slot, int lane)
 //
 // Bound by the matrix cores where trees are large (weights in two parts make 3/2 of the
 // products; the chip's power limit holds them to some 1 PFLOP/s) and by latency where there
-// is little to read.  Replays of a graph: eight dense lists of 16-32K, up to 64 nodes in groups
-// of 8, pages of 128 291 us (155 GFLOP, 0.4 GB), 32 sequences of 16-32K on the route, up to 32
-// nodes in groups of 2 32 us (93 MB), one sequence of 32K, 16 nodes, 11.1 us with its merge.
+// is little to read.  Replays of a graph: eight dense lists of 18-32K, up to 64 nodes in groups
+// of 8, pages of 128 272 us (155 GFLOP, 0.4 GB), 32 sequences of 16-32K on the route, up to 32
+// nodes in groups of 2 31 us (93 MB), one sequence of 32K, 16 nodes, 10.6 us with its merge.
 //
 // A key that a row does not read has weight 0 and does nothing, as long as its value is
 // finite.  Where an accumulator is not finite at the end, the wave goes over its keys
