@@ -76,6 +76,7 @@ __global__ __launch_bounds__(THREADS) void tree_step_kernel(const int32_t* __res
 // Attention
 // ---------------------------------------------------------------------------
 constexpr int UNIT = 32;       // keys of a wave's step
+constexpr int PARTS = 3;       // bf16 parts of a weight: all 24 bits of it
 constexpr int MAX_LIST = 96;   // 28 + 28 + 1 + 32: earlier blocks that nodes of two neighbouring blocks read, L <= 32
 
 struct Tree {
@@ -478,32 +479,38 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_tree_kernel(Tree a) {
                 l_run[c] += sc[x][r];
             }
     };
-    // Weights of 32 keys as two bf16 parts.
-    auto split = [&](const f32x4* sc, bf16x8& hi, bf16x8& lo) {
-        u32x4 h, l;
+    // Weights of 32 keys as three bf16 parts, each the rounded rest of the ones before.
+    struct Parts {
+        bf16x8 p[PARTS];
+    };
+    auto split = [&](const f32x4* sc) {
+        Parts w;
+        u32x4 h[PARTS];
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
             typedef float f32x2 __attribute__((ext_vector_type(2)));
-            const f32x2 w = {sc[x / 2][x % 2 * 2], sc[x / 2][x % 2 * 2 + 1]};
-            h[x] = __builtin_bit_cast(uint32_t, __builtin_convertvector(w, bf16x2));
-            const f32x2 rest = {w[0] - __uint_as_float(h[x] << 16), w[1] - __uint_as_float(h[x] & 0xffff0000u)};
-            l[x] = __builtin_bit_cast(uint32_t, __builtin_convertvector(rest, bf16x2));
+            f32x2 rest = {sc[x / 2][x % 2 * 2], sc[x / 2][x % 2 * 2 + 1]};
+#pragma unroll
+            for (int i = 0; i < PARTS; ++i) {
+                h[i][x] = __builtin_bit_cast(uint32_t, __builtin_convertvector(rest, bf16x2));
+                rest = f32x2{rest[0] - __uint_as_float(h[i][x] << 16), rest[1] - __uint_as_float(h[i][x] & 0xffff0000u)};
+            }
         }
-        hi = __builtin_bit_cast(bf16x8, h);
-        lo = __builtin_bit_cast(bf16x8, l);
+#pragma unroll
+        for (int i = 0; i < PARTS; ++i) w.p[i] = __builtin_bit_cast(bf16x8, h[i]);
+        return w;
     };
     // Their products with 16-wide tiles d and d + 1 of 32 V rows: two transpose reads each.
-    auto both = [&](int d, const bf16x8 (&hi)[NT], const bf16x8 (&lo)[NT], u32x2 v0, u32x2 v1, u32x2 v2, u32x2 v3) {
+    auto both = [&](int d, const Parts (&w)[NT], u32x2 v0, u32x2 v1, u32x2 v2, u32x2 v3) {
         const bf16x8 vt[2] = {__builtin_bit_cast(bf16x8, u32x4{v0[0], v0[1], v1[0], v1[1]}),
                               __builtin_bit_cast(bf16x8, u32x4{v2[0], v2[1], v3[0], v3[1]})};
 #pragma unroll
-        for (int part = 0; part < 2; ++part)
+        for (int part = 0; part < PARTS; ++part)
 #pragma unroll
             for (int y = 0; y < 2; ++y)
 #pragma unroll
                 for (int c = 0; c < NT; ++c)
-                    acc[c][d + y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt[y], part ? lo[c] : hi[c], acc[c][d + y], 0, 0,
-                                                                           0);
+                    acc[c][d + y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt[y], w[c].p[part], acc[c][d + y], 0, 0, 0);
     };
     clear();
     if constexpr (CW == 1) {
@@ -532,11 +539,11 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_tree_kernel(Tree a) {
             }
             __builtin_amdgcn_sched_barrier(0);
             mask_scores(w, 0, sc);
-            bf16x8 hi[NT], lo[NT];
+            Parts weights[NT];
 #pragma unroll
             for (int c = 0; c < NT; ++c) {
                 soften(c, sc[c], std::false_type{});
-                split(sc[c], hi[c], lo[c]);
+                weights[c] = split(sc[c]);
             }
 #pragma unroll
             for (int d = 0; d < DT; d += 2) {
@@ -548,7 +555,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_tree_kernel(Tree a) {
                     : "=&v"(v0), "=&v"(v1), "=&v"(v2), "=&v"(v3)
                     : "v"((vtr ^ (32 * d)) + buf * BUF_LDS), "v"((vtr ^ (32 * d + 32)) + buf * BUF_LDS), "i"(16 * RB)
                     : "memory");
-                both(d, hi, lo, v0, v1, v2, v3);
+                both(d, weights, v0, v1, v2, v3);
             }
         };
         if (u0 < units) {
@@ -619,15 +626,15 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_tree_kernel(Tree a) {
             ask(SEGS / 2, SEGS / 4 * 3);
 #pragma unroll
             for (int sub = 0; sub < SUBS; ++sub) {
-                bf16x8 hi[NT], lo[NT];
+                Parts weights[NT];
 #pragma unroll
-                for (int c = 0; c < NT; ++c) split(sc[c] + 2 * sub, hi[c], lo[c]);
+                for (int c = 0; c < NT; ++c) weights[c] = split(sc[c] + 2 * sub);
 #pragma unroll
                 for (int half = 0; half < 2; ++half) {
                     if (half == 0 || sub + 1 < SUBS) fetch(half ^ 1, sub + half, half ^ 1);
 #pragma unroll
                     for (int d = 0; d < HALF; d += 2)
-                        both(half * HALF + d, hi, lo, v[half][d][0], v[half][d][1], v[half][d + 1][0], v[half][d + 1][1]);
+                        both(half * HALF + d, weights, v[half][d][0], v[half][d][1], v[half][d + 1][0], v[half][d + 1][1]);
                     if (sub == 0 && half == 0) ask(SEGS / 4 * 3, SEGS);
                 }
             }
@@ -886,8 +893,7 @@ hipError_t launch(const Tree& a, hipStream_t s) {
                        dim3(64 * WAVES), 0, s, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.nsplit <= 1) return e;
-    constexpr int PARTS = COLS / (THREADS / (D / 4));
-    const dim3 grid(PARTS, (unsigned)a.groups, (unsigned)(a.batch * a.Hkv));
+    const dim3 grid(COLS / (THREADS / (D / 4)), (unsigned)a.groups, (unsigned)(a.batch * a.Hkv));
     if (a.slots > 0)
         hipLaunchKernelGGL((merge_tree_kernel<D, G, COLS, true>), grid, dim3(THREADS), 0, s, a);
     else

@@ -333,6 +333,53 @@ def test_attn_tree_infinity_under_a_small_weight(Hq, nodes, width):
     assert rest.isfinite().all() and got[1].isfinite().all()
 
 
+def bf16(x):
+    return f64(torch.as_tensor(x).bfloat16())
+
+
+@pytest.mark.parametrize("batch,Hq,nodes,width,d,B", [(2, 2, 8, 0, 64, 64), (2, 4, 16, 0, 128, 128), (2, 2, 20, 20000, 64, 128),
+                                                      (2, 4, 20, 20000, 128, 64), (130, 4, 20, 200, 64, 64),
+                                                      (2, 8, 40, 20000, 64, 64), (2, 8, 33, 20000, 128, 128)])  # 16 to 128 columns
+def test_attn_tree_weights_keep_their_24_bits(batch, Hq, nodes, width, d, B):
+    """Values that cancel all of a weight but what two bf16 parts leave out of it.
+
+    Rows read three committed keys: two of 0 and one whose score, -t / sqrt(d), gives it the
+    weight p in [0.5, 1), another one for each row.  Dim i of the values is -hi, -mid and 1, hi and mid the
+    rounded parts of row i's p: row i's output is (p - hi - mid) / (2 + p), below 2^-18.
+
+    Bar: the largest score is 0, so a weight's exponent, of size 0.73 at most, is off by three
+    roundings of log2(e) / sqrt(d) and its own, 3.2 * 2^-24, times ln 2 of p, and exp2 by one
+    step: 3.3 * 2^-24.  Parts and values are whole numbers of 2^-24, but for the tiniest middle
+    parts, and partial sums below 1: they round by 2^-24 in all.  The quotient is off by 2^-22 of
+    itself, and rounded once, 2^-8."""
+    none = lambda c, rng: [0] * len(c.masks)  # noqa: E731
+    c = Case([3] * batch, [nodes] * batch, Hq, 2, d, B, seed=1, width=width, masks=none)
+    rows = batch * nodes
+    at = (np.arange(rows * Hq) % d).reshape(rows, Hq)
+    t = (2 + at / 64) * (1 if d == 64 else 1.25)  # bf16 numbers
+    t = bf16(t)
+    c.q[:] = 0
+    c.q[:, :, 0] = torch.as_tensor(t).bfloat16()
+    p = np.exp(-t / np.sqrt(d))
+    assert (p >= 0.5).all() and (p < 1).all()
+    parts = np.zeros((3, d))
+    parts[0][at] = -bf16(p)
+    parts[1][at] = -bf16(p - bf16(p))
+    parts[2] = 1
+    first = c.table[:, 0]
+    for i in range(3):
+        c.k[first, :, i] = 0
+        c.v[first, :, i] = torch.as_tensor(parts[i]).bfloat16()
+    c.k[first, :, 2, 0] = -1
+    o, lse = c.run(dense=width > 0, max_nodes=nodes)
+    want = (p[..., None] + parts[0] + parts[1]) / (2 + p[..., None])
+    bar = 4.3 * 2.0 ** -24 / (2 + p[..., None]) + 2.0 ** -22 * np.abs(want)
+    bar = bar + 2.0 ** -8 * (np.abs(want) + bar)
+    off = np.abs(f64(o) - want)
+    assert (off <= bar).all(), (off - bar).max()
+    assert np.abs(f64(lse) - np.log(2 + p)).max() < 2.0 ** -21
+
+
 def test_attn_tree_missing_pages():
     for entry, dense in ((0, False), (3, True), (8, False), (9, False)):
         c = Case([600, 100], [40, 4], 4, 2, 64, 64, seed=10, deep=True)
