@@ -531,7 +531,7 @@ int bf1_qk_norm_rope_bwd(const void* dQ, const void* dK, int32_t grad_type, cons
  * number is max_nodes or more, or whose sequence lacks a page that some node of it reads,
  * gets NaN; a row that reads nothing 0 and LSE -infinity.  Rows behind the last tree are
  * left as they are.  What a row does not read does nothing, whatever it holds.  Weights
- * are applied with 16 bits, sums are fp32; deterministic.  head_dim and B in {64, 128},
+ * are applied with their 24 bits, sums are fp32; deterministic.  head_dim and B in {64, 128},
  * Hq / Hkv in {1, 2, 4, 8}, L <= 32.
  */
 int bf1_tree_step(const int32_t* parents, const int32_t* token_start, const int32_t* seq_lens_before,

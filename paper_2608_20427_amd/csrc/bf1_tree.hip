@@ -166,8 +166,10 @@ __device__ __forceinline__ Share share_of(const Tree& a, int32_t slot, int lane)
 // Scores S = K Q^T on 16x16x32 tiles: A = K rows (lane l: key l % 16, 16-byte chunk 4 s +
 // l / 16), B = Q rows, so lane l holds keys 4 (l / 16) + 0..3 of each of a unit's two tiles
 // and column l % 16: the eight of them are the B operand of O^T += V^T P^T as they stand.  A
-// weight goes in as two bf16 parts (16 of its bits: what is left out is below 2^-17 of it,
-// the output is rounded to 2^-9), its sum in fp32.
+// weight goes in as three bf16 parts that add up to the fp32 value, as in the decodes over the
+// cache, so that a token is verified with the products it is decoded with.  Two parts (16 bits)
+// take less, us in replays: the three cases below 265, 29.9 and 10.5, but leave 2^-18 of a weight
+// out, which shows where values cancel and now and then in the output's rounding.
 //
 // CW = 1: K rows go straight to registers, V rows through the wave's own LDS by transpose
 // reads, both asked for a unit ahead.  CW > 1: the waves of a key group share its tiles in
@@ -175,11 +177,11 @@ __device__ __forceinline__ Share share_of(const Tree& a, int32_t slot, int lane)
 // a K row r lies at c ^ (r & 7), 32-byte slots of V rows at s ^ vslot(r), so that no read has
 // a bank conflict.
 //
-// Bound by the matrix cores where trees are large (weights in two parts make 3/2 of the
+// Bound by the matrix cores where trees are large (weights in three parts make twice the
 // products; the chip's power limit holds them to some 1 PFLOP/s) and by latency where there
 // is little to read.  Replays of a graph: eight dense lists of 18-32K, up to 64 nodes in groups
-// of 8, pages of 128 272 us (155 GFLOP, 0.4 GB), 32 sequences of 16-32K on the route, up to 32
-// nodes in groups of 2 31 us (93 MB), one sequence of 32K, 16 nodes, 10.6 us with its merge.
+// of 8, pages of 128 317 us (155 GFLOP, 0.4 GB), 32 sequences of 16-32K on the route, up to 32
+// nodes in groups of 2 32 us (93 MB), one sequence of 32K, 16 nodes, 10.5 us with its merge.
 //
 // A key that a row does not read has weight 0 and does nothing, as long as its value is
 // finite.  Where an accumulator is not finite at the end, the wave goes over its keys
