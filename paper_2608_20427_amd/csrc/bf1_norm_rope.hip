@@ -24,6 +24,7 @@
 #include "../../include/bf1.h"
 #include "bf1_device.h"
 #include "bf1_rotary.h"
+#include "bf1_team.h"
 
 // every instance rounds the same way: contraction only where it is written
 #pragma clang fp contract(off)
@@ -36,40 +37,6 @@ constexpr int THREADS = 256;
 int status_of(hipError_t e) { return e == hipSuccess ? BF1_OK : BF1_ERR_HIP; }
 bool aligned(const void* p, uintptr_t a) { return p != nullptr && reinterpret_cast<uintptr_t>(p) % a == 0; }
 bool launchable(int64_t blocks) { return blocks < (int64_t(1) << 32) / THREADS; }
-
-// A row (one head of one token) belongs to a team of 1 << `lshift` lanes of one wave.  A
-// lane holds P elements from `a` and P from `b` on: the two halves of P pairs, 2 P
-// elements of pairs that lie side by side, or 2 P of the rest behind the pairs.  P is
-// what 16 bytes hold of x, also where rows are read element by element (na, nb: how
-// many there are), so that a row's sums do not go by its alignment.
-template <typename T>
-constexpr int PAIRS = 16 / sizeof(T);
-
-struct Lane {
-    int32_t a, b, na, nb;
-    bool turn;
-    int32_t pair, pairs;  // first pair and their number
-};
-template <bool INTER, int P>
-__device__ __forceinline__ Lane lane_of(int32_t l, int32_t d, int32_t half) {
-    const int32_t units = (half + P - 1) / P;
-    Lane x;
-    x.turn = l < units;
-    x.pair = l * P;
-    x.pairs = x.turn ? min(P, half - l * P) : 0;
-    if (x.turn && !INTER) {
-        x.a = l * P;
-        x.b = half + l * P;
-        x.na = x.nb = x.pairs;
-    } else {
-        x.a = x.turn ? 2 * l * P : 2 * half + 2 * (l - units) * P;
-        x.b = x.a + P;
-        const int32_t end = x.turn ? 2 * half : d;
-        x.na = min(max(end - x.a, 0), P);
-        x.nb = min(max(end - x.b, 0), P);
-    }
-    return x;
-}
 
 template <typename T, int P>
 __device__ __forceinline__ void load_vec(const T* p, float* f) {
@@ -227,9 +194,8 @@ __device__ __forceinline__ float root(float sum, const Shape& z) {
 // 256 lanes: teams of neighbouring tokens, `chunk` heads each, one after the other, so that a
 // lane's cosines and sines serve them all; workgroups follow each other over the heads of
 // the same tokens.
-template <typename T, typename TO, bool INTER, bool WIDE>
+template <typename T, typename TO, bool INTER, bool WIDE, int P>
 __global__ __launch_bounds__(THREADS) void norm_rope_kernel(Side q, Side k, Shape z) {
-    constexpr int P = PAIRS<T>;
     const uint32_t group = blockIdx.x / z.hsplit;
     const uint32_t item = group * THREADS + threadIdx.x;
     const bool live = item < z.items;
@@ -273,11 +239,10 @@ __global__ __launch_bounds__(THREADS) void norm_rope_kernel(Side q, Side k, Shap
 // meet in LDS and write one record [d], which the next kernel sums over
 // the workgroups, in their order.  The records go by the call's sizes alone, so the
 // result is the same each time.
-template <typename T, typename TD, typename TO, bool INTER, bool WIDE>
+template <typename T, typename TD, typename TO, bool INTER, bool WIDE, int P>
 __global__ __launch_bounds__(THREADS) void norm_rope_bwd_kernel(Side q, Side k, Shape z, uint32_t q_groups,
                                                                 float* __restrict__ q_dgain, float* __restrict__ k_dgain,
                                                                 float* __restrict__ records) {
-    constexpr int P = PAIRS<T>;
     __shared__ __align__(16) float part[THREADS * 2 * P];
     const Lane x = lane_of<INTER, P>((int32_t)(threadIdx.x & ((1u << z.lshift) - 1)), z.d, z.half);
     const bool isk = blockIdx.x >= q_groups;
@@ -371,13 +336,6 @@ __global__ __launch_bounds__(SUM_THREADS) void gain_sum_kernel(const float* __re
 // A dimension's stride where it is used: one with a single entry may have any.
 int64_t used(int64_t stride, int64_t entries) { return entries > 1 ? stride : 0; }
 
-int32_t team_shift(int32_t d, int32_t half, int32_t P) {
-    const int32_t units = (half + P - 1) / P + (d - 2 * half + 2 * P - 1) / (2 * P);
-    int32_t s = 0;
-    while ((1 << s) < units) ++s;
-    return s;
-}
-
 // Heads of a workgroup: as many as leave some 768 workgroups, three a compute unit, for
 // angles are the dearest part of a row (a double product, a reduction, cosine and sine of
 // every pair) and serve all of them; in equal parts.  us, 16 + 8 heads of 128, forward with 1 /
@@ -425,7 +383,7 @@ int check_sizes(int64_t batch, int64_t n, int32_t Hq, int32_t Hkv, int32_t d, in
     if (d < 2 || d > 512 || d % 2 || rot < 2 || rot > d || rot % 2) return BF1_ERR_UNSUPPORTED;
     if (n >= (int64_t(1) << 31) || Hq + (int64_t)Hkv > 65535) return BF1_ERR_UNSUPPORTED;
     if (batch == 0 || n == 0 || Hq + Hkv == 0) return BF1_OK;
-    const int32_t P = type == BF1_TYPE_BF16 ? 8 : 4, lshift = team_shift(d, rot / 2, P);
+    const int32_t lshift = team_shift(d, rot / 2, pairs_of(type == BF1_TYPE_BF16 ? 2 : 4, d, rot / 2));
     if ((double)batch * n * (1 << lshift) >= 2147483648.0) return BF1_ERR_UNSUPPORTED;
     if (!launchable((((batch * n) << lshift) / THREADS + 1) * (Hq + Hkv))) return BF1_ERR_UNSUPPORTED;
     *rows = batch * n;
@@ -481,12 +439,12 @@ int bf1_qk_norm_rope(const void* Q, const void* K, const void* q_gain, const voi
     if (rows == 0) return BF1_OK;
     if (!bf1::aligned(positions, 4) || !bf1::aligned(freqs, 8)) return BF1_ERR_INVALID_ARG;
     const int64_t esize = in_type == BF1_TYPE_BF16 ? 2 : 4, osize = out_type == BF1_TYPE_BF16 ? 2 : 4;
-    const int64_t gsize = gain_type == BF1_TYPE_BF16 ? 2 : 4, P = 16 / esize;
+    const int64_t gsize = gain_type == BF1_TYPE_BF16 ? 2 : 4;
     if ((q_gain && !bf1::aligned(q_gain, gsize)) || (k_gain && !bf1::aligned(k_gain, gsize))) return BF1_ERR_INVALID_ARG;
     // a side's output is read by no other row's lanes: it is not the other side's input or output
     if (Hq > 0 && Hkv > 0 && (Q_out == K_out || Q_out == K || K_out == Q)) return BF1_ERR_INVALID_ARG;
-    const int32_t half = rot_dim / 2;
-    bool wide = half % P == 0 && (head_dim - rot_dim) % P == 0;
+    const int32_t half = rot_dim / 2, P = bf1::pairs_of((int32_t)esize, head_dim, half);
+    bool wide = P * esize == 16 && half % P == 0 && (head_dim - rot_dim) % P == 0;
     for (const void* g : {q_gain, k_gain}) wide = wide && (!g || bf1::aligned(g, 16));
     bf1::Side side[2];
     for (int i = 0; i < 2; ++i) {
@@ -505,7 +463,7 @@ int bf1_qk_norm_rope(const void* Q, const void* K, const void* q_gain, const voi
         if (in == out && (in_type != out_type || x.b != o.b || x.h != o.h || x.t != o.t)) return BF1_ERR_INVALID_ARG;
         wide = wide && bf1::wide_rows(x, P, esize) && bf1::wide_rows(o, P, osize);
     }
-    const int32_t lshift = bf1::team_shift(head_dim, half, (int32_t)P);
+    const int32_t lshift = bf1::team_shift(head_dim, half, P);
     const int64_t groups = ((rows << lshift) + bf1::THREADS - 1) / bf1::THREADS;
     const int32_t heads = Hq + Hkv;
     const int32_t chunk = bf1::heads_each(groups, heads, heads, 12);
@@ -522,7 +480,9 @@ int bf1_qk_norm_rope(const void* Q, const void* K, const void* q_gain, const voi
         using T = decltype(in_c);
         using TO = decltype(out_c);
         constexpr bool I = decltype(inter_c)::value;
-        return wide ? go(bf1::norm_rope_kernel<T, TO, I, true>) : go(bf1::norm_rope_kernel<T, TO, I, false>);
+        constexpr int N = 16 / sizeof(T);
+        if (P != N) return go(bf1::norm_rope_kernel<T, TO, I, false, 8>);
+        return wide ? go(bf1::norm_rope_kernel<T, TO, I, true, N>) : go(bf1::norm_rope_kernel<T, TO, I, false, N>);
     };
     auto types = [&](auto inter_c) {
         if (in_type == BF1_TYPE_BF16) return pick((__bf16)0, (__bf16)0, inter_c);
@@ -539,7 +499,8 @@ int bf1_qk_norm_rope_bwd_workspace_size(int32_t batch, int64_t n, int32_t Hq, in
     if (bad != BF1_OK) return bad;
     *bytes = 0;
     if (rows == 0) return BF1_OK;
-    const int32_t lshift = bf1::team_shift(head_dim, rot_dim / 2, in_type == BF1_TYPE_BF16 ? 8 : 4);
+    const int32_t P = bf1::pairs_of(in_type == BF1_TYPE_BF16 ? 2 : 4, head_dim, rot_dim / 2);
+    const int32_t lshift = bf1::team_shift(head_dim, rot_dim / 2, P);
     *bytes = bf1::record_bytes(bf1::bwd_plan(rows, Hq, Hkv, lshift), head_dim);
     return BF1_OK;
 }
@@ -561,8 +522,8 @@ int bf1_qk_norm_rope_bwd(const void* dQ, const void* dK, int32_t grad_type, cons
     if ((dq_gain && !bf1::aligned(dq_gain, 4)) || (dk_gain && !bf1::aligned(dk_gain, 4)) || (dq_gain && dq_gain == dk_gain))
         return BF1_ERR_INVALID_ARG;
     const int64_t esize = in_type == BF1_TYPE_BF16 ? 2 : 4, osize = out_type == BF1_TYPE_BF16 ? 2 : 4;
-    const int64_t dsize = grad_type == BF1_TYPE_BF16 ? 2 : 4, gsize = gain_type == BF1_TYPE_BF16 ? 2 : 4, P = 16 / esize;
-    const int32_t half = rot_dim / 2;
+    const int64_t dsize = grad_type == BF1_TYPE_BF16 ? 2 : 4, gsize = gain_type == BF1_TYPE_BF16 ? 2 : 4;
+    const int32_t half = rot_dim / 2, P = bf1::pairs_of((int32_t)esize, head_dim, half);
     hipStream_t stm = (hipStream_t)stream;
     const dim3 sum_groups((unsigned)((head_dim + bf1::SUM_COLS - 1) / bf1::SUM_COLS), 2);
     if (rows == 0) {  // sums over nothing
@@ -575,7 +536,7 @@ int bf1_qk_norm_rope_bwd(const void* dQ, const void* dK, int32_t grad_type, cons
     if ((q_gain && !bf1::aligned(q_gain, gsize)) || (k_gain && !bf1::aligned(k_gain, gsize))) return BF1_ERR_INVALID_ARG;
     if (Hq > 0 && Hkv > 0 && (dQ_in == dK_in || dQ_in == dK || dK_in == dQ || dQ_in == K || dK_in == Q))
         return BF1_ERR_INVALID_ARG;
-    bool wide = half % P == 0 && (head_dim - rot_dim) % P == 0;
+    bool wide = P * esize == 16 && half % P == 0 && (head_dim - rot_dim) % P == 0;
     for (const void* g : {q_gain, k_gain}) wide = wide && (!g || bf1::aligned(g, 16));
     bf1::Side side[2];
     for (int i = 0; i < 2; ++i) {
@@ -600,7 +561,7 @@ int bf1_qk_norm_rope_bwd(const void* dQ, const void* dK, int32_t grad_type, cons
         wide = wide && bf1::wide_rows(side[i].dy, P, dsize) && bf1::wide_rows(side[i].x, P, esize) &&
                bf1::wide_rows(o, P, osize);
     }
-    const int32_t lshift = bf1::team_shift(head_dim, half, (int32_t)P);
+    const int32_t lshift = bf1::team_shift(head_dim, half, P);
     const bf1::BwdPlan plan = bf1::bwd_plan(rows, Hq, Hkv, lshift);
     side[0].chunk = plan.q_chunk;
     side[1].chunk = plan.k_chunk;
@@ -624,11 +585,14 @@ int bf1_qk_norm_rope_bwd(const void* dQ, const void* dK, int32_t grad_type, cons
         using T = decltype(x_c);
         using TD = decltype(d_c);
         using TO = decltype(out_c);
-        if (interleaved)
-            return wide ? go(bf1::norm_rope_bwd_kernel<T, TD, TO, true, true>)
-                        : go(bf1::norm_rope_bwd_kernel<T, TD, TO, true, false>);
-        return wide ? go(bf1::norm_rope_bwd_kernel<T, TD, TO, false, true>)
-                    : go(bf1::norm_rope_bwd_kernel<T, TD, TO, false, false>);
+        constexpr int N = 16 / sizeof(T);
+        auto way = [&](auto inter_c) {
+            constexpr bool I = decltype(inter_c)::value;
+            if (P != N) return go(bf1::norm_rope_bwd_kernel<T, TD, TO, I, false, 8>);
+            return wide ? go(bf1::norm_rope_bwd_kernel<T, TD, TO, I, true, N>)
+                        : go(bf1::norm_rope_bwd_kernel<T, TD, TO, I, false, N>);
+        };
+        return interleaved ? way(std::true_type{}) : way(std::false_type{});
     };
     auto outs = [&](auto x_c, auto d_c) {
         return out_type == BF1_TYPE_BF16 ? pick(x_c, d_c, (__bf16)0) : pick(x_c, d_c, 0.f);

@@ -155,6 +155,26 @@ def test_norm_rope_gradient_matches_the_oracle(batch, n, Hq, Hkv, d, r, dtype, i
             assert (np.abs(f64(dg) - want) <= bar).all(), np.abs(f64(dg) - want).max()
 
 
+@pytest.mark.parametrize("d,r", [(512, 2), (512, 12), (512, 508), (510, 4), (508, 2), (512, 8), (506, 2), (504, 252)])
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_norm_rope_of_wide_float32_rows(d, r, interleaved):
+    """Rows of four elements a lane and half that take all of a wave, or more than there is of
+    it: turning parts and tails that both leave a remainder.  The sums' chains are those of the
+    other rows, at most 16 elements of a lane and six moves."""
+    q, k, qg, kg, pos, freqs, f = case(2, 9, 3, 2, d, r, torch.float32)
+    for out in (None, torch.bfloat16):
+        got = bf1.qk_norm_rope(q, k, qg, kg, i32(pos), f, eps=1e-5, interleaved=interleaved, amplitude=1.139, dtype=out)
+        for x, y, g in zip((q, k), got, (qg, kg)):
+            check_forward(x, y, g, pos, freqs, interleaved, 1.139, 1e-5)
+        dq, dk = normal(5, *q.shape, dtype=torch.float32), normal(6, *k.shape, dtype=torch.float32)
+        got = bf1.qk_norm_rope_bwd(dq, dk, q, k, qg, kg, i32(pos), f, eps=1e-5, interleaved=interleaved, amplitude=1.139,
+                                   dtype=out)
+        for x, dy, g, dx, dg in zip((q, k), (dq, dk), (qg, kg), got[:2], got[2:]):
+            want, off, mag = check_backward(dy, x, g, pos, freqs, interleaved, 1.139, 1e-5, dx)
+            bar = off + (3 + 8 + 32 + 32) * U * mag + U * np.abs(want)  # three heads, teams of 32 lanes or more
+            assert (np.abs(f64(dg) - want) <= bar).all(), np.abs(f64(dg) - want).max()
+
+
 def test_norm_rope_gradient_by_differences():
     # the loss sum(w y) along a direction: the central difference in float32 at h = 2^-6 of
     # size-1 rows is off by h^2 / 6 times the third derivative (some 10 per row, times the
