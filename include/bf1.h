@@ -589,9 +589,14 @@ int bf1_kv_compact(void* K_pages, void* V_pages, const int32_t* accepted, int32_
  *
  * bf1_kv_copy: rows 0 .. copy_rows[i] - 1 (B at most) of K and V page copy_from[i] to page
  * copy_to[i], all heads, for i < count; entries outside the cache are left out.  No page is
- * copied to twice, or both to and from.  The tails of the 8-bit cache are such pages, too
- * (num_pages = batch): a place goes on inside the block that its source is writing, or from the
- * end of a full one; of a block that is complete no tail is left.
+ * copied to twice, or both to and from: the copies run at once.
+ *
+ * The 8-bit cache's tails belong to places, not to pages, so bf1_page_fork's lists are not for
+ * them: tail sources[b] goes to tail b wherever these differ, also where no page is copied.
+ * bf1_kv_copy does that (num_pages = batch) where no tail is both read and written, as for
+ * samples of one prompt; places that change about need copies of their tails first.  A place
+ * goes on inside the block that its source is writing, or from the end of a full one; of a
+ * block that is complete no tail is left.
  */
 int bf1_page_fork(int32_t batch, const int32_t* seq_lens, const int32_t* sources, const int32_t* keep_lens,
                   const int32_t* page_table, int32_t max_pages_per_seq, int32_t* shares, int32_t num_pages,

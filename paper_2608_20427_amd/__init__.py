@@ -1242,11 +1242,16 @@ def page_fork(seq_lens, sources, keep_lens, page_table, shares, free_pages, free
     free_pages, page_step's list with room for every page: pages that nobody holds any more
     go back below the head.  Full blocks are shared; a block that goes on being written
     stays with the first place that continues it, if nobody else holds its page, and is
-    copied for the others: kv_copy with the result's lists, for each layer's cache.  Of a
-    CacheQ8 the tails are copied instead, places as pages; there a sequence goes on inside
-    the block that its source is writing, or from the end of a full one.  Without a free page a sequence goes on without that
-    block's tokens.  To run the same call again (a warm-up before a capture, a retry), put
-    shares and free_pages back as they were first."""
+    copied for the others: kv_copy with the result's lists, for each layer's cache.  Without a
+    free page a sequence goes on without that block's tokens.  To run the same call again (a
+    warm-up before a capture, a retry), put shares and free_pages back as they were first.
+
+    A CacheQ8's tails belong to places, not to pages: instead of the result's lists, tail
+    sources[b] goes to tail b of every place, cache.k_tail.copy_(cache.k_tail[sources]) and
+    v_tail alike (for a place that ends, sources may name any).  kv_copy does it, tails as
+    pages, where no tail is both read and written (samples of one prompt; not places that
+    change about).  There a sequence goes on inside the block that its source is writing, or
+    from the end of a full one."""
     if out is None and stream is None:
         r = (_MARSHAL or _native()).page_fork(seq_lens, sources, keep_lens, page_table, shares, free_pages, free_head, B)
         if r is not None:
@@ -1278,7 +1283,8 @@ def page_fork(seq_lens, sources, keep_lens, page_table, shares, free_pages, free
 def kv_copy(k_pages, v_pages, copy_from, copy_to, copy_rows, stream=None):
     """Copy the first copy_rows[i] tokens of K and V page copy_from[i] to page copy_to[i]
     (int32 lists, page_fork's) in bf16 pages [num_pages, Hkv, B, d]; entries outside the
-    cache are left out.  No page is copied to twice, or both to and from."""
+    cache are left out.  No page is copied to twice, or both to and from: the copies run at
+    once."""
     if stream is None:
         r = (_MARSHAL or _native()).kv_copy(k_pages, v_pages, copy_from, copy_to, copy_rows)
         if r is not None:

@@ -236,6 +236,50 @@ def test_forked_8_bit_sequences():
     assert torch.equal(a, b) and pages_alone == 3 * 4 and pages == 2 + 3 * 2
 
 
+@pytest.mark.parametrize("sources,keep", [([1, 0, 0], [100, 150, 150]), ([2, 0, 1], [67, 140, 97]), ([1, -1, 2], [100, 0, 70]),
+                                          ([0, 0, 1], [128, 128, 65])])
+def test_8_bit_sequences_change_places(sources, keep):
+    """Places of the 8-bit cache that change with each other, follow each other round, end, or
+    go on from a full block: pages by page_fork, tails gathered, and each sequence decodes as if
+    it had always been there."""
+    B, L, Hq, Hkv, d, batch, lens0 = 64, 2, 4, 2, 64, 3, [150, 100, 70]
+    if 128 in keep:
+        lens0 = [128, 100, 70]
+    rows = [(normal(7 + b, n, Hkv, d), normal(17 + b, n, Hkv, d)) for b, n in enumerate(lens0)]
+
+    def serve(moved):
+        cache = bf1.cache_q8(40, batch, Hkv, d, B)
+        table = i32(np.full((batch, 8), -1))
+        shares, free, head = i32([0] * 40), i32(range(40)), i32([0])
+        lens = i32([0] * batch)
+
+        def step(new, k, v):
+            nonlocal head, lens
+            s = bf1.page_step(lens, i32(new), table, free, head, sum(new), B)
+            bf1.kv_append_q8(k, v, lens, s.seq_lens, s.token_start, s.block_start, table, cache)
+            lens, head = s.seq_lens, s.free_head
+
+        if moved:
+            step(lens0, *(torch.cat([r[i] for r in rows]) for i in (0, 1)))
+            f = bf1.page_fork(lens, i32(sources), i32(keep), table, shares, free, head)
+            lens, head = f.seq_lens, f.free_head
+            table.copy_(f.page_table)
+            for tail in (cache.k_tail, cache.v_tail):
+                tail.copy_(tail[torch.tensor(sources, device="cuda")])
+            assert lens.tolist() == keep
+        else:
+            step(keep, *(torch.cat([rows[s][i][:n] for s, n in zip(sources, keep)]) for i in (0, 1)))
+        out = []
+        for i in range(66):  # past the block's end: each sequence completes its own
+            step([1] * batch, normal(30 + i, batch, Hkv, d), normal(130 + i, batch, Hkv, d))
+            plan = bf1.decode_plan(lens, table, 40, bf1.decode_plan_stride(8 * B, B, L), B, L)
+            out.append(bf1.attn_decode_q8(normal(230 + i, batch, Hq, d), cache, lens, plan, B)[0].clone())
+        return torch.stack(out)
+
+    a, b = serve(False), serve(True)
+    assert a.isfinite().all() and torch.equal(a, b)
+
+
 def draft_steps(graph, steps=5):
     """Speculative decoding as a program runs it: trees of drafted tokens appended, normed and
     turned, verified, the accepted path kept, the rest taken back; one sequence starts again
