@@ -469,8 +469,8 @@ int bf1_decode_attn_q8(const void* Q, const void* K_pages, const void* V_pages, 
  *     forward   y = turn(x r gain)                 turn as bf1_rope's, with `amplitude`
  *     gradient  dn = the transposed turn of dy, u = dn gain,
  *               dx = r (u - x r mean(u x r)),  dgain = sum over rows of dn x r
- * Sums, the norm and the turn are fp32 (squares too: a row's elements lie below 2^59),
- * results are rounded once.
+ * A row's sums, the norm and the turn are fp32 (squares too: a row's elements lie below
+ * 2^59), the sums of dgain over rows are in 64 bits; results are rounded once.
  *   Q, K, positions, freqs, Q_out, K_out, interleaved, amplitude: as bf1_rope's; outputs
  *               may have any strides that write no element twice
  *   q_gain, k_gain : [head_dim] of gain_type, shared by the heads of a side; NULL: ones

@@ -9,11 +9,11 @@
 //
 //   dn = amplitude R^T dy,  u = dn g,  dx = r (u - n mean(u n)),  dg = sum over rows of dn n
 //
-// All sums and the turn are fp32, the result is rounded once.  Both are bound by
-// memory: a row is read once and written once, 16 bytes a lane and load.  Replays of a
-// graph: 32768 tokens of 16 + 8 heads of 128 from joined rows 91 us for 403 MB (4.4 TB/s; a
-// large copy reaches 5.0), 32 tokens 4.2; the gradient of 16382 such tokens from fp32
-// gradients 88 us for 403 MB, with the sums over workgroups, of 128 tokens 8.4.
+// A row's sums and the turn are fp32, the sum over rows is in 64 bits, results are rounded
+// once.  Both are bound by memory: a row is read once and written once, 16 bytes a lane and
+// load.  Replays of a graph: 32768 tokens of 16 + 8 heads of 128 from joined rows 89 us for 403
+// MB (4.5 TB/s; a large copy reaches 5.0), 32 tokens 4.1; the gradient of 16382 such tokens
+// from fp32 gradients 87 us for 403 MB, with the sums over workgroups, of 128 tokens 8.4.
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -238,21 +238,26 @@ __global__ __launch_bounds__(THREADS) void norm_rope_kernel(Side q, Side k, Shap
 // workgroups.  It keeps its sums of the gain's gradient in registers; at the end its teams
 // meet in LDS and write one record [d], which the next kernel sums over
 // the workgroups, in their order.  The records go by the call's sizes alone, so the
-// result is the same each time.
+// result is the same each time.  These sums, over every row of the call, are in 64 bits all the
+// way: fp32 sums were three times as far off (2e-7 of the gradient's size over 16382 tokens) and
+// no faster where memory bounds the call: us in replays, fp32 / 64 bits, of 16/8 heads of 128, 16382
+// tokens 87.8 / 86.7, from bf16 gradients 76.7 / 79.4, 1024 tokens 11.6 / 13.0.  Registers are held
+// to three waves a SIMD, which the compiler exceeds by itself (93.5 instead of 86.7).
 template <typename T, typename TD, typename TO, bool INTER, bool WIDE, int P>
-__global__ __launch_bounds__(THREADS) void norm_rope_bwd_kernel(Side q, Side k, Shape z, uint32_t q_groups,
+__global__ __launch_bounds__(THREADS, 3) void norm_rope_bwd_kernel(Side q, Side k, Shape z, uint32_t q_groups,
                                                                 float* __restrict__ q_dgain, float* __restrict__ k_dgain,
-                                                                float* __restrict__ records) {
-    __shared__ __align__(16) float part[THREADS * 2 * P];
+                                                                double* __restrict__ records) {
+    __shared__ double part[2 * P * (THREADS + 64)];
     const Lane x = lane_of<INTER, P>((int32_t)(threadIdx.x & ((1u << z.lshift) - 1)), z.d, z.half);
     const bool isk = blockIdx.x >= q_groups;
     const Side& w = isk ? k : q;
     const uint32_t me = isk ? blockIdx.x - q_groups : blockIdx.x, hop = isk ? gridDim.x - q_groups : q_groups;
     const uint32_t hsplit = (uint32_t)((w.heads + w.chunk - 1) / w.chunk);
     const uint32_t tiles = (z.items + THREADS - 1) / THREADS * hsplit;
-    float acc[2 * P], g[2 * P];
+    double acc[2 * P];
+    float g[2 * P];
 #pragma unroll
-    for (int e = 0; e < 2 * P; ++e) acc[e] = 0.f;
+    for (int e = 0; e < 2 * P; ++e) acc[e] = 0.;
     load_gain<P, WIDE>(w.gain, z.gain_f32, x, g);
     for (uint32_t tile = me; tile < tiles; tile += hop) {
         const uint32_t group = tile / hsplit;
@@ -279,7 +284,7 @@ __global__ __launch_bounds__(THREADS) void norm_rope_bwd_kernel(Side q, Side k, 
 #pragma unroll
             for (int e = 0; e < 2 * P; ++e) {
                 v[e] *= r;
-                acc[e] += live ? dy[e] * v[e] : 0.f;
+                acc[e] += (double)(live ? dy[e] * v[e] : 0.f);
                 dy[e] *= g[e];
                 along = fmaf(dy[e], v[e], along);
             }
@@ -291,35 +296,40 @@ __global__ __launch_bounds__(THREADS) void norm_rope_bwd_kernel(Side q, Side k, 
     }
     float* dgain = isk ? k_dgain : q_dgain;
     if (dgain == nullptr) return;
-    // Column c is element c % 2 P of a team's lane c / 2 P; a thread sums a column over the teams.
+    // Element e of all threads side by side, a team's width between two of them: no bank conflicts.
+    const int32_t team = 1 << z.lshift, step = THREADS + team;
 #pragma unroll
-    for (int e = 0; e < 2 * P; e += 4)
-        *reinterpret_cast<f32x4*>(part + threadIdx.x * 2 * P + e) = f32x4{acc[e], acc[e + 1], acc[e + 2], acc[e + 3]};
+    for (int e = 0; e < 2 * P; ++e) part[e * step + threadIdx.x] = acc[e];
     __syncthreads();
-    const int32_t cols = 2 * P << z.lshift;
-    for (int32_t c = threadIdx.x; c < cols; c += THREADS) {
-        float a = 0.f;
+    // A thread sums element e of lane l over the teams.
+    for (int32_t c = threadIdx.x; c < 2 * P * team; c += THREADS) {
+        const int32_t l = c & (team - 1), e = c >> z.lshift;
+        double a = 0.;
 #pragma unroll 8
-        for (int32_t at = c; at < THREADS * 2 * P; at += cols) a += part[at];
-        const Lane y = lane_of<INTER, P>(c / (2 * P), z.d, z.half);
-        const int32_t e = c % (2 * P), at = e < P ? y.a + e : y.b + e - P;
-        if (e < P ? e < y.na : e - P < y.nb) (records != nullptr ? records + (int64_t)blockIdx.x * z.d : dgain)[at] = a;
+        for (int32_t at = l; at < THREADS; at += team) a += part[e * step + at];
+        const Lane y = lane_of<INTER, P>(l, z.d, z.half);
+        const int32_t at = e < P ? y.a + e : y.b + e - P;
+        if (e < P ? e >= y.na : e - P >= y.nb) continue;
+        if (records != nullptr)
+            records[(int64_t)blockIdx.x * z.d + at] = a;
+        else
+            dgain[at] = (float)a;
     }
 }
 
 // The gains' gradients from the workgroups' records, the first q_groups of them Q's: 32
 // columns a workgroup, 32 threads each.
 constexpr int SUM_THREADS = 1024, SUM_COLS = 32;
-__global__ __launch_bounds__(SUM_THREADS) void gain_sum_kernel(const float* __restrict__ records, int32_t q_groups,
+__global__ __launch_bounds__(SUM_THREADS) void gain_sum_kernel(const double* __restrict__ records, int32_t q_groups,
                                                                int32_t groups, int32_t d, float* __restrict__ q_dgain,
                                                                float* __restrict__ k_dgain) {
     constexpr int PER = SUM_THREADS / SUM_COLS;
-    __shared__ float part[PER][SUM_COLS];
+    __shared__ double part[PER][SUM_COLS];
     float* out = blockIdx.y ? k_dgain : q_dgain;
     if (out == nullptr) return;
     const int32_t col = blockIdx.x * SUM_COLS + threadIdx.x % SUM_COLS, r0 = threadIdx.x / SUM_COLS;
     const int32_t begin = blockIdx.y ? q_groups : 0, end = blockIdx.y ? groups : q_groups;
-    float a = 0.f;
+    double a = 0.;
     if (col < d) {
 #pragma unroll 8
         for (int32_t r = begin + r0; r < end; r += PER) a += records[(int64_t)r * d + col];
@@ -327,10 +337,10 @@ __global__ __launch_bounds__(SUM_THREADS) void gain_sum_kernel(const float* __re
     part[r0][threadIdx.x % SUM_COLS] = a;
     __syncthreads();
     if (r0 != 0 || col >= d) return;
-    a = 0.f;
+    a = 0.;
 #pragma unroll
     for (int r = 0; r < PER; ++r) a += part[r][threadIdx.x];
-    out[col] = a;
+    out[col] = (float)a;
 }
 
 // A dimension's stride where it is used: one with a single entry may have any.
@@ -372,7 +382,7 @@ BwdPlan bwd_plan(int64_t rows, int32_t Hq, int32_t Hkv, int32_t lshift) {
 
 // None where each side is one workgroup, which then writes the result.
 int64_t record_bytes(const BwdPlan& p, int32_t d) {
-    return p.q_groups == 1 && p.groups == 2 ? 0 : (int64_t)p.groups * d * 4;
+    return p.q_groups == 1 && p.groups == 2 ? 0 : (int64_t)p.groups * d * 8;
 }
 
 // Sizes that forward, backward and workspace refuse the same way; BF1_OK with *rows == 0
@@ -575,9 +585,9 @@ int bf1_qk_norm_rope_bwd(const void* dQ, const void* dK, int32_t grad_type, cons
                        head_dim, half, lshift, gain_type == BF1_TYPE_F32, eps, amplitude, 1.f / (float)head_dim};
     auto go = [&](auto kern) {
         hipLaunchKernelGGL(kern, dim3((unsigned)plan.groups), dim3(bf1::THREADS), 0, stm, side[0], side[1], z,
-                           (uint32_t)plan.q_groups, dq_gain, dk_gain, sums ? (float*)workspace : nullptr);
+                           (uint32_t)plan.q_groups, dq_gain, dk_gain, sums ? (double*)workspace : nullptr);
         if (sums)
-            hipLaunchKernelGGL(bf1::gain_sum_kernel, sum_groups, dim3(bf1::SUM_THREADS), 0, stm, (const float*)workspace,
+            hipLaunchKernelGGL(bf1::gain_sum_kernel, sum_groups, dim3(bf1::SUM_THREADS), 0, stm, (const double*)workspace,
                                plan.q_groups, plan.groups, head_dim, dq_gain, dk_gain);
         return bf1::status_of(hipGetLastError());
     };

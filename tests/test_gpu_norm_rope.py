@@ -175,6 +175,35 @@ def test_norm_rope_of_wide_float32_rows(d, r, interleaved):
             assert (np.abs(f64(dg) - want) <= bar).all(), np.abs(f64(dg) - want).max()
 
 
+@pytest.mark.parametrize("batch,n,Hq,Hkv,d,r,dtype", [(1, 30, 1, 1, 128, 128, torch.bfloat16), (2, 300, 4, 2, 64, 16, torch.bfloat16),
+                                                      (1, 700, 5, 2, 128, 64, torch.float32), (1, 260, 2, 1, 512, 2, torch.float32),
+                                                      (1, 33000, 1, 1, 128, 128, torch.bfloat16),
+                                                      (1, 16500, 2, 1, 128, 32, torch.float32)])
+def test_gains_gradient_is_summed_in_64_bits(batch, n, Hq, Hkv, d, r, dtype):
+    """Rows of +-1 (their norm is 1) at position 0 with gradients that are whole numbers: each
+    row's share is one, below 2^24, and a sum in 64 bits is exact.  The large ones cancel, wherever
+    they lie: what is left is a number that float32 holds, and has to be equal.  One workgroup a
+    side, several, and more tiles than workgroups."""
+    f = torch.ones(r // 2, dtype=torch.float64, device="cuda")
+    pos, gain = i32([0] * n), torch.ones(d, device="cuda")
+    sides, want = [], []
+    for i, heads in enumerate((Hq, Hkv)):
+        g = torch.Generator().manual_seed(i)
+        rows = batch * heads * n
+        share = torch.randint(-2 ** 23, 2 ** 23, (rows, d), generator=g)
+        share[rows - rows // 2:] = -share[:rows // 2][torch.randperm(rows // 2, generator=g)]
+        if rows % 2:
+            share[rows // 2] = 0
+        share += torch.randint(-3, 4, (rows, d), generator=g)
+        x = 2 * torch.randint(0, 2, (rows, d), generator=g) - 1
+        want.append(share.sum(0))
+        assert want[-1].abs().max() < 2 ** 24
+        sides.append([t.view(batch, heads, n, d).cuda() for t in ((share * x).float(), x.to(dtype))])
+    (dq, q), (dk, k) = sides
+    _, _, dqg, dkg = bf1.qk_norm_rope_bwd(dq, dk, q, k, gain, gain, pos, f, eps=1e-30)
+    assert torch.equal(dqg.cpu().double(), want[0].double()) and torch.equal(dkg.cpu().double(), want[1].double())
+
+
 def test_norm_rope_gradient_by_differences():
     # the loss sum(w y) along a direction: the central difference in float32 at h = 2^-6 of
     # size-1 rows is off by h^2 / 6 times the third derivative (some 10 per row, times the
