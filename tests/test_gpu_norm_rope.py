@@ -204,6 +204,33 @@ def test_gains_gradient_is_summed_in_64_bits(batch, n, Hq, Hkv, d, r, dtype):
     assert torch.equal(dqg.cpu().double(), want[0].double()) and torch.equal(dkg.cpu().double(), want[1].double())
 
 
+@pytest.mark.parametrize("tokens,batch,n,Hq,Hkv,d,r,dtype", [(True, 1, 33000, 1, 1, 128, 128, torch.bfloat16),
+                                                            (False, 2, 16500, 3, 1, 128, 64, torch.bfloat16),
+                                                            (False, 1, 16500, 1, 1, 128, 128, torch.float32),
+                                                            (True, 1, 41, 6, 2, 128, 128, torch.bfloat16),
+                                                            (True, 1, 333, 3, 1, 80, 20, torch.float32)])
+def test_norm_rope_gradient_of_packed_and_of_many_rows(tokens, batch, n, Hq, Hkv, d, r, dtype):
+    """Gradients of packed rows [tokens, heads, d], parts of joined ones, and of so many rows
+    that a workgroup goes over several tiles (more than 2048 of them), gains included: their
+    sums, in 64 bits, add half a step to what the rows' own errors come to."""
+    freqs = list(1e6 ** (-np.arange(0, r, 2) / r))
+    f = torch.tensor(freqs, dtype=torch.float64, device="cuda")
+    pos = np.random.default_rng(n).integers(0, 100000, n if tokens else (batch, n)).astype(np.int32)
+    gains = [1 + 0.3 * normal(s, d, dtype=torch.float32) for s in (3, 4)]
+    if tokens:
+        joined = normal(1, n, Hq + Hkv + 1, d, dtype=dtype)
+        x = joined[:, :Hq], joined[:, Hq:Hq + Hkv]
+        dy = normal(5, n, Hq + 1, d, dtype=torch.float32)[:, 1:], normal(6, n, Hkv, d, dtype=torch.float32)
+    else:
+        x = normal(1, batch, Hq, n, d, dtype=dtype), normal(2, batch, Hkv, n, d, dtype=dtype)
+        dy = tuple(normal(5 + i, *t.shape, dtype=torch.float32) for i, t in enumerate(x))
+    got = bf1.qk_norm_rope_bwd(*dy, *x, *gains, i32(pos), f, amplitude=1.139)
+    for a, b, g, dx, dg in zip(x, dy, gains, got[:2], got[2:]):
+        assert dx.shape == a.shape and dx.is_contiguous()
+        want, off, _ = check_backward(b, a, g, pos, freqs, False, 1.139, 1e-6, dx, tokens=tokens)
+        assert (np.abs(f64(dg) - want) <= off + U * (np.abs(want) + off)).all(), np.abs(f64(dg) - want).max()
+
+
 def test_norm_rope_gradient_by_differences():
     # the loss sum(w y) along a direction: the central difference in float32 at h = 2^-6 of
     # size-1 rows is off by h^2 / 6 times the third derivative (some 10 per row, times the
