@@ -896,10 +896,13 @@ hipError_t launch(const Tree& a, hipStream_t s) {
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.nsplit <= 1) return e;
     const dim3 grid(COLS / (THREADS / (D / 4)), (unsigned)a.groups, (unsigned)(a.batch * a.Hkv));
-    if (a.slots > 0)
-        hipLaunchKernelGGL((merge_tree_kernel<D, G, COLS, true>), grid, dim3(THREADS), 0, s, a);
-    else
-        hipLaunchKernelGGL((merge_tree_kernel<D, G, COLS, false>), grid, dim3(THREADS), 0, s, a);
+    if constexpr (CW > 1) {
+        if (a.slots > 0) {
+            hipLaunchKernelGGL((merge_tree_kernel<D, G, COLS, true>), grid, dim3(THREADS), 0, s, a);
+            return hipGetLastError();
+        }
+    }
+    hipLaunchKernelGGL((merge_tree_kernel<D, G, COLS, false>), grid, dim3(THREADS), 0, s, a);
     return hipGetLastError();
 }
 
@@ -999,13 +1002,11 @@ int bf1_attn_tree(const void* Q, const void* K_pages, const void* V_pages, const
     hipStream_t s = (hipStream_t)stream;
     auto nt = [&](auto d_c, auto g_c, auto pw_c) {
         constexpr int D = decltype(d_c)::value, GG = decltype(g_c)::value, PW = decltype(pw_c)::value;
-        switch (p.cols) {
-            case 16: return bf1::launch<D, GG, PW, 1, 1, 4>(a, s);
-            case 32: return bf1::launch<D, GG, PW, 2, 1, 4>(a, s);
-            case 64:
-                return p.waves == 8 ? bf1::launch<D, GG, PW, 2, 2, 8>(a, s) : bf1::launch<D, GG, PW, 2, 2, 4>(a, s);
-            default: return bf1::launch<D, GG, PW, 2, 4, 4>(a, s);
-        }
+        if (p.cols == 16) return bf1::launch<D, GG, PW, 1, 1, 4>(a, s);
+        if (p.cols == 32) return bf1::launch<D, GG, PW, 2, 1, 4>(a, s);
+        if constexpr (GG > 1)  // one head a group has 64 columns at most
+            if (p.cols == 128) return bf1::launch<D, GG, PW, 2, 4, 4>(a, s);
+        return p.waves == 8 ? bf1::launch<D, GG, PW, 2, 2, 8>(a, s) : bf1::launch<D, GG, PW, 2, 2, 4>(a, s);
     };
     auto pw = [&](auto d_c, auto g_c) {
         return B == 64 ? nt(d_c, g_c, std::integral_constant<int, 64>{}) : nt(d_c, g_c, std::integral_constant<int, 128>{});

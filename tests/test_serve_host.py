@@ -3,6 +3,7 @@ oracle, workspace sizes, and refusals by the library (before any device call) an
 binding (before any pointer is taken)."""
 
 import ctypes
+import re
 
 import numpy as np
 import pytest
@@ -228,6 +229,20 @@ def test_page_refusals(lib):
                      ({7: 1 << 24, 10: 1 << 10}, UNSUPPORTED)]:
         assert lib.bf1_kv_compact(*_with(ok, at)) == want, at
     assert lib.bf1_kv_compact(*_with(ok, {7: 0, 0: None})) == bf1.BF1_OK
+
+
+def test_kernels_of_trees_are_those_that_calls_reach():
+    """64 nodes of groups of one head are 64 columns: none run 128; and lists are dealt by length
+    (a merge that looks up slots) at 64 columns or more."""
+    with open(bf1.lib_path(), "rb") as f:
+        names = f.read()
+    kernels = {tuple(map(int, m)) for m in re.findall(
+        rb"attn_tree_kernelILi(\d+)ELi(\d+)ELi(\d+)ELi(\d+)ELi(\d+)ELi(\d+)E", names)}
+    assert kernels == {(d, g, B, nt, cw, waves) for d in (64, 128) for g in (1, 2, 4, 8) for B in (64, 128)
+                       for nt, cw, waves in ((1, 1, 4), (2, 1, 4), (2, 2, 4), (2, 2, 8), (2, 4, 4)) if g > 1 or cw < 4}
+    merges = {tuple(map(int, m)) for m in re.findall(rb"merge_tree_kernelILi(\d+)ELi(\d+)ELi(\d+)ELb(\d)E", names)}
+    assert merges == {(d, g, cols, slots) for d in (64, 128) for g in (1, 2, 4, 8) for cols in (16, 32, 64, 128)
+                      for slots in (0, 1) if (g > 1 or cols < 128) and (cols >= 64 or not slots)}
 
 
 # ---- refusals of the binding -----------------------------------------------------------
