@@ -514,7 +514,8 @@ int bf1_qk_norm_rope_bwd(const void* dQ, const void* dK, int32_t grad_type, cons
  *   seq_lens  : [batch] int32, the lengths with the drafted tokens (bf1_page_step's): nodes
  *               past them have no place
  *   masks     : [rows] int64, bit k of a row: node k is the node or one before it
- *   positions : [rows] int32, for bf1_rope or bf1_qk_norm_rope, too
+ *   positions : [rows] int32, for bf1_rope or bf1_qk_norm_rope, too; both are buffers of
+ *               their own
  * Rows behind the last tree, of nodes without a place and past the 64th: mask 0, position -1.
  * Up to 2^30 rows.
  *

@@ -932,10 +932,12 @@ int bf1_tree_step(const int32_t* parents, const int32_t* token_start, const int3
     if (rows > bf1::MOST_ROWS || batch > (1 << 24)) return BF1_ERR_UNSUPPORTED;
     if (rows == 0) return BF1_OK;
     if (!bf1::aligned(parents, 4) || !bf1::aligned(masks, 8) || !bf1::aligned(positions, 4)) return BF1_ERR_INVALID_ARG;
-    if (positions == parents) return BF1_ERR_INVALID_ARG;
+    // a tree's rows are written while another's parents and lengths are read
+    const void* const m = masks;
+    if (positions == parents || m == parents || m == positions) return BF1_ERR_INVALID_ARG;
     if (batch > 0)
         for (const int32_t* p : {token_start, seq_lens_before, seq_lens})
-            if (!bf1::aligned(p, 4) || p == positions) return BF1_ERR_INVALID_ARG;
+            if (!bf1::aligned(p, 4) || p == positions || p == m) return BF1_ERR_INVALID_ARG;
     // a wave per tree, and at least one for the rows behind them
     hipLaunchKernelGGL(bf1::tree_step_kernel, dim3((unsigned)(batch / (bf1::THREADS / 64) + 1)), dim3(bf1::THREADS), 0,
                        (hipStream_t)stream, parents, token_start, seq_lens_before, seq_lens, batch, (int32_t)rows,

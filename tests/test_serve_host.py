@@ -178,6 +178,15 @@ def test_tree_step_refusals(lib):
     assert lib.bf1_tree_step(*_with(ok, {5: 0, 0: None})) == bf1.BF1_OK
 
 
+def test_tree_step_writes_buffers_of_its_own(lib):
+    """Masks over what other trees' waves still read, or over the positions."""
+    ok = [FAKE, FAKE + 64, FAKE + 128, FAKE + 192, 3, 20, FAKE + 4096, FAKE + 8192, None]
+    for over in (0, 1, 2, 3, 7):
+        assert lib.bf1_tree_step(*_with(ok, {6: ok[over]})) == INVALID, over
+        if over < 7:
+            assert lib.bf1_tree_step(*_with(ok, {7: ok[over]})) == INVALID, over
+
+
 def test_attn_tree_refusals(lib):
     ok = [FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, 900, 7, FAKE + 4096, FAKE + 8192, 3, 20, 16, 16, 8, 128, 64, 2, 0, FAKE,
           1 << 40, None]
