@@ -1151,9 +1151,10 @@ def attn_tree(q, k_pages, v_pages, masks, positions, lens_before, token_start, p
     q: [rows, Hq, d] bf16, packed; masks, positions: tree_step's, or any masks; lens_before:
     the lengths without the drafted tokens; token_start: page_step's.  A node at position
     p reads the committed keys of the blocks on the BF1 route of block p // B (dense: of
-    every block up to it) and the drafted ones of its mask.  max_nodes: the largest tree of
-    the call, 1 to 64; rows past it get NaN, as do those without a place and those of a
-    sequence that lacks a page.  Rows behind the last tree are left as they are."""
+    every block up to it) and the drafted ones of its mask; as in the decodes, weights are
+    applied with their 24 bits.  max_nodes: the largest tree of the call, 1 to 64; rows past
+    it get NaN, as do those without a place and those of a sequence that lacks a page.  Rows
+    behind the last tree are left as they are."""
     if out is None and lse is None and workspace is None and stream is None:
         r = (_MARSHAL or _native()).attn_tree(q, k_pages, v_pages, masks, positions, lens_before, token_start, page_table, B,
                                               L, dense, max_nodes)

@@ -351,7 +351,7 @@ int64_t used(int64_t stride, int64_t entries) { return entries > 1 ? stride : 0;
 // every pair) and serve all of them; in equal parts.  us, 16 + 8 heads of 128, forward with 1 /
 // 2 / 4 / 8 / 12 / 24 heads: 1024 tokens 6.8 / 7.5 / 7.6 / 12 / 15 / 25, 4096 21 / 17 / 15 / 18 /
 // 21 / 35, 32768 152 / 118 / 99 / 91 / 89 / 93; gradient with 1 / 2 / 4 / 8 / 16 of a side: 2048
-// tokens 31 / 21 / 23 / 27 / 41, 16382 139 / 125 / 115 / 108 / 89.
+// tokens 25 / 18 / 19 / 24 / 37, 16382 133 / 115 / 108 / 93 / 87.
 int32_t heads_each(int64_t groups, int32_t heads, int32_t all, int32_t most) {
     if (heads == 0) return 1;
     const int64_t c = std::min<int64_t>(std::max<int64_t>(groups * all / 768, 1), std::min(most, heads));

@@ -574,8 +574,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_tree_kernel(Tree a) {
     } else {
         // A tile is asked for a turn ahead, a load here and there among the products of the one
         // before it: all at once, behind the barrier, they kept the waves from their LDS reads
-        // (eight lists of 32K, 64 nodes in groups of 8, one workgroup a compute unit 1260 us,
-        // now 940; two 440, 430).  Where there is none any more the loads read nothing.
+        // (eight lists of 32K, 64 nodes in groups of 8, one workgroup a compute unit 621 us,
+        // now 568; two 496, 487).  Where there is none any more the loads read nothing.
         const int turns = max(0, (units - s * KW + hop - 1) / hop);  // of every key group, the last one maybe without keys
         auto ahead = [&](int u) {
             Where w = where(min(u, units - 1), page_of(min(u, units - 1)));
@@ -839,25 +839,25 @@ __global__ __launch_bounds__(THREADS) void merge_tree_kernel(Tree a) {
 // Columns of a workgroup: 16 for little work, where a short path counts, 32 to 128 for more,
 // where a key row should serve many columns.  Work: 16-column tiles times 32-key tiles.  us in
 // replays of a graph, 16 / 32 / 64 / 128 columns with their best splits, 64 nodes, heads of 128 in
-// groups of 2: sequences of 32K on the route, trees that cross a block, one (work 1500) 14.0 / 16.3
-// / 17.7 / 20.8, four (6100) 18.9 / 20.5 / 21.4 / 24.8, eight (12300) 30.1 / 24.8 / 25.8 / 28.0,
-// sixteen (25000) 55.5 / 35.0 / 30.7 / 38.8; dense lists of 8100, one (16400) 31.3 / 26.5 / 27.4 /
-// 34.1, four (66000) 83.8 / 53.8 / 47.1 / 47.2, eight (131000) 160 / 98 / 79.3 / 76.0.
+// groups of 2: sequences of 32K on the route, trees that cross a block, one (work 1500) 13.6 / 16.2
+// / 17.9 / 21.3, four (6100) 18.8 / 21.3 / 21.5 / 25.0, eight (12300) 30.3 / 25.9 / 26.2 / 29.0,
+// sixteen (25000) 55.2 / 35.7 / 32.2 / 42.0; dense lists of 8100, one (16400) 31.2 / 27.7 / 27.9 /
+// 34.5, four (66000) 82.5 / 54.8 / 51.8 / 54.8, eight (131000) 152 / 101 / 93.4 / 82.9.
 //
 // Splits fill 256 workgroups, one a compute unit; 128 columns over long lists 512 (eight
-// lists of 32K, 64 nodes in groups of 8: 475 / 290).  64 columns run as workgroups of eight
+// lists of 32K, 64 nodes in groups of 8: 568 / 487).  64 columns run as workgroups of eight
 // waves, four key groups, where there are no more than 256 of them (32 sequences of 32K, 32 nodes
-// in groups of 2 34.0, with four waves 40.8; 64 sequences 72.7 and 62.0).  Up to 32 columns are not
-// split where that would take fewer than twelve tiles off a workgroup's list, for the merge is a
-// launch.  16 nodes, unsplit / in splits: one sequence of 100 tokens 6.7 / 8.3, of 32K 12.3 / 11.1
-// and, crossing a block, 16.9 / 12.7; four of 700 11.4 / 11.7, of 8K 11.3 / 11.8 and 14.9 / 12.5;
-// eight of 8K 11.4 / 13.2 and 16.2 / 15.2, of 32K 13.0 / 13.4 and 19.1 / 17.2.  Eight waves in an
-// unsplit workgroup of 16 columns are no faster (eight of 8K 11.5, of 32K 13.7).
+// in groups of 2 25.9, with four waves 28.9, and crossing a block 34.6 and 42.0; 64 sequences 49.6
+// and 39.5).  Up to 32 columns are not split where that would take fewer than twelve tiles off a
+// workgroup's list, for the merge is a launch.  16 nodes, unsplit / in splits: one sequence of 100
+// tokens 6.7 / 8.2, of 32K 12.5 / 11.1; four of 700 11.7 / 11.8, of 8K 11.6 / 11.9 and, crossing a
+// block, 15.2 / 12.3; eight of 8K 11.6 / 13.3 and 16.2 / 15.5, of 32K 13.4 / 13.5.  Eight waves in
+// an unsplit workgroup of 16 columns are no faster.
 //
 // Dense lists of up to 64 sequences that run 64 or 128 columns and are split have as many splits in
 // all, but each sequence its share (share_of).  Heads of 128, 64 nodes in groups of 8, equal splits /
-// shares: one list of 32K among seven of 1K 247 / 93, lists of 32K, 16K, .. 250 248 / 129, eight of 18
-// to 32K with 32 to 64 nodes 275 / 267, eight of 32K 406 / 409; in groups of 2, eight of 8K 76.4 / 79.0.
+// shares: one list of 32K among seven of 1K 292 / 103, lists of 32K, 16K, .. 250 294 / 152, eight of 18
+// to 32K 361 / 362, eight of 32K 482 / 501; in groups of 2, eight of 8K 90.6 / 92.3.
 struct Plan {
     int32_t cols, groups, waves, nsplit, slots;
     int64_t bytes;
