@@ -1248,11 +1248,11 @@ def page_fork(seq_lens, sources, keep_lens, page_table, shares, free_pages, free
     warm-up before a capture, a retry), put shares and free_pages back as they were first.
 
     A CacheQ8's tails belong to places, not to pages: instead of the result's lists, tail
-    sources[b] goes to tail b of every place, cache.k_tail.copy_(cache.k_tail[sources]) and
-    v_tail alike (for a place that ends, sources may name any).  kv_copy does it, tails as
-    pages, where no tail is both read and written (samples of one prompt; not places that
-    change about).  There a sequence goes on inside the block that its source is writing, or
-    from the end of a full one."""
+    sources[b] goes to tail b of every place,
+    cache.k_tail.copy_(cache.k_tail[sources.clamp(0, batch - 1)]) and v_tail alike (a place that
+    ends may get any).  kv_copy does it, tails as pages, where no tail is both read and written
+    (samples of one prompt; not places that change about).  There a sequence goes on inside the
+    block that its source is writing, or from the end of a full one."""
     if out is None and stream is None:
         r = (_MARSHAL or _native()).page_fork(seq_lens, sources, keep_lens, page_table, shares, free_pages, free_head, B)
         if r is not None:
